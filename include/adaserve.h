@@ -22,7 +22,13 @@
  *   adaserve_select_trees      (before the pass) the two selection phases that
  *                              turn candidate trees into the draft trees;
  *   adaserve_beam_step         (before selection) one beam-search step of the
- *                              speculation phase that grows the candidate trees.
+ *                              speculation phase that grows the candidate trees;
+ * and what a request needs before and beside speculation:
+ *   adaserve_rope_append_kv    rotary embedding of q and k, and the keys and
+ *                              values written into the paged cache;
+ *   adaserve_prompt_attn       causal attention of packed prompts over it;
+ *   adaserve_decode_attn       attention of one new token per request;
+ *   adaserve_sample            a token per row by temperature, top-k, top-p, min-p.
  *
  * Conventions for every entry point:
  *  - Pointers without a _host suffix are DEVICE pointers owned by the caller;
@@ -426,6 +432,157 @@ int32_t adaserve_tree_accept_sampled(int32_t num_requests, int32_t total_nodes,
                                      int32_t max_accept, int32_t *accept_len,
                                      int32_t *accept_tokens, int32_t *accept_nodes,
                                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The serving operators below fill the paged cache that the verification pass
+ * reads and serve a request where it does not speculate: its prompt, and its
+ * single tokens.  Conventions, error codes and cache layouts are those above.
+ * Token packing: request r owns the token rows [token_indptr[r],
+ * token_indptr[r+1]), of any number, 0 among them; rows past the last request's
+ * (padding of a batch) are neither read nor written.
+ */
+
+/*
+ * Rotary position embedding of queries and keys, and the append of keys and
+ * values to the paged cache (what makes the post-RoPE q, k_tree and prefix
+ * keys of the attention calls).
+ *
+ * Token i of request r stands at cache position place = prefix_len[r] + i and
+ * is rotated by the angles p * inv_freq[j], j < rotary_dim / 2, where p is
+ * positions[t] of its row t, or place where positions is NULL.  Pair j of a
+ * head is columns (j, j + rotary_dim / 2), or (2j, 2j + 1) with interleaved = 1:
+ *   y1 = x1 cos - x2 sin,  y2 = x1 sin + x2 cos;
+ * columns from rotary_dim on are copied.  The angle is exact (fp64) at any
+ * position, sine, cosine and rotation are fp32, rounded once to dtype.
+ *
+ *   q [num_tokens, Hq, D], k, v [num_tokens, Hkv, D]: heads dense, rows
+ *     *_row_stride elements apart (slices of one projection's rows can be given
+ *     as they are);
+ *   q_out [num_tokens, Hq, D], k_out [num_tokens, Hkv, D]: dense rotated rows;
+ *     q_out may be q and k_out may be k where those are dense.  q and q_out may
+ *     both be NULL; k_out may be NULL when there are pages.
+ *   k_pages, v_pages [num_pages, Hkv, page_size, D]: rotated keys, and values
+ *     bit for bit, go to page block_table[r][place / page_size], slot
+ *     place % page_size.  Both NULL: nothing is appended (nodes of draft trees:
+ *     positions = prefix length + depth), and v is not read.
+ *   new_prefix_len [num_requests] int32 (required with pages, NULL without):
+ *     prefix_len[r] + the leading rows whose page lies in the block-table row
+ *     and in [0, num_pages).  A row whose page does not is not stored; rows
+ *     after it whose page does are.  prefix_len[r] < 0 stores nothing and is
+ *     kept.  May be the prefix_len array itself (a second, small launch).
+ *
+ * Every place belongs to one token: requests that share pages must not append
+ * to them in one call.  dtype F32 or BF16; head_dim * element size a multiple
+ * of 16 bytes, head_dim <= 512; rotary_dim * element size a multiple of 32
+ * bytes (0: plain append, inv_freq may be NULL); page_size >= 1; at most 4096
+ * heads of a kind.  num_requests = 0 is a no-op.
+ */
+int32_t adaserve_rope_append_kv(int32_t num_requests, int32_t num_tokens, const int32_t *token_indptr,
+                                const int32_t *prefix_len, const int32_t *positions, const void *q,
+                                int64_t q_row_stride, const void *k, int64_t k_row_stride, const void *v,
+                                int64_t v_row_stride, const float *inv_freq, int32_t rotary_dim,
+                                int32_t interleaved, int32_t num_q_heads, int32_t num_kv_heads,
+                                int32_t head_dim, int32_t page_size, int32_t dtype, void *q_out,
+                                void *k_out, void *k_pages, void *v_pages, int32_t num_pages,
+                                const int32_t *block_table, int32_t block_table_stride,
+                                int32_t *new_prefix_len, void *stream);
+
+/*
+ * Causal attention of packed prompts, or of a chunk of each, over the paged
+ * cache that already holds their keys and values (adaserve_rope_append_kv).
+ *
+ * Request r has n = token_indptr[r+1] - token_indptr[r] rows and c =
+ * context_len[r] cached keys, its own rows' among them (the length after the
+ * append).  Row i stands at position c - n + i and attends to positions
+ * 0 .. c - n + i, with scores sm_scale * <q, k> and head groups as in
+ * adaserve_tree_attn_verify.  A row whose position is negative (c < n) sees
+ * nothing and its output is 0.  Layouts: q [T, Hq, D] with rows q_row_stride
+ * elements apart, out [T, Hq, D] dense, T = token_indptr[num_requests];
+ * k_pages, v_pages, block_table, types, head dims, page size and scales as in
+ * adaserve_tree_attn_verify, and BF16 rounds as described there.  Slots past c
+ * are never read into the result; a key that a row does not see adds nothing to
+ * it, whatever key and value it holds.
+ * Block-table entries outside [0, num_pages) are all-zero pages.
+ * token_indptr_host and context_len_host mirror the device arrays.  T * Hq <
+ * 2^31.  workspace: at least adaserve_prompt_attn_workspace_bytes(...) bytes
+ * (0 for most batches; 256-byte aligned, no initialisation needed); calls that
+ * share one must not overlap in time.
+ */
+size_t adaserve_prompt_attn_workspace_bytes(int32_t num_requests, const int32_t *token_indptr_host,
+                                            const int32_t *context_len_host, int32_t num_q_heads,
+                                            int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                                            int32_t dtype);
+
+int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr,
+                             const int32_t *token_indptr_host, const void *q, int64_t q_row_stride,
+                             const void *k_pages, const void *v_pages, int32_t num_pages,
+                             const int32_t *block_table, int32_t block_table_stride,
+                             const int32_t *context_len, const int32_t *context_len_host,
+                             int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                             int32_t page_size, float sm_scale, int32_t dtype, void *out,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention of one new token per request over its paged cache: row r of q
+ * [num_requests, Hq, D] attends to positions 0 .. context_len[r] - 1 (its own
+ * key among them), as adaserve_prompt_attn with one row per request.  The
+ * lengths are read on the device only, so a captured call serves a batch whose
+ * lengths grow: max_context bounds them (a bound well above them costs little).
+ * context_len[r] = 0 (padding of a batch) gives an output of 0; a length
+ * outside [0, max_context] gives NaN.  The caches are split over their length
+ * where the batch alone would not fill the device, and joined by a second
+ * launch.  workspace: at least adaserve_decode_attn_workspace_bytes(...) bytes
+ * (it depends on sizes, not on lengths; 256-byte aligned, no initialisation
+ * needed); calls that share one must not overlap in time.  num_requests * Hq <
+ * 2^31.
+ */
+size_t adaserve_decode_attn_workspace_bytes(int32_t num_requests, int32_t max_context,
+                                            int32_t num_q_heads, int32_t num_kv_heads,
+                                            int32_t head_dim, int32_t page_size, int32_t dtype);
+
+int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_stride,
+                             const void *k_pages, const void *v_pages, int32_t num_pages,
+                             const int32_t *block_table, int32_t block_table_stride,
+                             const int32_t *context_len, int32_t max_context, int32_t num_q_heads,
+                             int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                             float sm_scale, int32_t dtype, void *out, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+/*
+ * One token per row of logits by temperature, top-k, top-p and min-p, from a
+ * given uniform number (the first token after a prompt, and every token of a
+ * request that does not speculate; the greedy counterpart is
+ * adaserve_node_argmax).
+ *
+ * logits [num_rows, row_stride] of dtype, columns 0 .. vocab - 1, of any
+ * alignment to the element.  temperature, top_p, min_p, u [num_rows] fp32,
+ * top_k [num_rows] int32 (device); each but u may be NULL: 1, off, off, off.
+ * With z = (x - max) / temperature, a token's mass is the whole number
+ * W = round(2^32 exp(z)), computed in fp64: a token below 2^-33 of the
+ * likeliest has none.  Tokens are ranked by logit (higher first; +0 == -0),
+ * equal ones by index.  Then, in this order:
+ *   top_k = k in [1, vocab) keeps the first k (other values: all);
+ *   top_p = p < 1 keeps of them those whose predecessors' mass is below
+ *     p * (their whole mass) (fp64 product);
+ *   min_p = m > 0 keeps of them those with W >= m * 2^32;
+ * the first token is always kept (m > 1 or p <= 0 leave it alone).  The token
+ * is the first, in index order, whose cumulative kept mass exceeds u * (the
+ * kept mass) (fp64 product); u >= 1 takes the last that has mass, u < 0 counts
+ * as 0.  temperature = 0 takes the first-ranked token.  Sums of masses are
+ * exact, so results depend on no order of summation.
+ * out_token [num_rows] int32; -1 for a row with a NaN or +inf logit or with no
+ * logit above -inf, with a temperature that is negative, infinite or NaN, or
+ * with a NaN top_p, min_p or u.  vocab <= 2^20.  workspace: at least
+ * adaserve_sample_workspace_bytes(...) bytes, 256-byte aligned, no
+ * initialisation needed; calls that share one must not overlap in time.
+ * num_rows = 0 is a no-op.
+ */
+size_t adaserve_sample_workspace_bytes(int32_t num_rows, int32_t vocab, int32_t dtype);
+
+int32_t adaserve_sample(const void *logits, int64_t row_stride, int32_t num_rows, int32_t vocab,
+                        int32_t dtype, const float *temperature, const int32_t *top_k,
+                        const float *top_p, const float *min_p, const float *u, int32_t *out_token,
+                        void *workspace, size_t workspace_bytes, void *stream);
 
 /* Message describing the last non-OK status returned on this thread. */
 const char *adaserve_last_error(void);

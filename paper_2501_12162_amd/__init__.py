@@ -50,6 +50,16 @@ SIGNATURES = {
     "adaserve_tree_accept_sampled_workspace_bytes": (_SZ, [_I32]),
     "adaserve_tree_accept_sampled": (_I32, [_I32, _I32, _P, _P, _P, _P, _P, _I64, _I32, _I32, _P, _P, _I32,
                                             _P, _P, _P, _P, _SZ, _P]),
+    "adaserve_rope_append_kv": (_I32, [_I32, _I32, _P, _P, _P, _P, _I64, _P, _I64, _P, _I64, _P, _I32, _I32,
+                                       _I32, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _I32, _P, _I32, _P, _P]),
+    "adaserve_prompt_attn_workspace_bytes": (_SZ, [_I32, _P, _P, _I32, _I32, _I32, _I32, _I32]),
+    "adaserve_prompt_attn": (_I32, [_I32, _P, _P, _P, _I64, _P, _P, _I32, _P, _I32, _P, _P, _I32, _I32, _I32,
+                                    _I32, _F32, _I32, _P, _P, _SZ, _P]),
+    "adaserve_decode_attn_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32, _I32, _I32, _I32]),
+    "adaserve_decode_attn": (_I32, [_I32, _P, _I64, _P, _P, _I32, _P, _I32, _P, _I32, _I32, _I32, _I32, _I32,
+                                    _F32, _I32, _P, _P, _SZ, _P]),
+    "adaserve_sample_workspace_bytes": (_SZ, [_I32, _I32, _I32]),
+    "adaserve_sample": (_I32, [_P, _I64, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "adaserve_last_error": (ctypes.c_char_p, []),
 }
 
@@ -291,3 +301,179 @@ def adaserve_tree_accept_sampled(*, node_indptr, parent, draft_tokens, target_lo
         _dptr(accept_nodes), _dptr(workspace), int(0 if workspace is None else workspace.numel() * workspace.element_size()),
         _stream(stream))
     _check(st)
+
+
+def _device_call(name: str, tensors, stream, *args) -> None:
+    """Calls entry point ``name`` on the tensors' device: its current stream where none is given, and
+    the device made current for the call where it is not."""
+    import torch
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("expected a device tensor")
+        if device is None:
+            device = t.device.index
+        elif t.device.index != device:
+            raise ValueError("tensors are on different devices")
+    fn = getattr(load_library(), name)
+    if device is None or device == torch.cuda.current_device():
+        st = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, _stream(stream))
+    if st != ADASERVE_OK:
+        _check(st)
+
+
+def _rows(t, name: str):
+    """(pointer, elements between rows) of a [rows, heads, dim] tensor whose rows are dense."""
+    if t is None:
+        return None, 0
+    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        if t.shape[1] * t.shape[2] > 1 and t.numel():
+            raise ValueError("%s must have dense heads" % name)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _typed(t, dtype, name: str) -> None:
+    if t is not None and t.dtype != dtype:
+        raise ValueError("%s must be %s" % (name, dtype))
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def adaserve_rope_append_kv(*, token_indptr, prefix_len, q=None, k=None, v=None, inv_freq=None, interleaved=False,
+                            positions=None, q_out=None, k_out=None, k_pages=None, v_pages=None, block_table=None,
+                            new_prefix_len=None, stream=None) -> None:
+    """Rotates q [T, Hq, D] and k [T, Hkv, D] and appends k, v to the pages [P, Hkv, page_size, D].
+    Rows of q, k, v may lie apart (slices of a projection's output); inv_freq [rotary_dim / 2] float32."""
+    import torch
+    main = k if k is not None else q
+    if main is None:
+        raise ValueError("neither q nor k is given")
+    B = token_indptr.shape[0] - 1
+    T, _, D = main.shape
+    hq = 0 if q is None else q.shape[1]
+    hkv = 1 if k is None else k.shape[1]
+    if k_pages is not None and (k is None or k_pages.shape[1] != hkv or k_pages.shape[3] != D
+                                or v_pages is None or v_pages.shape != k_pages.shape):
+        raise ValueError("k_pages and v_pages must be [pages, %d, page_size, %d]" % (hkv, D))
+    for t, name, like in ((q, "q", main), (v, "v", k), (q_out, "q_out", q), (k_out, "k_out", k)):
+        if t is not None:
+            if like is None or t.shape[0] != T or t.shape[2] != D or (t is not q and t.shape[1] != like.shape[1]):
+                raise ValueError("%s does not fit the tokens, heads and head dim of the other rows" % name)
+            _typed(t, main.dtype, name)
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        _typed(t, main.dtype, name)
+    for t, name, n in ((token_indptr, "token_indptr", None), (prefix_len, "prefix_len", B), (positions, "positions", T),
+                       (block_table, "block_table", B), (new_prefix_len, "new_prefix_len", B)):
+        _typed(t, torch.int32, name)
+        if t is not None and n is not None and t.shape[0] != n:
+            raise ValueError("%s has %d rows, expected %d" % (name, t.shape[0], n))
+    _typed(inv_freq, torch.float32, "inv_freq")
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+    pages, ps = (0, 1) if k_pages is None else (k_pages.shape[0], k_pages.shape[2])
+    _device_call("adaserve_rope_append_kv", (main, q, v, token_indptr, prefix_len, positions, inv_freq, q_out, k_out,
+                                             k_pages, v_pages, block_table, new_prefix_len), stream,
+                 B, T, _dptr(token_indptr), _dptr(prefix_len), _dptr(positions), qp, qs, kp, ks, vp, vs,
+                 _dptr(inv_freq), 0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved), hq, hkv, D, ps,
+                 _dtype_code(main), _dptr(q_out), _dptr(k_out), _dptr(k_pages), _dptr(v_pages), pages,
+                 _dptr(block_table), 0 if block_table is None else block_table.shape[1], _dptr(new_prefix_len))
+
+
+def _check_paged(q, k_pages, v_pages, block_table, context_len, out, requests) -> None:
+    import torch
+    if v_pages.shape != k_pages.shape or k_pages.dim() != 4 or k_pages.shape[3] != q.shape[2]:
+        raise ValueError("k_pages and v_pages must be [pages, kv-heads, page_size, %d]" % q.shape[2])
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages"), (out, "out")):
+        _typed(t, q.dtype, name)
+    _typed(block_table, torch.int32, "block_table")
+    _typed(context_len, torch.int32, "context_len")
+    if block_table.dim() != 2 or block_table.shape[0] != requests or context_len.shape[0] != requests:
+        raise ValueError("block_table and context_len must have %d rows" % requests)
+
+
+def adaserve_prompt_attn_workspace_bytes(token_indptr_host, context_len_host, num_q_heads: int, num_kv_heads: int,
+                                         head_dim: int, page_size: int, dtype: int) -> int:
+    ip, cl = _host_i32(token_indptr_host), _host_i32(context_len_host)
+    n = load_library().adaserve_prompt_attn_workspace_bytes(cl.size, ip.ctypes.data, cl.ctypes.data, num_q_heads,
+                                                            num_kv_heads, head_dim, page_size, dtype)
+    if n == ctypes.c_size_t(-1).value:
+        _check(ADASERVE_ERR_INVALID_ARGUMENT)
+    return n
+
+
+def adaserve_prompt_attn(*, token_indptr, token_indptr_host, q, k_pages, v_pages, block_table, context_len,
+                         context_len_host, sm_scale: float, out, workspace=None, stream=None) -> None:
+    """Causal attention of packed prompts; q/out [T, Hq, D] (rows of q may lie apart), k_pages/v_pages
+    [P, Hkv, page_size, D], block_table [B, stride], context_len [B] with the rows' own keys counted."""
+    import torch
+    ip, cl = _host_i32(token_indptr_host), _host_i32(context_len_host)
+    B = cl.size
+    T, Hq, D = q.shape
+    if ip.size != B + 1 or token_indptr.shape[0] != B + 1 or (B and T < ip[B]):
+        raise ValueError("token_indptr must have %d entries, the last at most %d" % (B + 1, T))
+    _check_paged(q, k_pages, v_pages, block_table, context_len, out, B)
+    _typed(token_indptr, torch.int32, "token_indptr")
+    qp, qs = _rows(q, "q")
+    _device_call("adaserve_prompt_attn", (q, token_indptr, k_pages, v_pages, block_table, context_len, out, workspace),
+                 stream, B, _dptr(token_indptr), ip.ctypes.data, qp, qs, _dptr(k_pages), _dptr(v_pages),
+                 k_pages.shape[0], _dptr(block_table), block_table.shape[1], _dptr(context_len), cl.ctypes.data, Hq,
+                 k_pages.shape[1], D, k_pages.shape[2], sm_scale, _dtype_code(q), _dptr(out), _dptr(workspace),
+                 _bytes(workspace))
+
+
+def adaserve_decode_attn_workspace_bytes(num_requests: int, max_context: int, num_q_heads: int, num_kv_heads: int,
+                                         head_dim: int, page_size: int, dtype: int) -> int:
+    n = load_library().adaserve_decode_attn_workspace_bytes(num_requests, max_context, num_q_heads, num_kv_heads,
+                                                            head_dim, page_size, dtype)
+    if n == ctypes.c_size_t(-1).value:
+        _check(ADASERVE_ERR_INVALID_ARGUMENT)
+    return n
+
+
+def adaserve_decode_attn(*, q, k_pages, v_pages, block_table, context_len, max_context: int, sm_scale: float, out,
+                         workspace=None, stream=None) -> None:
+    """Attention of one token per request; q/out [B, Hq, D], context_len [B] (device) at most max_context."""
+    B, Hq, D = q.shape
+    _check_paged(q, k_pages, v_pages, block_table, context_len, out, B)
+    qp, qs = _rows(q, "q")
+    _device_call("adaserve_decode_attn", (q, k_pages, v_pages, block_table, context_len, out, workspace), stream, B,
+                 qp, qs, _dptr(k_pages), _dptr(v_pages), k_pages.shape[0], _dptr(block_table), block_table.shape[1],
+                 _dptr(context_len), max_context, Hq, k_pages.shape[1], D, k_pages.shape[2], sm_scale,
+                 _dtype_code(q), _dptr(out), _dptr(workspace), _bytes(workspace))
+
+
+def adaserve_sample_workspace_bytes(num_rows: int, vocab: int, dtype: int) -> int:
+    n = load_library().adaserve_sample_workspace_bytes(num_rows, vocab, dtype)
+    if n == ctypes.c_size_t(-1).value:
+        _check(ADASERVE_ERR_INVALID_ARGUMENT)
+    return n
+
+
+def adaserve_sample(*, logits, vocab: int, u, out_token, temperature=None, top_k=None, top_p=None, min_p=None,
+                    workspace=None, stream=None) -> None:
+    """A token per row of logits [rows, >= vocab] (rows may lie apart); temperature, top_p, min_p, u [rows]
+    float32, top_k and out_token [rows] int32."""
+    import torch
+    rows, width = logits.shape
+    if vocab > width:
+        raise ValueError("vocab %d > %d columns" % (vocab, width))
+    if width > 1 and logits.stride(1) != 1:
+        raise ValueError("logits must have dense rows")
+    for t, dtype, name in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                           (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"), (u, torch.float32, "u"),
+                           (out_token, torch.int32, "out_token")):
+        _typed(t, dtype, name)
+        if t is not None and t.shape[0] != rows:
+            raise ValueError("%s has %d entries, expected %d" % (name, t.shape[0], rows))
+    _device_call("adaserve_sample", (logits, temperature, top_k, top_p, min_p, u, out_token, workspace), stream,
+                 logits.data_ptr(), logits.stride(0) if rows > 1 else width, rows, vocab, _dtype_code(logits),
+                 _dptr(temperature), _dptr(top_k), _dptr(top_p), _dptr(min_p), _dptr(u), _dptr(out_token),
+                 _dptr(workspace), _bytes(workspace))

@@ -16,6 +16,7 @@
 #include <utility>
 #include <vector>
 
+#include "host_device.h"
 #include "host_plan.h"
 #include "kernels.h"
 #include "plan.h"
@@ -23,33 +24,6 @@
 namespace {
 
 using namespace adaserve;
-
-bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
-
-// gfx950 check, once per device ordinal.
-int32_t check_device() {
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return fail(ADASERVE_ERR_DEVICE, "hipGetDevice failed: %s", hipGetErrorString(e));
-  static std::mutex mu;
-  static signed char arch_ok[256];  // 0 unknown, 1 gfx950, -1 other
-  if (dev < 0 || dev >= 256) return fail(ADASERVE_ERR_DEVICE, "device ordinal %d out of range", dev);
-  std::lock_guard<std::mutex> lock(mu);
-  if (arch_ok[dev] == 0) {
-    hipDeviceProp_t prop;
-    e = hipGetDeviceProperties(&prop, dev);
-    if (e != hipSuccess)
-      return fail(ADASERVE_ERR_DEVICE, "hipGetDeviceProperties failed: %s", hipGetErrorString(e));
-    arch_ok[dev] = std::strncmp(prop.gcnArchName, "gfx950", 6) == 0 ? 1 : -1;
-  }
-  if (arch_ok[dev] < 0) return fail(ADASERVE_ERR_UNSUPPORTED, "device %d is not gfx950", dev);
-  return ADASERVE_OK;
-}
-
-int32_t launch_status(hipError_t e, const char *what) {
-  if (e == hipSuccess) return ADASERVE_OK;
-  return fail(ADASERVE_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
-}
 
 }  // namespace
 
