@@ -392,11 +392,12 @@ def _own(s):
             context_len_host=s["context_len_host"], sm_scale=s["sm_scale"], out=s["out"], workspace=ws)
         return s["out"]
     if c["kind"] == "decode":
+        most = min(s["max_context"], s["block_table"].shape[1] * PAGE)   # the bound is at most what the table holds
         ws = _workspace(s, lambda: ada.adaserve_decode_attn_workspace_bytes(
-            c["requests"], s["max_context"], c["hq"], c["hkv"], c["dim"], PAGE, code))
+            c["requests"], most, c["hq"], c["hkv"], c["dim"], PAGE, code))
         ada.adaserve_decode_attn(
             q=s["q"], k_pages=s["k_pages"], v_pages=s["v_pages"], block_table=s["block_table"],
-            context_len=s["context_len"], max_context=s["max_context"], sm_scale=s["sm_scale"], out=s["out"], workspace=ws)
+            context_len=s["context_len"], max_context=most, sm_scale=s["sm_scale"], out=s["out"], workspace=ws)
         return s["out"]
     if "token" not in s:
         s["token"] = torch.empty(c["requests"], dtype=torch.int32, device=DEVICE)
