@@ -1,6 +1,31 @@
 // Attention of one new token per request over its paged cache on gfx950.
+//
+// A unit of work is (request, kv-head, up to 8 of its query heads, a run of
+// 32-key blocks); the requests' caches are cut into runs so that the batch
+// fills the device whatever its lengths, and the runs of one request are
+// joined by a second launch.  The lengths are read on the device only: every
+// workgroup finds its unit from all of them (schedule()), so a captured launch
+// follows them.
+//
+// Bound by memory: 2 c Hkv D s bytes per request against 4 c Hq D flops.  So
+// everything serves to keep loads in flight: no LDS in the loop and no
+// barrier; each of a workgroup's four waves walks its own blocks with K and V
+// straight in registers, 16 KB of them in flight per wave.
+//  * S^T = K Q^T on the matrix cores (16 keys x 16 rows; K as it lies in
+//    memory is the A operand, lanes without a row multiply zeros).  A lane then
+//    holds 4 keys of one row.
+//  * O += P V on the vector ALUs: the matrix cores would want V transposed,
+//    which only LDS could give.  The 16 lanes that hold the weights of 4 keys
+//    also load the V rows of those 4 keys, a slice of columns each, so a weight
+//    reaches them by a broadcast within 16 lanes (DPP), and a row's output is
+//    spread over columns; the four groups of lanes are summed once at the end.
+//    Weights stay fp32.
+//  * exponentials are 2^x of scores in log2 units; the running maximum moves
+//    only when it is exceeded by 2^8, which spares the rescaling of the output.
+#include <type_traits>
+#include <utility>
+
 #include "device_common.h"
-#include "paged_rows.h"
 #include "plan.h"
 #include "serving.h"
 
@@ -9,36 +34,434 @@ namespace adaserve {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr float kLowest = -1e30f;      // running maximum before any key
+constexpr float kRescaleLog2 = 8.f;
 
-template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads) void decode_attn_kernel(PagedAttnArgs a) {
-  const int wave = threadIdx.x >> 6;
-  const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + wave;
-  const int64_t r = id / a.num_q_heads;
-  const int h = (int)(id - r * a.num_q_heads);
-  if (r >= a.num_requests) return;
-  const int32_t len = a.context_len[r];
-  if (len < 0 || len > a.max_context) {
-    const int lane = threadIdx.x & 63;
-    for (int i = lane; i < D; i += 64) {
-      if (BF16) ((__bf16 *)a.out)[(r * a.num_q_heads + h) * D + i] = (__bf16)__builtin_nanf("");
-      else ((float *)a.out)[(r * a.num_q_heads + h) * D + i] = __builtin_nanf("");
+// The value of lane L of each 16 lanes.
+template <int L>
+__device__ __forceinline__ float row_bcast(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + L, 0xf, 0xf, false));
+}
+
+// f(row) for every row, the row a constant.
+template <class F, int... I>
+__device__ __forceinline__ void each_row(F &&f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+struct DecodeUnit {
+  int32_t r;        // request, or -1: no such unit
+  int32_t len;      // its length (-1: out of range)
+  int32_t chunk;    // run of blocks
+  int32_t chunks;   // runs of the request
+  int32_t per;      // blocks per run
+  int32_t first;    // the request's first unit
+};
+
+__device__ __forceinline__ int32_t decode_blocks(int32_t len) { return (len + kKeysPerBlock - 1) / kKeysPerBlock; }
+
+// Unit u of the batch.  The batch's blocks are dealt into `target` equal runs,
+// none shorter than min_blocks; a request takes as many as cover it, and one
+// if it is empty.  Each thread takes 1 to 4 neighbouring requests (at most
+// kDecodeSplitRequests in all); every thread ends with the same answer.
+__device__ __forceinline__ DecodeUnit schedule(const PagedAttnArgs &a, int32_t u) {
+  __shared__ int32_t part[2][kWaves];
+  __shared__ DecodeUnit found;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  DecodeUnit d;
+  auto valid = [&](int32_t len) { return len >= 0 && len <= a.max_context ? len : -1; };
+  if (a.units_per_head == a.num_requests) {   // nothing is split
+    d = {u < a.num_requests ? u : -1, 0, 0, 1, 1 << 20, u};
+    if (d.r >= 0) d.len = valid(a.context_len[d.r]);
+    return d;
+  }
+  const int per_thread = (a.num_requests + kThreads - 1) / kThreads;
+  int32_t len[4], nb[4], blocks = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = tid * per_thread + i;
+    len[i] = i < per_thread && r < a.num_requests ? valid(a.context_len[r]) : -2;
+    nb[i] = len[i] > 0 ? decode_blocks(len[i]) : 0;
+    blocks += nb[i];
+  }
+  // sum over the workgroup, then the scan of the runs
+  int32_t sum = blocks;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+  if (lane == 0) part[0][wave] = sum;
+  if (tid == 0) found.r = -1;
+  __syncthreads();
+  const int32_t total = part[0][0] + part[0][1] + part[0][2] + part[0][3];
+  const int32_t per = max(a.min_blocks, (total + a.target - 1) / a.target);
+  int32_t chunks[4], mine = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    chunks[i] = len[i] == -2 ? 0 : max(1, (nb[i] + per - 1) / per);
+    mine += chunks[i];
+  }
+  int32_t upto = mine;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int32_t o = __shfl_up(upto, off, 64);
+    if (lane >= off) upto += o;
+  }
+  if (lane == 63) part[1][wave] = upto;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) upto += part[1][w];
+  int32_t before = upto - mine;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (u >= before && u < before + chunks[i])
+      found = {tid * per_thread + i, len[i], u - before, chunks[i], per, before};
+    before += chunks[i];
+  }
+  __syncthreads();
+  return found;
+}
+
+template <bool BF16, int D, int R, bool NT>
+__global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs a) {
+  constexpr int T = BF16 ? 2 : 1;          // 16-key tiles (pages) per block of a wave
+  constexpr int KB = T * 16;
+  constexpr int EPL = D / 16;              // columns of a lane
+  constexpr int ESZ = BF16 ? 2 : 4;
+  constexpr int NK = D * ESZ / 64;         // 16-byte K loads per lane and tile
+  __shared__ float mo[kWaves][R][D];
+  __shared__ float mw[kWaves][R], lw[kWaves][R];
+
+  // blocks of 8 neighbouring (unit, head) pairs, their row groups 8 ids apart:
+  // those read the same keys and run on one XCD
+  const int64_t id = blockIdx.x;
+  const int64_t octet = id / (8 * a.row_groups);
+  const int rg = (int)(id - octet * (8 * a.row_groups)) / 8;
+  const int64_t pair = octet * 8 + (id & 7);
+  const int32_t u = (int32_t)(pair / a.num_kv_heads);
+  const int g = (int)(pair - (int64_t)u * a.num_kv_heads);
+  if (u >= a.units_per_head) return;
+  const DecodeUnit un = schedule(a, u);
+  const int r = __builtin_amdgcn_readfirstlane(un.r);
+  if (r < 0) return;
+  const int32_t len = __builtin_amdgcn_readfirstlane(un.len);
+  const int32_t chunk = __builtin_amdgcn_readfirstlane(un.chunk), chunks = __builtin_amdgcn_readfirstlane(un.chunks);
+  const int32_t per = __builtin_amdgcn_readfirstlane(un.per);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int quad = lane >> 4, j = lane & 15;
+  const int row0 = rg * R, rows = min(R, a.group - row0);
+  const int64_t out_row = (int64_t)r * a.num_q_heads + (int64_t)g * a.group + row0;
+  // the request's units, for the join
+  if (a.ws_request && chunk == 0 && g == 0 && rg == 0 && tid == 0) {
+    a.ws_request[2 * r] = un.first;
+    a.ws_request[2 * r + 1] = chunks;
+  }
+  if (len <= 0) {   // empty: zeros; out of range: NaN
+    const float x = len < 0 ? __builtin_nanf("") : 0.f;
+    for (int i = tid; i < rows * D; i += kThreads) {
+      if (BF16) ((__bf16 *)a.out)[out_row * D + i] = (__bf16)x;
+      else ((float *)a.out)[out_row * D + i] = x;
     }
     return;
   }
-  attend_row<BF16, D>(a, (int)r, r, h, len);
+  // keys of the run, in blocks of KB; this wave takes blocks wave, wave + 4, ...
+  const int32_t k0 = chunk * per * kKeysPerBlock;
+  const int32_t k1 = min(len, k0 + per * kKeysPerBlock);
+  const int32_t nb = k1 > k0 ? (k1 - k0 + KB - 1) / KB : 0;
+  const int32_t mine = nb > wave ? (nb - wave + kWaves - 1) / kWaves : 0;
+
+  // page ids: lane i holds that of tile i of this wave's blocks, 64 tiles at a time
+  int32_t pages = -1, page_base = 0;
+  auto load_pages = [&](int base) {
+    const int i = base + lane;                       // tile of the wave
+    const int32_t b = wave + (i / T) * kWaves;
+    const int32_t e = (k0 + b * KB) / kPageSize + i % T;
+    int32_t p = -1;
+    if (b < nb && e < a.bt_stride && e * kPageSize < k1) {
+      p = a.block_table[(int64_t)r * a.bt_stride + e];
+      if (p < 0 || p >= a.num_pages) p = -1;
+    }
+    pages = p;
+    page_base = base;
+  };
+  load_pages(0);
+
+  // query rows as the B operand: lane holds row j (none: zeros)
+  u32x4 qf[NK];
+  {
+    const char *qp = (const char *)a.q + ((int64_t)r * a.q_stride + ((int64_t)g * a.group + row0 + (j < rows ? j : 0)) * D) * ESZ;
+#pragma unroll
+    for (int c = 0; c < NK; ++c) {
+      u32x4 v = *(const u32x4 *)(qp + c * 64 + quad * 16);
+      qf[c] = j < rows ? v : u32x4{0, 0, 0, 0};
+    }
+  }
+
+  const int64_t page_bytes = (int64_t)a.num_kv_heads * kPageSize * D * ESZ;
+  const int64_t head_bytes = (int64_t)g * kPageSize * D * ESZ;
+  u32x4 kr[T][NK];
+  constexpr int NV = EPL * ESZ / 4;        // 32-bit words of a lane's V slice: 4 or 2 (bf16), 8 or 4 (fp32)
+  uint32_t vr[T][4][NV];
+  bool have[T];                            // the tile's page exists (of the tiles in kr)
+  bool have_v[T];
+  auto page_of = [&](int i, int t) { return __builtin_amdgcn_readlane(pages, i * T + t - page_base); };
+  auto load16 = [&](const char *p) -> u32x4 {
+    if constexpr (NT) return __builtin_nontemporal_load((const u32x4 *)p);
+    else return *(const u32x4 *)p;
+  };
+  auto load8 = [&](const char *p) -> u32x2 {
+    if constexpr (NT) return __builtin_nontemporal_load((const u32x2 *)p);
+    else return *(const u32x2 *)p;
+  };
+  // A missing page reads page 0 (its values are not used): no branch around the loads.
+  auto load_k = [&](int i) {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const int32_t p = page_of(i, t);
+      have[t] = p >= 0;
+      const char *base = (const char *)a.k_pages + max(p, 0) * page_bytes + head_bytes + j * D * ESZ + quad * 16;
+#pragma unroll
+      for (int c = 0; c < NK; ++c) kr[t][c] = load16(base + c * 64);
+    }
+  };
+  auto load_v = [&](int i) {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const int32_t p = page_of(i, t);
+      have_v[t] = p >= 0;
+      const char *base = (const char *)a.v_pages + max(p, 0) * page_bytes + head_bytes + (quad * 4) * D * ESZ + j * EPL * ESZ;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (NV == 2) {
+          const u32x2 x = load8(base + e * D * ESZ);
+          vr[t][e][0] = x[0], vr[t][e][1] = x[1];
+        } else {
+#pragma unroll
+          for (int w = 0; w < NV; w += 4) {
+            const u32x4 x = load16(base + e * D * ESZ + w * 4);
+            vr[t][e][w] = x[0], vr[t][e][w + 1] = x[1], vr[t][e][w + 2] = x[2], vr[t][e][w + 3] = x[3];
+          }
+        }
+      }
+    }
+  };
+
+  float o[R][EPL];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) o[i][e] = 0.f;
+  float m = kLowest, l = 0.f;   // of row j: the reference in log2 units; this lane's part of the sum
+
+  if (mine > 0) {
+    load_k(0);
+    load_v(0);
+  }
+  for (int i = 0; i < mine; ++i) {
+    const int nxt = min(i + 1, mine - 1);
+    f32x4 s[T];
+    bool hk[T], hv[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      hk[t] = have[t];
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        if constexpr (BF16) {
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[t][c]),
+                                                         __builtin_bit_cast(bf16x8, qf[c]), s[t], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[t][c][e]), __uint_as_float(qf[c][e]), s[t], 0, 0, 0);
+        }
+      }
+    }
+    if ((nxt + 1) * T - page_base > 64) load_pages(nxt * T);
+    load_k(nxt);
+    // s[t][e]: key 16 t + 4 quad + e of the block, row j
+    const int32_t left = k1 - (k0 + (wave + i * kWaves) * KB);   // keys of the block and after
+    float p[T][4];
+    float bm = kLowest;
+    const bool edge = left < KB;
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = hk[t] ? s[t][e] * a.scale_log2 : 0.f;
+        p[t][e] = !edge || t * 16 + quad * 4 + e < left ? x : -INFINITY;
+        bm = fmaxf(bm, p[t][e]);
+      }
+    bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
+    bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
+    const bool up = bm > m + kRescaleLog2 || (m == kLowest && bm > m);
+    if (__any(up)) {
+      const float mn = up ? bm : m;
+      const float al = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= al;
+      auto scale_row = [&](auto row) {
+        constexpr int I = decltype(row)::value;
+        const float f = row_bcast<I>(al);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) o[I][e] *= f;
+      };
+      each_row(scale_row, std::make_integer_sequence<int, R>{});
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[t][e] = __builtin_amdgcn_exp2f(p[t][e] - m);
+        l += p[t][e];
+      }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      hv[t] = have_v[t];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        // a slot past the run's keys may hold anything
+        const bool use = hv[t] && (!edge || t * 16 + quad * 4 + e < left);
+        float v[EPL];
+#pragma unroll
+        for (int w = 0; w < NV; ++w) {
+          const uint32_t x = use ? vr[t][e][w] : 0u;
+          if constexpr (BF16) {
+            v[2 * w] = __uint_as_float(x << 16);
+            v[2 * w + 1] = __uint_as_float(x & 0xffff0000u);
+          } else {
+            v[w] = __uint_as_float(x);
+          }
+        }
+        auto add_row = [&](auto row) {
+          constexpr int I = decltype(row)::value;
+          const float f = row_bcast<I>(p[t][e]);
+#pragma unroll
+          for (int c = 0; c < EPL; ++c) o[I][c] = __builtin_fmaf(f, v[c], o[I][c]);
+        };
+        each_row(add_row, std::make_integer_sequence<int, R>{});
+      }
+    }
+    load_v(nxt);
+  }
+
+  // the four groups of lanes, then the four waves
+  l = sum_over_lane_rows(l);
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) {
+      const float x = sum_over_lane_rows(o[i][e]);
+      if (quad == (i & 3)) mo[wave][i][j * EPL + e] = x;
+    }
+  if (quad == 0 && j < R) {
+    mw[wave][j] = m;
+    lw[wave][j] = l;
+  }
+  __syncthreads();
+  const int64_t slot = ((int64_t)u * a.num_kv_heads + g) * a.row_groups + rg;
+  for (int it = tid; it < rows * D; it += kThreads) {
+    const int i = it / D, c = it % D;
+    float mm = mw[0][i];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, mw[w][i]);
+    float den = 0.f, num = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(mw[w][i] - mm);
+      den = __builtin_fmaf(f, lw[w][i], den);
+      num = __builtin_fmaf(f, mo[w][i][c], num);
+    }
+    if (chunks == 1) {
+      const float x = den != 0.f ? num / den : 0.f;
+      if (BF16) ((__bf16 *)a.out)[out_row * D + it] = (__bf16)x;
+      else ((float *)a.out)[out_row * D + it] = x;
+    } else {
+      a.ws_o[(slot * kDecodeRows + i) * D + c] = num;
+      if (c == 0) *(f32x2 *)(a.ws_ml + (slot * kDecodeRows + i) * 2) = f32x2{mm, den};
+    }
+  }
+}
+
+// Joins the runs of a request's row: with reference m over the runs' m_c,
+// out = sum 2^(m_c - m) o_c / sum 2^(m_c - m) l_c.  One workgroup per row, its
+// four waves taking every fourth run.
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads) void decode_join_kernel(PagedAttnArgs a) {
+  constexpr int EPL = D / 64;
+  __shared__ float so[kWaves][D], sm[kWaves], sl[kWaves];
+  const int64_t row = blockIdx.x;
+  const int r = (int)(row / a.num_q_heads), h = (int)(row - (int64_t)r * a.num_q_heads);
+  const int32_t chunks = a.ws_request[2 * r + 1];
+  if (chunks <= 1) return;
+  const int32_t first = a.ws_request[2 * r];
+  const int g = h / a.group, in = h - g * a.group, rows_per = a.rows_per_group;
+  const int rg = in / rows_per, i = in - rg * rows_per;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float m = kLowest, l = 0.f, o[EPL] = {};
+  for (int c = wave; c < chunks; c += kWaves) {
+    const int64_t slot = (((int64_t)(first + c) * a.num_kv_heads + g) * a.row_groups + rg) * kDecodeRows + i;
+    const f32x2 ml = *(const f32x2 *)(a.ws_ml + slot * 2);
+    float x[EPL];
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) x[e] = a.ws_o[slot * D + lane * EPL + e];
+    const float mn = fmaxf(m, ml[0]);
+    const float f = __builtin_amdgcn_exp2f(m - mn), w = __builtin_amdgcn_exp2f(ml[0] - mn);
+    m = mn;
+    l = l * f + w * ml[1];
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) o[e] = o[e] * f + w * x[e];
+  }
+  if (lane == 0) sm[wave] = m, sl[wave] = l;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) so[wave][lane * EPL + e] = o[e];
+  __syncthreads();
+  const int c = threadIdx.x;
+  if (c >= D) return;
+  float mm = sm[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, sm[w]);
+  float den = 0.f, num = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float f = __builtin_amdgcn_exp2f(sm[w] - mm);
+    den = __builtin_fmaf(f, sl[w], den);
+    num = __builtin_fmaf(f, so[w][c], num);
+  }
+  const float x = den != 0.f ? num / den : 0.f;
+  if (BF16) ((__bf16 *)a.out)[row * D + c] = (__bf16)x;
+  else ((float *)a.out)[row * D + c] = x;
+}
+
+template <bool BF16, int D, int R>
+hipError_t launch(const PagedAttnArgs &a, hipStream_t stream) {
+  const int64_t pairs = (int64_t)a.units_per_head * a.num_kv_heads;
+  const int64_t blocks = (pairs + 7) / 8 * 8 * a.row_groups;
+  if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (a.row_groups == 1)
+    hipLaunchKernelGGL((decode_attn_kernel<BF16, D, R, true>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((decode_attn_kernel<BF16, D, R, false>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.ws_request) return e;
+  hipLaunchKernelGGL((decode_join_kernel<BF16, D>), dim3((unsigned)((int64_t)a.num_requests * a.num_q_heads)),
+                     dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <bool BF16, int D>
+hipError_t launch_rows(const PagedAttnArgs &a, hipStream_t stream) {
+  switch (a.rows_per_group) {
+    case 1: return launch<BF16, D, 1>(a, stream);
+    case 2: return launch<BF16, D, 2>(a, stream);
+    case 4: return launch<BF16, D, 4>(a, stream);
+    default: return launch<BF16, D, 8>(a, stream);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_decode_attn(const PagedAttnArgs &a, int head_dim, bool bf16, hipStream_t stream) {
-  const int64_t waves = (int64_t)a.num_requests * a.num_q_heads;
-  const dim3 grid((unsigned)((waves + 3) / 4)), block(kThreads);
-  if (bf16 && head_dim == 128) hipLaunchKernelGGL((decode_attn_kernel<true, 128>), grid, block, 0, stream, a);
-  else if (bf16) hipLaunchKernelGGL((decode_attn_kernel<true, 64>), grid, block, 0, stream, a);
-  else if (head_dim == 128) hipLaunchKernelGGL((decode_attn_kernel<false, 128>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((decode_attn_kernel<false, 64>), grid, block, 0, stream, a);
-  return hipGetLastError();
+  if (bf16) return head_dim == 128 ? launch_rows<true, 128>(a, stream) : launch_rows<true, 64>(a, stream);
+  return head_dim == 128 ? launch_rows<false, 128>(a, stream) : launch_rows<false, 64>(a, stream);
 }
 
 }  // namespace adaserve

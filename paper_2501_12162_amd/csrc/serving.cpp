@@ -95,6 +95,14 @@ int32_t validate_pages(bool any_key, const void *k_pages, const void *v_pages, i
   return ADASERVE_OK;
 }
 
+int32_t validate_workspace(const void *workspace, size_t given, size_t need) {
+  if (need == 0) return ADASERVE_OK;
+  if (!workspace || given < need)
+    return fail(ADASERVE_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace ? given : (size_t)0, need);
+  if (!aligned(workspace, 256)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "workspace must be 256-byte aligned");
+  return ADASERVE_OK;
+}
+
 int32_t validate_decode(int32_t num_requests, int32_t hq, int32_t max_context, int32_t bt_stride_or_neg) {
   if (max_context < 0) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "max_context %d < 0", max_context);
   if (max_context > kMaxPrefixLen) return fail(ADASERVE_ERR_UNSUPPORTED, "max_context %d > %d", max_context, kMaxPrefixLen);
@@ -286,7 +294,7 @@ size_t adaserve_decode_attn_workspace_bytes(int32_t num_requests, int32_t max_co
   if (validate_paged(num_requests, 0, 0, num_q_heads, num_kv_heads, head_dim, page_size, 1.f, dtype) != ADASERVE_OK ||
       validate_decode(num_requests, num_q_heads, max_context, -1) != ADASERVE_OK)
     return SIZE_MAX;
-  return 0;
+  return decode_plan(num_requests, num_q_heads, num_kv_heads, head_dim, max_context).ws_bytes;
 }
 
 int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_stride, const void *k_pages,
@@ -295,8 +303,6 @@ int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_
                              int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
                              float sm_scale, int32_t dtype, void *out, void *workspace, size_t workspace_bytes,
                              void *stream) {
-  (void)workspace;
-  (void)workspace_bytes;
   int32_t st = validate_paged(num_requests, num_pages, block_table_stride, num_q_heads, num_kv_heads, head_dim,
                               page_size, sm_scale, dtype);
   if (st != ADASERVE_OK) return st;
@@ -308,6 +314,9 @@ int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_
   if (st != ADASERVE_OK) return st;
   if (!aligned(out, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "out must be 16-byte aligned");
   st = validate_pages(max_context > 0, k_pages, v_pages, num_pages, block_table);
+  if (st != ADASERVE_OK) return st;
+  const DecodePlan plan = decode_plan(num_requests, num_q_heads, num_kv_heads, head_dim, max_context);
+  st = validate_workspace(workspace, workspace_bytes, plan.ws_bytes);
   if (st != ADASERVE_OK) return st;
   st = check_device();
   if (st != ADASERVE_OK) return st;
@@ -327,6 +336,16 @@ int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_
   a.num_kv_heads = num_kv_heads;
   a.group = num_q_heads / num_kv_heads;
   a.max_context = max_context;
+  a.rows_per_group = plan.rows_per_group;
+  a.row_groups = plan.row_groups;
+  a.units_per_head = plan.units_per_head;
+  a.target = plan.target;
+  a.min_blocks = kDecodeMinBlocks;
+  if (plan.split) {
+    a.ws_request = (int32_t *)workspace;
+    a.ws_ml = (float *)((char *)workspace + plan.ml_offset);
+    a.ws_o = (float *)((char *)workspace + plan.o_offset);
+  }
   a.sm_scale = sm_scale;
   a.scale_log2 = sm_scale * 1.4426950408889634f;
   return launch_status(launch_decode_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),

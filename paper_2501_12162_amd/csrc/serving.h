@@ -52,10 +52,59 @@ struct PagedAttnArgs {
   int32_t num_q_heads;
   int32_t num_kv_heads;
   int32_t group;                 // Hq / Hkv
-  int32_t max_context;           // (decode attention)
   float sm_scale;
   float scale_log2;              // sm_scale * log2(e)
+  // decode attention (DecodePlan)
+  int32_t max_context;
+  int32_t rows_per_group;
+  int32_t row_groups;
+  int32_t units_per_head;
+  int32_t target;
+  int32_t min_blocks;
+  int32_t *ws_request;           // [B, 2] first unit, units; null: nothing is split
+  float *ws_ml;                  // [units, heads, row groups, kDecodeRows, 2] reference, sum
+  float *ws_o;                   // [units, heads, row groups, kDecodeRows, D] weighted sums of V
 };
+
+// Decode attention's work, from sizes alone.  Query heads that share a kv-head
+// go in groups of 1, 2, 4 or 8 rows (a group of 8 reads the keys once for all;
+// more than 8 read them once per 8, the second time out of L2).  Per kv-head
+// and row group the batch's 32-key blocks are cut into about `target` runs of
+// at least kDecodeMinBlocks: a batch that fills the device with whole requests
+// (or that has more of them than the workgroups' scan takes) is not cut.
+constexpr int kDecodeRows = 8;
+constexpr int kDecodeMinBlocks = 4;          // one block per wave
+constexpr int kDecodeUnits = 1024;           // on the device: two rounds of two workgroups per CU
+constexpr int kDecodeSplitRequests = 1024;
+
+struct DecodePlan {
+  int32_t rows_per_group, row_groups, units_per_head, target;
+  bool split;
+  int64_t ml_offset, o_offset;
+  size_t ws_bytes;
+};
+
+inline DecodePlan decode_plan(int32_t B, int32_t hq, int32_t hkv, int32_t head_dim, int32_t max_context) {
+  DecodePlan p{};
+  const int32_t group = hq / hkv;
+  p.rows_per_group = group > 4 ? 8 : group > 2 ? 4 : group;
+  p.row_groups = (group + p.rows_per_group - 1) / p.rows_per_group;
+  const int64_t heads = (int64_t)hkv * p.row_groups;
+  p.target = (int32_t)((kDecodeUnits + heads - 1) / heads);
+  const int64_t blocks = (max_context + 31) / 32;
+  const int64_t most = (blocks + kDecodeMinBlocks - 1) / kDecodeMinBlocks;   // runs of one request
+  int64_t units = (int64_t)p.target + B;
+  if (units > B * most) units = B * most;
+  p.split = most > 1 && B <= kDecodeSplitRequests && B < p.target * 4 && units > B;
+  p.units_per_head = (int32_t)(p.split ? units : B);
+  if (p.split) {
+    const size_t slots = (size_t)(units * heads) * kDecodeRows;
+    p.ml_offset = ((int64_t)B * 8 + 255) / 256 * 256;
+    p.o_offset = p.ml_offset + (int64_t)((slots * 8 + 255) / 256 * 256);
+    p.ws_bytes = (size_t)p.o_offset + slots * head_dim * 4;
+  }
+  return p;
+}
 
 hipError_t launch_prompt_attn(const PagedAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
 hipError_t launch_decode_attn(const PagedAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
