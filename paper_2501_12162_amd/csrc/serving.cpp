@@ -85,6 +85,30 @@ int32_t validate_prompt(int32_t num_requests, const int32_t *indptr, const int32
   return ADASERVE_OK;
 }
 
+// The requests' workgroups, those with the longest tiles first; more requests
+// than the table holds are found by a scan on the device, in their own order.
+void fill_prompt_table(PagedAttnArgs &a, const int32_t *indptr, const int32_t *ctx) {
+  int64_t units = 0;
+  const bool fits = a.num_requests <= kPromptTable;
+  int32_t count = 0;
+  for (int32_t r = 0; r < a.num_requests; ++r) {
+    const int32_t n = indptr[r + 1] - indptr[r];
+    units += (int64_t)prompt_tiles(n, a.group, a.tile_rows) * a.num_kv_heads;
+    if (fits && n > 0) {
+      int32_t i = count++;
+      for (; i > 0 && a.table[i - 1].ctx < ctx[r]; --i) a.table[i] = a.table[i - 1];
+      a.table[i] = {0, r, indptr[r], n, ctx[r]};
+    }
+  }
+  int64_t end = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    end += (int64_t)prompt_tiles(a.table[i].n, a.group, a.tile_rows) * a.num_kv_heads;
+    a.table[i].unit_end = (int32_t)end;
+  }
+  a.units = units;
+  a.table_count = count;
+}
+
 int32_t validate_pages(bool any_key, const void *k_pages, const void *v_pages, int32_t num_pages, const int32_t *table) {
   if (any_key && (!k_pages || !v_pages || !table))
     return fail(ADASERVE_ERR_INVALID_ARGUMENT, "k_pages, v_pages and block_table are required when a context is non-empty");
@@ -285,6 +309,8 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
   a.group = num_q_heads / num_kv_heads;
   a.sm_scale = sm_scale;
   a.scale_log2 = sm_scale * 1.4426950408889634f;
+  a.tile_rows = 128;
+  fill_prompt_table(a, token_indptr_host, context_len_host);
   return launch_status(launch_prompt_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
                        "prompt attention launch");
 }

@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "plan.h"
+
 namespace adaserve {
 
 constexpr int kMaxHeads = 4096;          // of one kind, in the serving operators
@@ -37,6 +39,20 @@ struct RopeAppendArgs {
 
 hipError_t launch_rope_append(const RopeAppendArgs &a, bool bf16, hipStream_t stream);
 
+// A request of a prompt attention call, in dispatch order.
+constexpr int kPromptTable = 128;
+struct PromptEntry {
+  int32_t unit_end;   // exclusive end of its workgroups
+  int32_t request;
+  int32_t token0;     // token_indptr[request]
+  int32_t n, ctx;     // its rows and its keys
+};
+
+// Row tiles of n tokens with `group` query heads per kv-head.
+ADASERVE_HD int32_t prompt_tiles(int32_t n, int32_t group, int32_t tile_rows) {
+  return (int32_t)(((int64_t)n * group + tile_rows - 1) / tile_rows);
+}
+
 struct PagedAttnArgs {
   int32_t num_requests;
   const int32_t *token_indptr;   // [B + 1] (prompt attention)
@@ -54,6 +70,10 @@ struct PagedAttnArgs {
   int32_t group;                 // Hq / Hkv
   float sm_scale;
   float scale_log2;              // sm_scale * log2(e)
+  // prompt attention
+  int64_t units;                 // workgroups
+  int32_t tile_rows;             // rows per workgroup: 256 or 128
+  int32_t table_count;           // entries used in table[] (0: the device arrays are scanned)
   // decode attention (DecodePlan)
   int32_t max_context;
   int32_t rows_per_group;
@@ -64,6 +84,7 @@ struct PagedAttnArgs {
   int32_t *ws_request;           // [B, 2] first unit, units; null: nothing is split
   float *ws_ml;                  // [units, heads, row groups, kDecodeRows, 2] reference, sum
   float *ws_o;                   // [units, heads, row groups, kDecodeRows, D] weighted sums of V
+  PromptEntry table[kPromptTable];
 };
 
 // Decode attention's work, from sizes alone.  Query heads that share a kv-head
