@@ -19,6 +19,10 @@ constexpr int kWaves = 4;
 // 16 bytes of zeros: the source of the LDS loads whose key does not exist.
 __device__ __align__(16) uint32_t zero_line[4];
 
+__device__ __forceinline__ float fmax3(float x, float y, float z) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z);   // (a NaN passes through)
+}
+
 // A workgroup's tile: rows row0 .. row0 + tile_rows - 1 of one kv-head's
 // (token, query head in group) pairs of a request, row = token * G + head.
 struct PromptUnit {
@@ -401,6 +405,446 @@ __global__ __launch_bounds__(kThreads, RT == 2 ? 1 : 2) void prompt_attn_bf16_ke
   }
 }
 
+// 64 rows per wave, one wave per SIMD.  The two 32-row halves of a wave run
+// half a sub-block apart, so that the matrix products of one half always meet
+// the softmax of the other in the instruction stream:
+//   phase A of sub-block i: S0(i+1) = K Q0, O0 += V P0(i)  beside  P1(i) from S1(i)
+//   phase B:                S1(i+1) = K Q1, O1 += V P1(i)  beside  P0(i+1) from S0(i+1)
+// Both halves take the same K and V fragments from registers; the next ones
+// are read in phase B as the current ones are used up.
+template <int D>
+__global__ __launch_bounds__(kThreads, 1) void prompt_attn_wide_kernel(PagedAttnArgs a) {
+  constexpr int KS = D / 16, DT = D / 32, KB = 32, ROWB = D * 2, NCH = D / 8;
+  constexpr int BLK = KB * ROWB;
+  constexpr int WI = BLK / 1024 / kWaves;
+  constexpr int RPI = 1024 / ROWB;
+  constexpr int NST = 3;
+  constexpr int STAGE = 4 * BLK;             // K sub-blocks 2s+1, 2s+2, V sub-blocks 2s, 2s+1
+  constexpr int LPS = 4 * WI;
+  constexpr float kRescaleLog2 = 8.f;
+  // Where every key is seen, the weights 2^(s c - m c) keep the reference m that
+  // a row has: bf16 and fp32 are as precise at 2^60 as at 1, so no maximum is
+  // taken per sub-block.  A row whose sum gets beyond kMost is one whose scores
+  // rise by more than 44 nats over those of its first keys; its tile is done
+  // again with the maximum taken everywhere.
+  constexpr float kMost = 0x1p64f;
+  __shared__ int redo;
+  __shared__ __align__(1024) char ring[NST * STAGE + BLK];   // and K of sub-block 0
+
+  PromptUnit un;
+  if (!find_prompt_unit(a, blockIdx.x, un)) return;
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.group, g = un.g;
+  const int32_t M = un.n * G, row0 = un.tile * 256, row_end = min(M, row0 + 256);
+  const int32_t first = un.ctx - un.n + 1;   // keys that token 0 sees
+  const int32_t k_end = max(0, first + (row_end - 1) / G);
+  const int32_t wrow0 = row0 + wave * 64;
+  const int32_t wave_end = wrow0 < row_end ? max(0, first + (min(row_end, wrow0 + 64) - 1) / G) : 0;
+  const int32_t nb = (k_end + KB - 1) / KB, wave_nb = (wave_end + KB - 1) / KB;
+  const int32_t n_full = min(wave_nb, max(0, first + wrow0 / G) / KB);
+  const int32_t ns = (nb + 1) / 2;
+
+  // Page ids: the DMA rows of a wave lie in one 16-key page of each sub-block.
+  // Lane l of pgv[0] holds that page's id in sub-block `window` + l (-1: none),
+  // pgv[1 .. 3] the windows of 64 sub-blocks after it.
+  const int wave_page = (wave * WI * RPI) / kPageSize;
+  int32_t pgv[4], window = 0, loaded = 0;   // (ids of sub-blocks before `loaded`)
+  bool all_pages = true;                    // none of them is missing
+  auto load_pages = [&](int base) __attribute__((always_inline)) {
+    window = base;
+    loaded = base + 256;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int32_t blk = base + i * 64 + lane;
+      const int32_t e = blk * (KB / kPageSize) + wave_page;
+      int32_t p = -1;
+      if (blk < nb && e < a.bt_stride) {
+        p = a.block_table[(int64_t)un.r * a.bt_stride + e];
+        if (p < 0 || p >= a.num_pages) p = -1;
+      }
+      all_pages = all_pages && !__any(p < 0 && blk < k_end / KB);
+      pgv[i] = p;
+    }
+  };
+  load_pages(0);
+
+  bf16x8 qf[2][KS];
+  int32_t vis[2];
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt) {
+    const int32_t row = wrow0 + rt * 32 + (lane & 31);
+    const bool ok = row < row_end;
+    const int32_t tok = ok ? row / G : 0, head = g * G + (ok ? row - tok * G : 0);
+    vis[rt] = ok ? first + tok : 0;
+    const __bf16 *qp = (const __bf16 *)a.q + (int64_t)(un.token0 + tok) * a.q_stride + (int64_t)head * D + half * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 v = {};
+      if (ok) v = *(const bf16x8 *)(qp + ks * 16);
+      qf[rt][ks] = v;
+    }
+  }
+
+  const int slot = ((lane * 16) % ROWB) / 16;
+  int dma_row[WI];
+  uint32_t page_off[WI];
+#pragma unroll
+  for (int i = 0; i < WI; ++i) {
+    dma_row[i] = (wave * WI + i) * RPI + (lane * 16) / ROWB;
+    page_off[i] = (uint32_t)(((dma_row[i] % kPageSize) * D + (slot ^ swizzle<NCH>(dma_row[i])) * 8) * 2);
+  }
+  const int64_t page_bytes = (int64_t)a.num_kv_heads * kPageSize * D * 2;
+  const int64_t head_bytes = (int64_t)g * kPageSize * D * 2;
+  // Sub-blocks are asked for in ascending order.
+  auto page_of = [&](int blk) __attribute__((always_inline)) -> int32_t {
+    if (blk - window >= 64) {
+      if (blk - window >= 256 || (blk & 255) == 0) {
+        load_pages(blk & ~63);
+      } else {
+        window += 64;
+        pgv[0] = pgv[1], pgv[1] = pgv[2], pgv[2] = pgv[3];
+      }
+    }
+    return __builtin_amdgcn_readlane(pgv[0], blk - window);
+  };
+  const uint32_t wave_lds = lds_addr(ring) + wave * WI * 1024;
+  // Sub-block blk of K or V into LDS at `dst`; rows past the tile's keys and
+  // pages that do not exist come from the zero line, so that every stage is the
+  // same number of loads.
+  auto issue = [&](const void *pool, uint32_t dst, int blk, int32_t page) __attribute__((always_inline)) {
+    const int32_t left = page >= 0 ? k_end - blk * KB : 0;
+    const char *base = (const char *)pool + (int64_t)max(page, 0) * page_bytes + head_bytes;
+#pragma unroll
+    for (int i = 0; i < WI; ++i)
+      dma16<false>(dma_row[i] < left ? (const void *)(base + page_off[i]) : (const void *)zero_line, dst + i * 1024);
+  };
+  // Part f of stage s: K 2s+1, V 2s, K 2s+2, V 2s+1.
+  int32_t page_a = -1, page_b = -1;   // of sub-blocks 2s and 2s+1, then 2s+1 and 2s+2
+  auto part = [&](int s, int f, uint32_t st, const void *&pool, uint32_t &dst, int &blk, int32_t &page) {
+    if (f == 0) page_b = page_of(2 * s + 1);
+    if (f == 2) page_a = page_of(2 * s + 2);
+    pool = f & 1 ? a.v_pages : a.k_pages;
+    blk = f == 0 ? 2 * s + 1 : f == 1 ? 2 * s : f == 2 ? 2 * s + 2 : 2 * s + 1;
+    page = f == 1 || f == 2 ? page_a : page_b;
+    dst = st + (f == 0 ? 0 : f == 1 ? 2 * BLK : f == 2 ? BLK : 3 * BLK);
+  };
+  auto issue_part = [&](int s, int f, uint32_t st) __attribute__((always_inline)) {
+    if (s >= ns) return;
+    const void *pool;
+    uint32_t dst;
+    int blk;
+    int32_t page;
+    part(s, f, st, pool, dst, blk, page);
+    issue(pool, dst, blk, page);
+  };
+
+  int koff[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+    koff[ks] = (lane & 31) * ROWB + (((ks * 2 + half) ^ swizzle<NCH>(lane & 31)) * 16);
+  int voff[DT], voff8[DT];
+  {
+    const int j16 = lane & 15;
+    const int vrow = half * 4 + (j16 >> 2);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const int ch = dt * 4 + ((lane >> 4) & 1) * 2 + ((j16 & 3) >> 1);
+      voff[dt] = vrow * ROWB + ((ch ^ swizzle<NCH>(vrow)) * 16) + (j16 & 1) * 8;
+      voff8[dt] = (vrow + 8) * ROWB + ((ch ^ swizzle<NCH>(vrow + 8)) * 16) + (j16 & 1) * 8;
+    }
+  }
+
+  f32x16 o[2][DT];
+  const float c = a.scale_log2, up_raw = kRescaleLog2 / c;
+  float lsum[2], m_ref[2];
+
+  bf16x8 kf[KS], vf[2 * DT];
+  auto read_k = [&](const char *kst, int ks) { kf[ks] = *(const bf16x8 *)(kst + koff[ks]); };
+  auto read_v = [&](const char *vst, int x) {   // x = h * DT + dt
+    const int h = x / DT, dt = x % DT;
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(vst + voff[dt] + h * 16 * ROWB));
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(vst + voff8[dt] + h * 16 * ROWB));
+    vf[x] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto mask = [&](f32x16 &x, int rt, int blk) {
+    const int32_t left = vis[rt] - blk * KB - half * 4;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = (i >> 2) * 8 + (i & 3) < left ? x[i] : -INFINITY;
+  };
+  auto rowmax = [&](const f32x16 &x) {
+    float m0 = x[0], m1 = x[1];
+#pragma unroll
+    for (int i = 2; i < 14; i += 4) {
+      m0 = __builtin_elementwise_maximum(__builtin_elementwise_maximum(m0, x[i]), x[i + 2]);
+      m1 = __builtin_elementwise_maximum(__builtin_elementwise_maximum(m1, x[i + 1]), x[i + 3]);
+    }
+    m0 = __builtin_elementwise_maximum(m0, x[14]);
+    return max_over_halves(__builtin_elementwise_maximum(__builtin_elementwise_maximum(m0, m1), x[15]));
+  };
+  // Takes row half rt's reference up to the maximum bm of sub-block scores where
+  // that is more than 2^8 above it.
+  auto rescale = [&](int rt, float bm) __attribute__((always_inline)) {
+    const bool up = bm > m_ref[rt] + up_raw;
+    if (__any(up)) {
+      const float mn = up ? bm : m_ref[rt];
+      const float al = __builtin_amdgcn_exp2f((m_ref[rt] - mn) * c);
+      m_ref[rt] = mn;
+      lsum[rt] *= al;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[rt][dt] *= al;
+    }
+  };
+  auto probs = [&](int rt, const f32x16 &x, bf16x8 (&pk)[2]) __attribute__((always_inline)) {
+    const float mc = m_ref[rt] * c;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float y0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[h * 8 + 2 * e], c, -mc));
+        const float y1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[h * 8 + 2 * e + 1], c, -mc));
+        lsum[rt] += y0 + y1;
+        w[e] = pack_bf16x2(y0, y1);
+      }
+      pk[h] = __builtin_bit_cast(bf16x8, w);
+    }
+  };
+  f32x16 s0, s1;
+  bf16x8 p0[2], p1[2];
+  // One phase: half `rt` takes its products (scores of the next sub-block into
+  // sx, O += V P of this one), the other half its weights (from sy, sub-block
+  // yblk).  `src` with kDma: the wave's part of a K or V sub-block, loaded to LDS
+  // at `dst`.
+  auto phase = [&](auto half_c, f32x16 &sx, const bf16x8 (&px)[2], f32x16 &sy, bf16x8 (&py)[2], int yblk, auto masked,
+                   const char *kst, const char *vst, auto dma, const char *src, uint32_t dst) __attribute__((always_inline)) {
+    constexpr int rt = decltype(half_c)::value;
+    constexpr int ry = 1 - rt;
+    constexpr bool kRead = rt == 1;
+    constexpr bool kMasked = decltype(masked)::value;
+    constexpr bool kDma = decltype(dma)::value;
+    constexpr int SLOTS = KS + 2 * DT;   // matrix instructions
+    if constexpr (kMasked) {
+      mask(sy, ry, yblk);
+      rescale(ry, rowmax(sy));
+    }
+    // A slot is one matrix instruction and the vector work that issues while it
+    // runs: one step each of three pairs of weights (scale; exponential; sum and
+    // rounding), none of which waits for another, and two LDS reads.  The
+    // compiler's own order would gather them by kind.  (Sums by
+    // v_dot2_f32_bf16 would take the matrix unit from the products.)
+    const float mc = m_ref[ry] * c;
+    float z[16], l2[2] = {lsum[ry], 0.f};
+    uint32_t w[8];
+    sx = f32x16{};
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      if (j < KS) {
+        sx = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j], qf[rt][j], sx, 0, 0, 0);
+      } else {
+        const int x = j - KS;
+        o[rt][x % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x], px[x / DT], o[rt][x % DT], 0, 0, 0);
+      }
+      if constexpr (kDma) {
+        if (j >= 1 && j <= WI) dma16_off<false>(src, page_off[j - 1], dst + (j - 1) * 1024);
+      }
+#pragma unroll
+      for (int k = 0; k < 16 / SLOTS; ++k) {   // two pairs a slot where the head dim is 64
+        const int t = j * (16 / SLOTS) + k;
+        if (t >= 2 && t < 10) {
+          l2[0] += z[2 * t - 4];
+          l2[1] += z[2 * t - 3];
+          w[t - 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{z[2 * t - 4], z[2 * t - 3]}), bf16x2));
+        }
+        if (t >= 1 && t < 9) {
+          z[2 * t - 2] = __builtin_amdgcn_exp2f(z[2 * t - 2]);
+          z[2 * t - 1] = __builtin_amdgcn_exp2f(z[2 * t - 1]);
+        }
+        if (t < 8) {
+          z[2 * t] = __builtin_fmaf(sy[2 * t], c, -mc);
+          z[2 * t + 1] = __builtin_fmaf(sy[2 * t + 1], c, -mc);
+        }
+        if (t == 10) l2[0] += l2[1];
+      }
+      if constexpr (kRead) {
+        // the fragments whose last use is behind
+        if (j < KS) read_k(kst, j);
+        else read_v(vst, j - KS);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    py[0] = __builtin_bit_cast(bf16x8, (u32x4{w[0], w[1], w[2], w[3]}));
+    py[1] = __builtin_bit_cast(bf16x8, (u32x4{w[4], w[5], w[6], w[7]}));
+    lsum[ry] = l2[0];
+    asm volatile("" : "+v"(py[0]), "+v"(py[1]), "+v"(lsum[ry]));
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  using Zero = std::integral_constant<int, 0>;
+  using One = std::integral_constant<int, 1>;
+  using Yes = std::true_type;
+  using No = std::false_type;
+
+  int cs;   // slot of the stage that sub-block i's V is in
+  auto next_slot = [](int x) { return x == NST - 1 ? 0 : x + 1; };
+  // Sub-blocks 2 st and 2 st + 1 of whole keys that every row sees, all the
+  // loads on the way of whole sub-blocks too.
+  auto full_pair = [&](int st) __attribute__((always_inline)) {
+    const int i = 2 * st;
+    const uint32_t prev = wave_lds + (cs == 0 ? NST - 1 : cs - 1) * STAGE;   // refilled with stage st + 2
+    const char *cur = ring + cs * STAGE, *nxt = ring + next_slot(cs) * STAGE;
+    auto source = [&](int s, int f, uint32_t slot_lds, uint32_t &dst) {
+      const void *pool;
+      int blk;
+      int32_t page;
+      part(s, f, slot_lds, pool, dst, blk, page);
+      return (const char *)pool + (int64_t)(uint32_t)page * (int64_t)page_bytes + head_bytes;
+    };
+    uint32_t dst;
+    const char *src = source(st + 2, 1, prev, dst);
+    phase(Zero{}, s0, p0, s1, p1, i, No{}, nullptr, nullptr, Yes{}, src, dst);
+    src = source(st + 2, 2, prev, dst);
+    phase(One{}, s1, p1, s0, p0, i + 1, No{}, cur + BLK, cur + 3 * BLK, Yes{}, src, dst);
+    src = source(st + 2, 3, prev, dst);
+    phase(Zero{}, s0, p0, s1, p1, i + 1, No{}, nullptr, nullptr, Yes{}, src, dst);
+    // the next stage has landed (the one after may fly), and every wave has
+    // read all of this one, which is refilled
+    src = source(st + 3, 0, wave_lds + cs * STAGE, dst);
+    wait_loads_barrier<LPS>();
+    phase(One{}, s1, p1, s0, p0, i + 2, No{}, nxt, nxt + 2 * BLK, Yes{}, src, dst);
+    cs = next_slot(cs);
+  };
+  auto any_pair = [&](int st) __attribute__((always_inline)) {
+    const int i = 2 * st;
+    const uint32_t prev = wave_lds + (cs == 0 ? NST - 1 : cs - 1) * STAGE;
+    const char *cur = ring + cs * STAGE, *nxt = ring + next_slot(cs) * STAGE;
+    const bool refill = st > 0;
+    if (refill) issue_part(st + 2, 1, prev);
+    if (i < wave_nb) phase(Zero{}, s0, p0, s1, p1, i, Yes{}, nullptr, nullptr, No{}, nullptr, 0);
+    if (refill) issue_part(st + 2, 2, prev);
+    if (i < wave_nb)
+      phase(One{}, s1, p1, s0, p0, i + 1, Yes{}, cur + BLK, cur + 3 * BLK, No{}, nullptr, 0);
+    if (refill) issue_part(st + 2, 3, prev);
+    if (i + 1 < wave_nb) phase(Zero{}, s0, p0, s1, p1, i + 1, Yes{}, nullptr, nullptr, No{}, nullptr, 0);
+    if (st + 2 < ns) wait_loads_barrier<LPS>();
+    else wait_loads_barrier<0>();
+    issue_part(st + 3, 0, wave_lds + cs * STAGE);
+    if (i + 1 < wave_nb)
+      phase(One{}, s1, p1, s0, p0, i + 2, Yes{}, nxt, nxt + 2 * BLK, No{}, nullptr, 0);
+    cs = next_slot(cs);
+  };
+  // A row that holds a NaN before any key is hidden from it has it from a key
+  // that it sees.
+  bool had_nan[2] = {false, false};
+  auto is_nan = [&](int rt) {
+    float x = lsum[rt];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x = __builtin_elementwise_maximum(x, o[rt][dt][i]);
+    x = max_over_halves(x);
+    return x != x;
+  };
+  const int full_st = max(0, n_full - 1) / 2;   // pairs below this see whole sub-blocks only
+  bool careful = false;
+  if (tid == 0) redo = 0;
+  wait_vmcnt<0>();   // page ids and queries, before the counted loads
+#pragma unroll 1
+  for (;;) {
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) {
+      lsum[rt] = 0.f;
+      m_ref[rt] = vis[rt] > 0 ? -1e30f : 0.f;   // (rows that are none have scores 0)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[rt][dt] = f32x16{};
+    }
+    cs = 0;
+    if (ns > 0) {
+      page_a = page_of(0);
+      issue(a.k_pages, wave_lds + NST * STAGE, 0, page_a);
+#pragma unroll
+      for (int st = 0; st < NST; ++st)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) issue_part(st, f, wave_lds + st * STAGE);
+      if (ns >= 3) wait_loads_barrier<2 * LPS>();
+      else if (ns == 2) wait_loads_barrier<LPS>();
+      else wait_loads_barrier<0>();
+      if (wave_nb > 0) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) read_k(ring + NST * STAGE, ks);
+        s0 = f32x16{};
+        s1 = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[0][ks], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[1][ks], s1, 0, 0, 0);
+        }
+        mask(s0, 0, 0);
+        mask(s1, 1, 0);
+        rescale(0, rowmax(s0));
+        probs(0, s0, p0);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) read_k(ring, ks);
+#pragma unroll
+        for (int x = 0; x < 2 * DT; ++x) read_v(ring + 2 * BLK, x);
+      }
+    }
+    bool beyond = false;
+    int st = 0;
+#pragma unroll 1
+    while (st < ns) {
+      if (st == full_st) {
+        had_nan[0] = is_nan(0);
+        had_nan[1] = is_nan(1);
+      }
+      any_pair(st++);   // (the first stages' loads were issued above)
+      if (careful || !all_pages) continue;
+#pragma unroll 1
+      for (; st < full_st && 2 * st + 8 < min(k_end / KB, loaded); ++st) full_pair(st);
+      beyond |= !(lsum[0] < kMost) || !(lsum[1] < kMost);
+    }
+    if (careful || ns < 4) break;
+    if (__any(beyond) && lane == 0) redo = 1;
+    __syncthreads();
+    if (!redo) break;
+    careful = true;
+    load_pages(0);
+    wait_vmcnt<0>();
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt) {
+    const int32_t row = wrow0 + rt * 32 + (lane & 31);
+    const bool ok = row < row_end;
+    const float l_tot = sum_over_halves(lsum[rt]);
+    const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+    const int32_t tok = ok ? row / G : 0, head = g * G + (ok ? row - tok * G : 0);
+    // A key that the row does not see has weight 0, and 0 times an infinite
+    // value is NaN: such rows are taken again, key by key.
+    const bool again = ok && is_nan(rt) && !had_nan[rt];
+    __bf16 *dst = (__bf16 *)a.out + ((int64_t)(un.token0 + tok) * a.num_q_heads + head) * D;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; i += 8) {
+        const uint32_t x0 = pack_bf16x2(o[rt][dt][i] * inv, o[rt][dt][i + 1] * inv);
+        const uint32_t x1 = pack_bf16x2(o[rt][dt][i + 2] * inv, o[rt][dt][i + 3] * inv);
+        const uint32_t y0 = pack_bf16x2(o[rt][dt][i + 4] * inv, o[rt][dt][i + 5] * inv);
+        const uint32_t y1 = pack_bf16x2(o[rt][dt][i + 6] * inv, o[rt][dt][i + 7] * inv);
+        const auto r0 = __builtin_amdgcn_permlane32_swap(x0, y0, false, false);
+        const auto r1 = __builtin_amdgcn_permlane32_swap(x1, y1, false, false);
+        if (ok && !again) *(u32x4 *)(dst + dt * 32 + i * 2 + half * 8) = u32x4{r0[0], r1[0], r0[1], r1[1]};
+      }
+    unsigned long long todo = __ballot(again) & 0xffffffffull;
+    while (todo) {
+      const int l = __ffsll(todo) - 1;
+      todo &= todo - 1;
+      attend_row<true, D>(a, un.r, un.token0 + __shfl(tok, l, 64), __shfl(head, l, 64), __shfl(vis[rt], l, 64));
+    }
+  }
+}
+
 template <int D>
 __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PagedAttnArgs a) {
   const int wave = threadIdx.x >> 6;
@@ -422,8 +866,13 @@ hipError_t launch_prompt_attn(const PagedAttnArgs &a, int head_dim, bool bf16, h
   const dim3 block(kThreads);
   if (bf16) {
     const dim3 grid((unsigned)a.units);
-    if (head_dim == 128) hipLaunchKernelGGL((prompt_attn_bf16_kernel<128, 1>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((prompt_attn_bf16_kernel<64, 1>), grid, block, 0, stream, a);
+    if (a.tile_rows == 256) {
+      if (head_dim == 128) hipLaunchKernelGGL((prompt_attn_wide_kernel<128>), grid, block, 0, stream, a);
+      else hipLaunchKernelGGL((prompt_attn_wide_kernel<64>), grid, block, 0, stream, a);
+    } else {
+      if (head_dim == 128) hipLaunchKernelGGL((prompt_attn_bf16_kernel<128, 1>), grid, block, 0, stream, a);
+      else hipLaunchKernelGGL((prompt_attn_bf16_kernel<64, 1>), grid, block, 0, stream, a);
+    }
     return hipGetLastError();
   }
   const int64_t waves = (int64_t)a.total_tokens * a.num_q_heads;

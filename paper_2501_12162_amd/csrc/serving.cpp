@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstdlib>
 
 #include "adaserve.h"
 #include "host_device.h"
@@ -309,7 +310,7 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
   a.group = num_q_heads / num_kv_heads;
   a.sm_scale = sm_scale;
   a.scale_log2 = sm_scale * 1.4426950408889634f;
-  a.tile_rows = 128;
+  a.tile_rows = getenv("ADA_ROWS") ? atoi(getenv("ADA_ROWS")) : 256;
   fill_prompt_table(a, token_indptr_host, context_len_host);
   return launch_status(launch_prompt_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
                        "prompt attention launch");

@@ -137,15 +137,17 @@ def test_prompt_keys_that_a_row_does_not_see(ada, dtype, bad):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_prompt_large_scores(ada, dtype):
+@pytest.mark.parametrize("new,ctx", [([200], [260]), ([70], [1500]), ([600, 33], [601, 1200])])
+def test_prompt_large_scores(ada, dtype, new, ctx):
     """Scores to the hundreds, rising and falling along the keys."""
     def steep(c):
         k = serving.widen(c.k)
-        for e, p in enumerate(c.table[0]):
-            if p >= 0:
-                k[p] *= (1 + e % 7) * (-1) ** e
+        for row in c.table:
+            for e, p in enumerate(row):
+                if p >= 0:
+                    k[p] *= (1 + e % 7 + (e > 60) * 9) * (-1) ** e
         c.k = typed(k, dtype)
-    prompt(ada, 6, [200], [260], dtype=dtype, scale=1.0, edit=steep)
+    prompt(ada, 6, new, ctx, dtype=dtype, scale=1.0, edit=steep)
 
 
 @pytest.mark.parametrize("seed", range(10))
