@@ -718,13 +718,12 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_wide_kernel(PagedAttn
     const int i = 2 * st;
     const uint32_t prev = wave_lds + (cs == 0 ? NST - 1 : cs - 1) * STAGE;
     const char *cur = ring + cs * STAGE, *nxt = ring + next_slot(cs) * STAGE;
-    const bool refill = st > 0;
-    if (refill) issue_part(st + 2, 1, prev);
+    issue_part(st + 2, 1, prev);
     if (i < wave_nb) phase(Zero{}, s0, p0, s1, p1, i, Yes{}, nullptr, nullptr, No{}, nullptr, 0);
-    if (refill) issue_part(st + 2, 2, prev);
+    issue_part(st + 2, 2, prev);
     if (i < wave_nb)
       phase(One{}, s1, p1, s0, p0, i + 1, Yes{}, cur + BLK, cur + 3 * BLK, No{}, nullptr, 0);
-    if (refill) issue_part(st + 2, 3, prev);
+    issue_part(st + 2, 3, prev);
     if (i + 1 < wave_nb) phase(Zero{}, s0, p0, s1, p1, i + 1, Yes{}, nullptr, nullptr, No{}, nullptr, 0);
     if (st + 2 < ns) wait_loads_barrier<LPS>();
     else wait_loads_barrier<0>();
@@ -763,10 +762,11 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_wide_kernel(PagedAttn
       page_a = page_of(0);
       issue(a.k_pages, wave_lds + NST * STAGE, 0, page_a);
 #pragma unroll
-      for (int st = 0; st < NST; ++st)
+      for (int st = 0; st < NST - 1; ++st)
 #pragma unroll
         for (int f = 0; f < 4; ++f) issue_part(st, f, wave_lds + st * STAGE);
-      if (ns >= 3) wait_loads_barrier<2 * LPS>();
+      issue_part(NST - 1, 0, wave_lds + (NST - 1) * STAGE);
+      if (ns >= 3) wait_loads_barrier<LPS + WI>();
       else if (ns == 2) wait_loads_barrier<LPS>();
       else wait_loads_barrier<0>();
       if (wave_nb > 0) {
@@ -782,6 +782,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_wide_kernel(PagedAttn
         mask(s0, 0, 0);
         mask(s1, 1, 0);
         rescale(0, rowmax(s0));
+        rescale(1, rowmax(s1));
         probs(0, s0, p0);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) read_k(ring, ks);
@@ -793,15 +794,16 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_wide_kernel(PagedAttn
     int st = 0;
 #pragma unroll 1
     while (st < ns) {
+      if (!careful && all_pages) {
+#pragma unroll 1
+        for (; st < full_st && 2 * st + 8 < min(k_end / KB, loaded); ++st) full_pair(st);
+        beyond |= !(lsum[0] < kMost) || !(lsum[1] < kMost);
+      }
       if (st == full_st) {
         had_nan[0] = is_nan(0);
         had_nan[1] = is_nan(1);
       }
-      any_pair(st++);   // (the first stages' loads were issued above)
-      if (careful || !all_pages) continue;
-#pragma unroll 1
-      for (; st < full_st && 2 * st + 8 < min(k_end / KB, loaded); ++st) full_pair(st);
-      beyond |= !(lsum[0] < kMost) || !(lsum[1] < kMost);
+      any_pair(st++);
     }
     if (careful || ns < 4) break;
     if (__any(beyond) && lane == 0) redo = 1;
