@@ -39,10 +39,12 @@ struct RopeAppendArgs {
 
 hipError_t launch_rope_append(const RopeAppendArgs &a, bool bf16, hipStream_t stream);
 
-// A request of a prompt attention call, in dispatch order.
+// The requests of a prompt attention call in descending order of tiles.
+constexpr int kPromptTileRows = 256;   // 4 waves x 64 rows
+constexpr int kPromptGrid = 256;       // workgroups on the device at a time: one per CU
 constexpr int kPromptTable = 128;
 struct PromptEntry {
-  int32_t unit_end;   // exclusive end of its workgroups
+  int32_t unit_end;   // exclusive end of the units of the levels that this and the requests before it have
   int32_t request;
   int32_t token0;     // token_indptr[request]
   int32_t n, ctx;     // its rows and its keys
@@ -71,8 +73,8 @@ struct PagedAttnArgs {
   float sm_scale;
   float scale_log2;              // sm_scale * log2(e)
   // prompt attention
-  int64_t units;                 // workgroups
-  int32_t tile_rows;             // rows per workgroup: 256 or 128
+  int64_t units;                 // tiles of all heads
+  int32_t grid;                  // workgroups: one per unit, or kPromptGrid
   int32_t table_count;           // entries used in table[] (0: the device arrays are scanned)
   // decode attention (DecodePlan)
   int32_t max_context;
