@@ -113,9 +113,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   constexpr int STAGE = 4 * BLK;             // K sub-blocks 2s+1, 2s+2, V sub-blocks 2s, 2s+1
   constexpr int LPS = 4 * WI;
   constexpr float kRescaleLog2 = 8.f;
-  // Where every key is seen, the weights 2^(s c - m c) keep the reference m that
-  // a row has: bf16 and fp32 are as precise at 2^60 as at 1, so no maximum is
-  // taken per sub-block.  A row whose sum gets beyond kMost is one whose scores
+  // The weights 2^(s c - m c) keep the reference m that a row has from its first
+  // 32 keys: bf16 and fp32 are as precise at 2^60 as at 1, so no maximum is taken
+  // per sub-block.  A row whose sum gets beyond kMost is one whose scores
   // rise by more than 44 nats over those of its first keys; its tile is done
   // again with the maximum taken everywhere.
   constexpr float kMost = 0x1p64f;
@@ -151,27 +151,25 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   derive();
 
   // Page ids: the DMA rows of a wave lie in one 16-key page of each sub-block.
-  // Lane l of pgv[0] holds that page's id in sub-block `window` + l (-1: none),
-  // pgv[1 .. 3] the windows of 64 sub-blocks after it.
+  // Lane l of `pages` holds that page's id in sub-block `window` + l (-1: none),
+  // `pages_after` the 64 sub-blocks after those.
   const int wave_page = (wave * WI * RPI) / kPageSize;
-  int32_t pgv[4], window = 0, loaded = 0;   // (ids of sub-blocks before `loaded`)
-  bool all_pages = true;                    // none of them is missing
-  auto load_pages = [&](int base) __attribute__((always_inline)) {
-    window = base;
-    loaded = base + 256;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int32_t blk = base + i * 64 + lane;
-      const int32_t e = blk * (KB / kPageSize) + wave_page;
-      int32_t p = -1;
-      if (blk < nb && e < a.bt_stride) {
-        p = a.block_table[(int64_t)un.r * a.bt_stride + e];
-        if (p < 0 || p >= a.num_pages) p = -1;
-      }
-      all_pages = all_pages && !__any(p < 0 && blk < k_end / KB);
-      pgv[i] = p;
-    }
+  int32_t pages, pages_after, window;
+  bool all_pages;   // no whole sub-block of the windows so far lacks its page
+  auto load_pages = [&](const PromptUnit &of, int base) __attribute__((always_inline)) -> int32_t {
+    const int32_t e = (base + lane) * (KB / kPageSize) + wave_page;
+    return e < a.bt_stride && e < (of.ctx + kPageSize - 1) / kPageSize ? a.block_table[(int64_t)of.r * a.bt_stride + e] : -1;
   };
+  auto take_pages = [&](int32_t ids) __attribute__((always_inline)) {
+    pages = ids >= 0 && ids < a.num_pages ? ids : -1;
+    all_pages = all_pages && !__any(pages < 0 && window + lane < k_end / KB);
+    pages_after = load_pages(un, window + 64);
+  };
+  auto next_window = [&]() __attribute__((always_inline)) {
+    window += 64;
+    take_pages(pages_after);
+  };
+
   // Query fragments (B operand of S^T = K Q^T): lane holds row (lane & 31) of
   // each half, head-dim elements ks*16 + (lane >> 5)*8 .. +7.
   bf16x8 qf[2][KS];
@@ -204,15 +202,8 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   const int64_t page_bytes = (int64_t)a.num_kv_heads * kPageSize * D * 2;
   // Sub-blocks are asked for in ascending order.
   auto page_of = [&](int blk) __attribute__((always_inline)) -> int32_t {
-    if (blk - window >= 64) {
-      if (blk - window >= 256 || (blk & 255) == 0) {
-        load_pages(blk & ~63);
-      } else {
-        window += 64;
-        pgv[0] = pgv[1], pgv[1] = pgv[2], pgv[2] = pgv[3];
-      }
-    }
-    return __builtin_amdgcn_readlane(pgv[0], blk - window);
+    if (blk >= window + 64) next_window();
+    return __builtin_amdgcn_readlane(pages, blk - window);
   };
   const uint32_t wave_lds = lds_addr(ring) + wave * WI * 1024;
   // Sub-block blk of K or V into LDS at `dst`; rows past the tile's keys and
@@ -227,9 +218,10 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   };
   // Part f of stage s: K 2s+1, V 2s, K 2s+2, V 2s+1.
   int32_t page_a = -1, page_b = -1;   // of sub-blocks 2s and 2s+1, then 2s+1 and 2s+2
-  auto part = [&](int s, int f, uint32_t st, const void *&pool, uint32_t &dst, int &blk, int32_t &page) {
-    if (f == 0) page_b = page_of(2 * s + 1);
-    if (f == 2) page_a = page_of(2 * s + 2);
+  auto part = [&](int s, int f, uint32_t st, const void *&pool, uint32_t &dst, int &blk, int32_t &page,
+                  auto lookup) __attribute__((always_inline)) {
+    if (f == 0) page_b = lookup(2 * s + 1);
+    if (f == 2) page_a = lookup(2 * s + 2);
     pool = f & 1 ? a.v_pages : a.k_pages;
     blk = f == 0 ? 2 * s + 1 : f == 1 ? 2 * s : f == 2 ? 2 * s + 2 : 2 * s + 1;
     page = f == 1 || f == 2 ? page_a : page_b;
@@ -241,7 +233,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     uint32_t dst;
     int blk;
     int32_t page;
-    part(s, f, st, pool, dst, blk, page);
+    part(s, f, st, pool, dst, blk, page, page_of);
     issue(pool, dst, blk, page);
   };
 
@@ -318,6 +310,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   };
   f32x16 s0, s1;
   bf16x8 p0[2], p1[2];
+  bool careful = false;   // the tile is done again, with maxima
   // One phase: half `rt` takes its products (scores of the next sub-block into
   // sx, O += V P of this one), the other half its weights (from sy, sub-block
   // yblk).  `src` with kDma: the wave's part of a K or V sub-block, loaded to LDS
@@ -330,10 +323,8 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     constexpr bool kMasked = decltype(masked)::value;
     constexpr bool kDma = decltype(dma)::value;
     constexpr int SLOTS = KS + 2 * DT;   // matrix instructions
-    if constexpr (kMasked) {
-      mask(sy, ry, yblk);
-      rescale(ry, rowmax(sy));
-    }
+    if constexpr (kMasked) mask(sy, ry, yblk);
+    if (kMasked && careful) rescale(ry, rowmax(sy));
     // A slot is one matrix instruction and the vector work that issues while it
     // runs: one step each of three pairs of weights (scale; exponential; sum and
     // rounding), none of which waits for another, and two LDS reads.  The
@@ -403,7 +394,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
       const void *pool;
       int blk;
       int32_t page;
-      part(s, f, slot_lds, pool, dst, blk, page);
+      part(s, f, slot_lds, pool, dst, blk, page, [&](int b) { return __builtin_amdgcn_readlane(pages, b - window); });
       return (const char *)pool + (int64_t)(uint32_t)page * (int64_t)page_bytes + head_bytes;
     };
     uint32_t dst;
@@ -450,12 +441,14 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     x = max_over_halves(x);
     return x != x;
   };
-  // The unit's first loads: page ids and queries, then K of sub-block 0, stages 0
-  // and 1 and the first part of stage 2 (a step's loads go on from there).
-  auto start = [&]() __attribute__((always_inline)) {
-    load_pages(0);
+  // The unit's first loads (`ids`: its first page ids): queries, then K of
+  // sub-block 0, stages 0 and 1 and the first part of stage 2 (a step's loads go
+  // on from there).
+  auto start = [&](int32_t ids) __attribute__((always_inline)) {
     load_q();
-    wait_vmcnt<0>();   // before the counted loads
+    window = 0;
+    all_pages = true;
+    take_pages(ids);
     if (ns > 0) {
       page_a = page_of(0);
       issue(a.k_pages, wave_lds + NST * STAGE, 0, page_a);
@@ -466,9 +459,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
       issue_part(NST - 1, 0, wave_lds + (NST - 1) * STAGE);
     }
   };
-  bool careful = false, fresh = true;   // maxima everywhere; no store since the unit's loads
+  bool fresh = true;   // no store since the unit's loads
   if (tid == 0) redo = 0;
-  start();
+  start(load_pages(un, 0));
 #pragma unroll 1
   for (;;) {
 #pragma unroll
@@ -502,14 +495,22 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
 #pragma unroll
       for (int x = 0; x < 2 * DT; ++x) read_v(ring + 2 * BLK, x);
     }
-    bool beyond = false;
+    // the next unit and its first page ids, long before they are used
+    PromptUnit next;
+    int32_t next_ids = -1;
+    const bool more = a.units > gridDim.x &&
+                      find_prompt_unit(a, prompt_round_unit(blockIdx.x, round + 1, gridDim.x), entry, next);
+    if (more) next_ids = load_pages(next, 0);
     int st = 0;
 #pragma unroll 1
     while (st < ns) {
-      if (!careful && all_pages) {
+      if (!careful) {
 #pragma unroll 1
-        for (; st < full_st && 2 * st + 8 < min(k_end / KB, loaded); ++st) full_pair(st);
-        beyond |= !(lsum[0] < kMost) || !(lsum[1] < kMost);
+        for (; st < full_st && 2 * st + 8 < k_end / KB; ++st) {
+          if (2 * st + 6 >= window + 64) break;   // (the other path moves the window)
+          if (!all_pages) break;
+          full_pair(st);
+        }
       }
       if (st == full_st) {
         had_nan[0] = is_nan(0);
@@ -517,25 +518,26 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
       }
       any_pair(st++);
     }
-    if (__any(beyond) && lane == 0) redo = 1;
+    const bool beyond = !(lsum[0] < kMost) || !(lsum[1] < kMost);
+    if (!careful && __any(beyond) && lane == 0) redo = 1;
     __syncthreads();   // every wave is done with the ring, too
     if (redo) {
       __syncthreads();
       if (tid == 0) redo = 0;
       careful = true;
       fresh = true;
-      start();
+      start(load_pages(un, 0));
       continue;
     }
     // the next unit's loads, then this one's output
     const PromptUnit done = un;
     const int32_t done_end = row_end, done_row0 = wrow0;
     const int32_t done_vis[2] = {vis[0], vis[1]};
-    bool more = false;
-    if (a.units > gridDim.x) more = find_prompt_unit(a, prompt_round_unit(blockIdx.x, ++round, gridDim.x), entry, un);
     if (more) {
+      ++round;
+      un = next;
       derive();
-      start();
+      start(next_ids);
       careful = false;
       fresh = false;
     }
