@@ -109,9 +109,12 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   constexpr int BLK = KB * ROWB;
   constexpr int WI = BLK / 1024 / kWaves;
   constexpr int RPI = 1024 / ROWB;
-  constexpr int NST = 3;
-  constexpr int STAGE = 4 * BLK;             // K sub-blocks 2s+1, 2s+2, V sub-blocks 2s, 2s+1
-  constexpr int LPS = 4 * WI;
+  // Stage i of the ring holds K of sub-block i + 1 and V of sub-block i; three
+  // are in flight while one is read.  At 64 KB every place in it is within reach
+  // of an LDS instruction's offset.
+  constexpr int NST = 4;
+  constexpr int STAGE = 2 * BLK;
+  constexpr int LPS = 2 * WI;                // loads per wave and stage
   constexpr float kRescaleLog2 = 8.f;
   // The weights 2^(s c - m c) keep the reference m that a row has from its first
   // 32 keys: bf16 and fp32 are as precise at 2^60 as at 1, so no maximum is taken
@@ -120,7 +123,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   // again with the maximum taken everywhere.
   constexpr float kMost = 0x1p64f;
   __shared__ int redo;
-  __shared__ __align__(1024) char ring[NST * STAGE + BLK];   // and K of sub-block 0
+  __shared__ __align__(1024) char ring[NST * STAGE];   // (K of sub-block 0: in the last stage at first)
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -131,7 +134,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   if (!find_prompt_unit(a, blockIdx.x, entry, un)) return;
 
   // what follows from the unit
-  int32_t row_end, wrow0, first, k_end, nb, wave_nb, n_full, ns, full_st;
+  int32_t row_end, wrow0, first, k_end, nb, wave_nb, n_full;
   int64_t head_bytes;
   auto derive = [&]() __attribute__((always_inline)) {
     const int32_t row0 = un.tile * kTileRows;
@@ -144,8 +147,6 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     nb = (k_end + KB - 1) / KB;
     wave_nb = (wave_end + KB - 1) / KB;
     n_full = min(wave_nb, max(0, first + wrow0 / G) / KB);
-    ns = (nb + 1) / 2;
-    full_st = max(0, n_full - 1) / 2;             // pairs below this see whole sub-blocks only
     head_bytes = (int64_t)un.g * kPageSize * D * 2;
   };
   derive();
@@ -216,25 +217,17 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     for (int i = 0; i < WI; ++i)
       dma16<false>(dma_row[i] < left ? (const void *)(base + page_off[i]) : (const void *)zero_line, dst + i * 1024);
   };
-  // Part f of stage s: K 2s+1, V 2s, K 2s+2, V 2s+1.
-  int32_t page_a = -1, page_b = -1;   // of sub-blocks 2s and 2s+1, then 2s+1 and 2s+2
-  auto part = [&](int s, int f, uint32_t st, const void *&pool, uint32_t &dst, int &blk, int32_t &page,
-                  auto lookup) __attribute__((always_inline)) {
-    if (f == 0) page_b = lookup(2 * s + 1);
-    if (f == 2) page_a = lookup(2 * s + 2);
-    pool = f & 1 ? a.v_pages : a.k_pages;
-    blk = f == 0 ? 2 * s + 1 : f == 1 ? 2 * s : f == 2 ? 2 * s + 2 : 2 * s + 1;
-    page = f == 1 || f == 2 ? page_a : page_b;
-    dst = st + (f == 0 ? 0 : f == 1 ? 2 * BLK : f == 2 ? BLK : 3 * BLK);
+  // Stage i's loads: K first, then V.
+  int32_t page = -1;   // of sub-block i (before stage i's loads)
+  int32_t page_v = -1;
+  auto issue_k = [&](int i) __attribute__((always_inline)) {
+    if (i >= nb) return;
+    page_v = page;
+    page = page_of(i + 1);
+    issue(a.k_pages, wave_lds + (i & 3) * STAGE, i + 1, page);
   };
-  auto issue_part = [&](int s, int f, uint32_t st) __attribute__((always_inline)) {
-    if (s >= ns) return;
-    const void *pool;
-    uint32_t dst;
-    int blk;
-    int32_t page;
-    part(s, f, st, pool, dst, blk, page, page_of);
-    issue(pool, dst, blk, page);
+  auto issue_v = [&](int i) __attribute__((always_inline)) {
+    if (i < nb) issue(a.v_pages, wave_lds + (i & 3) * STAGE + BLK, i, page_v);
   };
 
   int koff[KS];
@@ -326,9 +319,10 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     if constexpr (kMasked) mask(sy, ry, yblk);
     if (kMasked && careful) rescale(ry, rowmax(sy));
     // A slot is one matrix instruction and the vector work that issues while it
-    // runs: one step each of three pairs of weights (scale; exponential; sum and
-    // rounding), none of which waits for another, and two LDS reads.  The
-    // compiler's own order would gather them by kind.  (Sums by
+    // runs: one step each of a few weights (scale; exponential; sum and
+    // rounding), none of which waits for another, and two LDS reads.  The empty
+    // asm statements and scheduling barriers keep that order: the compiler would
+    // gather the instructions by kind.  (Sums by
     // v_dot2_f32_bf16 would take the matrix unit from the products.)
     const float mc = m_ref[ry] * c;
     float z[16], l2[2] = {lsum[ry], 0.f};
@@ -346,23 +340,27 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
       if constexpr (kDma) {
         if (j >= 1 && j <= WI) dma16_off<false>(src, page_off[j - 1], dst + (j - 1) * 1024);
       }
+      // scaled by the end of slot j: the first `to` scores; exponentials are a slot
+      // behind, sums and roundings two
+      const auto to = [](int j) { return j < 0 ? 0 : (j + 1) * 16 / (SLOTS - 2) + 1 < 16 ? (j + 1) * 16 / (SLOTS - 2) + 1 : 16; };
 #pragma unroll
-      for (int k = 0; k < 16 / SLOTS; ++k) {   // two pairs a slot where the head dim is 64
-        const int t = j * (16 / SLOTS) + k;
-        if (t >= 2 && t < 10) {
-          l2[0] += z[2 * t - 4];
-          l2[1] += z[2 * t - 3];
-          w[t - 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{z[2 * t - 4], z[2 * t - 3]}), bf16x2));
+      for (int t = to(j - 3); t < to(j - 2); ++t) {
+        l2[t & 1] += z[t];
+        asm volatile("" : "+v"(l2[t & 1]));
+        if (t & 1) {
+          w[t / 2] = pack_bf16x2(z[t - 1], z[t]);
+          asm volatile("" : "+v"(w[t / 2]));
         }
-        if (t >= 1 && t < 9) {
-          z[2 * t - 2] = __builtin_amdgcn_exp2f(z[2 * t - 2]);
-          z[2 * t - 1] = __builtin_amdgcn_exp2f(z[2 * t - 1]);
-        }
-        if (t < 8) {
-          z[2 * t] = __builtin_fmaf(sy[2 * t], c, -mc);
-          z[2 * t + 1] = __builtin_fmaf(sy[2 * t + 1], c, -mc);
-        }
-        if (t == 10) l2[0] += l2[1];
+      }
+#pragma unroll
+      for (int t = to(j - 2); t < to(j - 1); ++t) {
+        z[t] = __builtin_amdgcn_exp2f(z[t]);
+        asm volatile("" : "+v"(z[t]));
+      }
+#pragma unroll
+      for (int t = to(j - 1); t < to(j); ++t) {
+        z[t] = __builtin_fmaf(sy[t], c, -mc);
+        asm volatile("" : "+v"(z[t]));
       }
       if constexpr (kRead) {
         // the fragments whose last use is behind
@@ -373,7 +371,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     }
     py[0] = __builtin_bit_cast(bf16x8, (u32x4{w[0], w[1], w[2], w[3]}));
     py[1] = __builtin_bit_cast(bf16x8, (u32x4{w[4], w[5], w[6], w[7]}));
-    lsum[ry] = l2[0];
+    lsum[ry] = l2[0] + l2[1];
     asm volatile("" : "+v"(py[0]), "+v"(py[1]), "+v"(lsum[ry]));
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -382,52 +380,29 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   using Yes = std::true_type;
   using No = std::false_type;
 
-  int cs;   // slot of the stage that sub-block i's V is in
-  auto next_slot = [](int x) { return x == NST - 1 ? 0 : x + 1; };
-  // Sub-blocks 2 st and 2 st + 1 of whole keys that every row sees, all the
-  // loads on the way of whole sub-blocks too.
-  auto full_pair = [&](int st) __attribute__((always_inline)) {
-    const int i = 2 * st;
-    const uint32_t prev = wave_lds + (cs == 0 ? NST - 1 : cs - 1) * STAGE;   // refilled with stage st + 2
-    const char *cur = ring + cs * STAGE, *nxt = ring + next_slot(cs) * STAGE;
-    auto source = [&](int s, int f, uint32_t slot_lds, uint32_t &dst) {
-      const void *pool;
-      int blk;
-      int32_t page;
-      part(s, f, slot_lds, pool, dst, blk, page, [&](int b) { return __builtin_amdgcn_readlane(pages, b - window); });
-      return (const char *)pool + (int64_t)(uint32_t)page * (int64_t)page_bytes + head_bytes;
-    };
-    uint32_t dst;
-    const char *src = source(st + 2, 1, prev, dst);
-    phase(Zero{}, s0, p0, s1, p1, i, No{}, nullptr, nullptr, Yes{}, src, dst);
-    src = source(st + 2, 2, prev, dst);
-    phase(One{}, s1, p1, s0, p0, i + 1, No{}, cur + BLK, cur + 3 * BLK, Yes{}, src, dst);
-    src = source(st + 2, 3, prev, dst);
-    phase(Zero{}, s0, p0, s1, p1, i + 1, No{}, nullptr, nullptr, Yes{}, src, dst);
-    // the next stage has landed (the one after may fly), and every wave has
-    // read all of this one, which is refilled
-    src = source(st + 3, 0, wave_lds + cs * STAGE, dst);
-    wait_loads_barrier<LPS>();
-    phase(One{}, s1, p1, s0, p0, i + 2, No{}, nxt, nxt + 2 * BLK, Yes{}, src, dst);
-    cs = next_slot(cs);
+  // Sub-block i, all of whose keys the wave's rows see, as they do those of
+  // sub-block i + 1, and all loads on the way of whole sub-blocks.  X = i mod 4.
+  // Phase B opens with the barrier after which stage i + 1 has landed (the two
+  // after it may fly) and stage i, which every wave has read, is refilled.
+  auto full_sub = [&](int i, auto slot_c) __attribute__((always_inline)) {
+    constexpr int X = decltype(slot_c)::value, Y = (X + 1) & 3, Z = (X + 3) & 3;
+    const char *src = (const char *)a.v_pages + (int64_t)(uint32_t)page_v * page_bytes + head_bytes;
+    phase(Zero{}, s0, p0, s1, p1, i, No{}, nullptr, nullptr, Yes{}, src, wave_lds + Z * STAGE + BLK);
+    page_v = page;
+    page = __builtin_amdgcn_readlane(pages, i + 5 - window);
+    src = (const char *)a.k_pages + (int64_t)(uint32_t)page * page_bytes + head_bytes;
+    wait_loads_barrier<2 * LPS>();
+    phase(One{}, s1, p1, s0, p0, i + 1, No{}, ring + Y * STAGE, ring + Y * STAGE + BLK, Yes{}, src, wave_lds + X * STAGE);
   };
-  auto any_pair = [&](int st) __attribute__((always_inline)) {
-    const int i = 2 * st;
-    const uint32_t prev = wave_lds + (cs == 0 ? NST - 1 : cs - 1) * STAGE;
-    const char *cur = ring + cs * STAGE, *nxt = ring + next_slot(cs) * STAGE;
-    issue_part(st + 2, 1, prev);
+  auto any_sub = [&](int i) __attribute__((always_inline)) {
+    issue_v(i + 3);
     if (i < wave_nb) phase(Zero{}, s0, p0, s1, p1, i, Yes{}, nullptr, nullptr, No{}, nullptr, 0);
-    issue_part(st + 2, 2, prev);
-    if (i < wave_nb)
-      phase(One{}, s1, p1, s0, p0, i + 1, Yes{}, cur + BLK, cur + 3 * BLK, No{}, nullptr, 0);
-    issue_part(st + 2, 3, prev);
-    if (i + 1 < wave_nb) phase(Zero{}, s0, p0, s1, p1, i + 1, Yes{}, nullptr, nullptr, No{}, nullptr, 0);
-    if (st + 2 < ns) wait_loads_barrier<LPS>();
+    if (i + 3 < nb) wait_loads_barrier<2 * LPS>();
+    else if (i + 2 < nb) wait_loads_barrier<LPS>();
     else wait_loads_barrier<0>();
-    issue_part(st + 3, 0, wave_lds + cs * STAGE);
-    if (i + 1 < wave_nb)
-      phase(One{}, s1, p1, s0, p0, i + 2, Yes{}, nxt, nxt + 2 * BLK, No{}, nullptr, 0);
-    cs = next_slot(cs);
+    issue_k(i + 4);
+    const char *nxt = ring + ((i + 1) & 3) * STAGE;
+    if (i < wave_nb) phase(One{}, s1, p1, s0, p0, i + 1, Yes{}, nxt, nxt + BLK, No{}, nullptr, 0);
   };
   // A row that holds a NaN before any key is hidden from it has it from a key
   // that it sees.
@@ -442,21 +417,20 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     return x != x;
   };
   // The unit's first loads (`ids`: its first page ids): queries, then K of
-  // sub-block 0, stages 0 and 1 and the first part of stage 2 (a step's loads go
-  // on from there).
+  // sub-block 0, stages 0 to 2 and K of stage 3 once sub-block 0's is used.
   auto start = [&](int32_t ids) __attribute__((always_inline)) {
     load_q();
     window = 0;
     all_pages = true;
     take_pages(ids);
-    if (ns > 0) {
-      page_a = page_of(0);
-      issue(a.k_pages, wave_lds + NST * STAGE, 0, page_a);
+    if (nb > 0) {
+      page = page_of(0);
+      issue(a.k_pages, wave_lds + 3 * STAGE, 0, page);
 #pragma unroll
-      for (int st = 0; st < NST - 1; ++st)
-#pragma unroll
-        for (int f = 0; f < 4; ++f) issue_part(st, f, wave_lds + st * STAGE);
-      issue_part(NST - 1, 0, wave_lds + (NST - 1) * STAGE);
+      for (int i = 0; i < 3; ++i) {
+        issue_k(i);
+        issue_v(i);
+      }
     }
   };
   bool fresh = true;   // no store since the unit's loads
@@ -471,13 +445,12 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[rt][dt] = f32x16{};
     }
-    cs = 0;
-    if (fresh && ns >= 3) wait_loads_barrier<LPS + WI>();
-    else if (fresh && ns == 2) wait_loads_barrier<LPS>();
+    if (fresh && nb >= 3) wait_loads_barrier<2 * LPS>();
+    else if (fresh && nb == 2) wait_loads_barrier<LPS>();
     else wait_loads_barrier<0>();
     if (wave_nb > 0) {
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) read_k(ring + NST * STAGE, ks);
+      for (int ks = 0; ks < KS; ++ks) read_k(ring + 3 * STAGE, ks);
       s0 = f32x16{};
       s1 = f32x16{};
 #pragma unroll
@@ -493,30 +466,35 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) read_k(ring, ks);
 #pragma unroll
-      for (int x = 0; x < 2 * DT; ++x) read_v(ring + 2 * BLK, x);
+      for (int x = 0; x < 2 * DT; ++x) read_v(ring + BLK, x);
     }
+    wait_loads_barrier<15>();   // (every wave has read K of sub-block 0)
+    issue_k(3);
     // the next unit and its first page ids, long before they are used
     PromptUnit next;
     int32_t next_ids = -1;
     const bool more = a.units > gridDim.x &&
                       find_prompt_unit(a, prompt_round_unit(blockIdx.x, round + 1, gridDim.x), entry, next);
     if (more) next_ids = load_pages(next, 0);
-    int st = 0;
+    int i = 0;
 #pragma unroll 1
-    while (st < ns) {
-      if (!careful) {
+    while (i < nb) {
+      if (!careful && (i & 3) == 0) {
 #pragma unroll 1
-        for (; st < full_st && 2 * st + 8 < k_end / KB; ++st) {
-          if (2 * st + 6 >= window + 64) break;   // (the other path moves the window)
+        for (; i + 4 < n_full && i + 8 < k_end / KB; i += 4) {
+          if (i + 8 >= window + 64) break;   // (the other path moves the window)
           if (!all_pages) break;
-          full_pair(st);
+          full_sub(i, std::integral_constant<int, 0>{});
+          full_sub(i + 1, std::integral_constant<int, 1>{});
+          full_sub(i + 2, std::integral_constant<int, 2>{});
+          full_sub(i + 3, std::integral_constant<int, 3>{});
         }
       }
-      if (st == full_st) {
+      if (i == n_full) {   // hidden keys from here on
         had_nan[0] = is_nan(0);
         had_nan[1] = is_nan(1);
       }
-      any_pair(st++);
+      any_sub(i++);
     }
     const bool beyond = !(lsum[0] < kMost) || !(lsum[1] < kMost);
     if (!careful && __any(beyond) && lane == 0) redo = 1;
