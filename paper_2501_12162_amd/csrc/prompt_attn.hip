@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   };
   auto take_pages = [&](int32_t ids) __attribute__((always_inline)) {
     pages = ids >= 0 && ids < a.num_pages ? ids : -1;
-    all_pages = all_pages && !__any(pages < 0 && window + lane < k_end / KB);
+    all_pages = all_pages && !__any(pages < 0 && window + lane < nb);
     pages_after = load_pages(un, window + 64);
   };
   auto next_window = [&]() __attribute__((always_inline)) {
@@ -178,17 +178,12 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   auto load_q = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
-      const int32_t row = wrow0 + rt * 32 + (lane & 31);
-      const bool ok = row < row_end;
-      const int32_t tok = ok ? row / G : 0, head = un.g * G + (ok ? row - tok * G : 0);
-      vis[rt] = ok ? first + tok : 0;
+      const int32_t row = min(wrow0 + rt * 32 + (lane & 31), row_end - 1);   // (a row past the end repeats the last)
+      const int32_t tok = row / G, head = un.g * G + row - tok * G;
+      vis[rt] = first + tok;
       const __bf16 *qp = (const __bf16 *)a.q + (int64_t)(un.token0 + tok) * a.q_stride + (int64_t)head * D + half * 8;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        bf16x8 v = {};
-        if (ok) v = *(const bf16x8 *)(qp + ks * 16);
-        qf[rt][ks] = v;
-      }
+      for (int ks = 0; ks < KS; ++ks) qf[rt][ks] = *(const bf16x8 *)(qp + ks * 16);
     }
   };
 
@@ -207,6 +202,8 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     return __builtin_amdgcn_readlane(pages, blk - window);
   };
   const uint32_t wave_lds = lds_addr(ring) + wave * WI * 1024;
+  const void *zeros = zero_line;
+  asm volatile("" : "+s"(zeros));   // (its address is looked up once)
   // Sub-block blk of K or V into LDS at `dst`; rows past the tile's keys and
   // pages that do not exist come from the zero line, so that every stage is the
   // same number of loads.
@@ -215,7 +212,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     const char *base = (const char *)pool + (int64_t)max(page, 0) * page_bytes + head_bytes;
 #pragma unroll
     for (int i = 0; i < WI; ++i)
-      dma16<false>(dma_row[i] < left ? (const void *)(base + page_off[i]) : (const void *)zero_line, dst + i * 1024);
+      dma16<false>(dma_row[i] < left ? (const void *)(base + page_off[i]) : zeros, dst + i * 1024);
   };
   // Stage i's loads: K first, then V.
   int32_t page = -1;   // of sub-block i (before stage i's loads)
@@ -386,11 +383,12 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   // after it may fly) and stage i, which every wave has read, is refilled.
   auto full_sub = [&](int i, auto slot_c) __attribute__((always_inline)) {
     constexpr int X = decltype(slot_c)::value, Y = (X + 1) & 3, Z = (X + 3) & 3;
-    const char *src = (const char *)a.v_pages + (int64_t)(uint32_t)page_v * page_bytes + head_bytes;
+    // (past the tile's keys any page will do: nothing reads those stages)
+    const char *src = (const char *)a.v_pages + (int64_t)max(page_v, 0) * page_bytes + head_bytes;
     phase(Zero{}, s0, p0, s1, p1, i, No{}, nullptr, nullptr, Yes{}, src, wave_lds + Z * STAGE + BLK);
     page_v = page;
     page = __builtin_amdgcn_readlane(pages, i + 5 - window);
-    src = (const char *)a.k_pages + (int64_t)(uint32_t)page * page_bytes + head_bytes;
+    src = (const char *)a.k_pages + (int64_t)max(page, 0) * page_bytes + head_bytes;
     wait_loads_barrier<2 * LPS>();
     phase(One{}, s1, p1, s0, p0, i + 1, No{}, ring + Y * STAGE, ring + Y * STAGE + BLK, Yes{}, src, wave_lds + X * STAGE);
   };
@@ -441,7 +439,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
       lsum[rt] = 0.f;
-      m_ref[rt] = vis[rt] > 0 ? -1e30f : 0.f;   // (rows that are none have scores 0)
+      m_ref[rt] = -1e30f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[rt][dt] = f32x16{};
     }
@@ -481,7 +479,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     while (i < nb) {
       if (!careful && (i & 3) == 0) {
 #pragma unroll 1
-        for (; i + 4 < n_full && i + 8 < k_end / KB; i += 4) {
+        for (; i + 4 < n_full && (k_end % KB == 0 || i + 8 < k_end / KB); i += 4) {
           if (i + 8 >= window + 64) break;   // (the other path moves the window)
           if (!all_pages) break;
           full_sub(i, std::integral_constant<int, 0>{});
