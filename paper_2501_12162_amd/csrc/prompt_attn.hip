@@ -25,9 +25,10 @@ __device__ __forceinline__ float fmax3(float x, float y, float z) {
 }
 
 // A unit: one tile of kTileRows rows of one kv-head's (token, query head in
-// group) pairs of a request, row = token * G + head.
+// group) pairs of a request, row = token * G + head; where the keys are split,
+// over those from k0 on.
 struct PromptUnit {
-  int32_t r, token0, n, ctx, tile, g;
+  int32_t r, token0, n, ctx, tile, g, k0;
 };
 
 // Unit u.  With a table (requests in descending order of tiles) units run from
@@ -35,12 +36,23 @@ struct PromptUnit {
 // the tile's number, all requests that have the level, the kv-heads of a tile
 // next to each other, so that with 8 kv-heads each XCD's L2 holds the keys of
 // one.  Entry e ends the units of the levels that e + 1 requests have; `e` is
-// where the search starts and stays.  Without one: request by request, the last
-// tile first.
+// where the search starts and stays.  With split keys the table holds the
+// requests one after another, and a tile's heads come once per chunk.  Without a
+// table: request by request, the last tile first.
 __device__ __forceinline__ bool find_prompt_unit(const PagedAttnArgs &a, int64_t u, int32_t &e, PromptUnit &un) {
   if (u >= a.units) return false;
-  int32_t r = -1, token0 = 0, n = 0, ctx = 0, tile = 0, g = 0;
-  if (a.table_count > 0) {
+  int32_t r = -1, token0 = 0, n = 0, ctx = 0, tile = 0, g = 0, k0 = 0;
+  if (a.chunks > 1) {
+    const int32_t row = (int32_t)u / a.num_kv_heads, level = row / a.chunks;
+    g = (int32_t)u - row * a.num_kv_heads;
+    k0 = (row - level * a.chunks) * a.chunk_keys;
+    while (e < a.table_count - 1 && a.table[e].unit_end <= level * a.num_kv_heads) ++e;
+    tile = a.table[e].unit_end / a.num_kv_heads - 1 - level;
+    r = a.table[e].request;
+    token0 = a.table[e].token0;
+    n = a.table[e].n;
+    ctx = a.table[e].ctx;
+  } else if (a.table_count > 0) {
     while (e < a.table_count - 1 && a.table[e].unit_end <= u) ++e;
     const int32_t before = e > 0 ? a.table[e - 1].unit_end : 0;
     const int32_t per_level = (e + 1) * a.num_kv_heads;
@@ -84,6 +96,7 @@ __device__ __forceinline__ bool find_prompt_unit(const PagedAttnArgs &a, int64_t
   un.ctx = __builtin_amdgcn_readfirstlane(ctx);
   un.tile = __builtin_amdgcn_readfirstlane(tile);
   un.g = __builtin_amdgcn_readfirstlane(g);
+  un.k0 = __builtin_amdgcn_readfirstlane(k0);
   return un.tile >= 0 && un.token0 >= 0 && un.n > 0 && un.token0 + un.n <= a.total_tokens;
 }
 
@@ -140,10 +153,10 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     const int32_t row0 = un.tile * kTileRows;
     row_end = min(un.n * G, row0 + kTileRows);
     wrow0 = row0 + wave * 64;
-    first = un.ctx - un.n + 1;                    // keys that token 0 sees
+    first = un.ctx - un.n + 1 - un.k0;            // keys (of the unit's) that token 0 sees
     // keys that the tile's (the wave's) last row sees; sub-blocks whose keys the wave's rows all see
-    k_end = max(0, first + (row_end - 1) / G);
-    const int32_t wave_end = wrow0 < row_end ? max(0, first + (min(row_end, wrow0 + 64) - 1) / G) : 0;
+    k_end = min(max(0, first + (row_end - 1) / G), a.chunk_keys);
+    const int32_t wave_end = wrow0 < row_end ? min(max(0, first + (min(row_end, wrow0 + 64) - 1) / G), a.chunk_keys) : 0;
     nb = (k_end + KB - 1) / KB;
     wave_nb = (wave_end + KB - 1) / KB;
     n_full = min(wave_nb, max(0, first + wrow0 / G) / KB);
@@ -158,7 +171,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
   int32_t pages, pages_after, window;
   bool all_pages;   // no whole sub-block of the windows so far lacks its page
   auto load_pages = [&](const PromptUnit &of, int base) __attribute__((always_inline)) -> int32_t {
-    const int32_t e = (base + lane) * (KB / kPageSize) + wave_page;
+    const int32_t e = of.k0 / kPageSize + (base + lane) * (KB / kPageSize) + wave_page;
     return e < a.bt_stride && e < (of.ctx + kPageSize - 1) / kPageSize ? a.block_table[(int64_t)of.r * a.bt_stride + e] : -1;
   };
   auto take_pages = [&](int32_t ids) __attribute__((always_inline)) {
@@ -180,7 +193,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     for (int rt = 0; rt < 2; ++rt) {
       const int32_t row = min(wrow0 + rt * 32 + (lane & 31), row_end - 1);   // (a row past the end repeats the last)
       const int32_t tok = row / G, head = un.g * G + row - tok * G;
-      vis[rt] = first + tok;
+      vis[rt] = min(first + tok, a.chunk_keys);
       const __bf16 *qp = (const __bf16 *)a.q + (int64_t)(un.token0 + tok) * a.q_stride + (int64_t)head * D + half * 8;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) qf[rt][ks] = *(const bf16x8 *)(qp + ks * 16);
@@ -527,6 +540,21 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
       // A key that the row does not see has weight 0, and 0 times an infinite
       // value is NaN: such rows are taken again, key by key.
       const bool again = ok && is_nan(rt) && !had_nan[rt];
+      if (a.chunks > 1) {
+        // the chunk's part: sums, and (reference in log2 units, sum of weights);
+        // an infinite reference has the join take the row again
+        const int64_t slot = (int64_t)blockIdx.x * kTileRows + (row - done.tile * kTileRows);
+        if (ok) {
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+              *(f32x4 *)(a.ws_o + slot * D + dt * 32 + i * 2 + half * 4) =
+                  f32x4{o[rt][dt][i], o[rt][dt][i + 1], o[rt][dt][i + 2], o[rt][dt][i + 3]};
+          if (half == 0) *(f32x2 *)(a.ws_ml + slot * 2) = f32x2{again ? INFINITY : m_ref[rt] * c, l_tot};
+        }
+        continue;
+      }
       __bf16 *dst = (__bf16 *)a.out + ((int64_t)(done.token0 + tok) * a.num_q_heads + head) * D;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
@@ -549,6 +577,56 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
     }
     if (!more) return;
   }
+}
+
+// Joins the chunks of split keys: with m the largest reference of the row's
+// chunks, out = sum 2^(m_c - m) o_c / sum 2^(m_c - m) l_c.  One wave per row.
+template <int D>
+__global__ __launch_bounds__(kThreads) void prompt_join_kernel(PagedAttnArgs a) {
+  constexpr int EPL = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t id = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int32_t t = __builtin_amdgcn_readfirstlane((int32_t)(id / a.num_q_heads));
+  const int32_t h = __builtin_amdgcn_readfirstlane((int32_t)(id - (int64_t)t * a.num_q_heads));
+  if (t >= a.total_tokens) return;
+  int e = -1;
+  for (int i0 = 0; i0 < a.table_count; i0 += 64) {
+    const int i = i0 + lane;
+    const unsigned long long hit =
+        __ballot(i < a.table_count && t >= a.table[i].token0 && t < a.table[i].token0 + a.table[i].n);
+    if (hit) {
+      e = i0 + __ffsll(hit) - 1;
+      break;
+    }
+  }
+  if (e < 0) return;
+  const int32_t g = h / a.group, row = (t - a.table[e].token0) * a.group + (h - g * a.group);
+  const int32_t tile = row / kTileRows;
+  const int32_t level = a.table[e].unit_end / a.num_kv_heads - 1 - tile;
+  const int32_t seen = max(0, a.table[e].ctx - a.table[e].n + 1 + (t - a.table[e].token0));
+  const int32_t chunks = min(a.chunks, (seen + a.chunk_keys - 1) / a.chunk_keys);
+  float m = -1e30f, l = 0.f, o[EPL] = {};
+  for (int c = 0; c < chunks; ++c) {
+    const int64_t slot = (((int64_t)level * a.chunks + c) * a.num_kv_heads + g) * kTileRows + (row - tile * kTileRows);
+    const f32x2 ml = *(const f32x2 *)(a.ws_ml + slot * 2);
+    float x[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) x[i] = a.ws_o[slot * D + lane * EPL + i];
+    const float mn = fmaxf(m, ml[0]);
+    const float f = __builtin_amdgcn_exp2f(m - mn), w = __builtin_amdgcn_exp2f(ml[0] - mn);
+    m = mn;
+    l = l * f + w * ml[1];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) o[i] = o[i] * f + w * x[i];
+  }
+  if (m == INFINITY) {
+    attend_row<true, D>(a, a.table[e].request, t, h, seen);
+    return;
+  }
+  const float inv = l > 0.f ? 1.f / l : l == l ? 0.f : l;
+  __bf16 *dst = (__bf16 *)a.out + id * D + lane * EPL;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) dst[i] = (__bf16)(o[i] * inv);
 }
 
 template <int D>
@@ -574,6 +652,13 @@ hipError_t launch_prompt_attn(const PagedAttnArgs &a, int head_dim, bool bf16, h
     const dim3 grid((unsigned)a.grid);
     if (head_dim == 128) hipLaunchKernelGGL((prompt_attn_bf16_kernel<128>), grid, block, 0, stream, a);
     else hipLaunchKernelGGL((prompt_attn_bf16_kernel<64>), grid, block, 0, stream, a);
+    if (a.chunks > 1) {
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      const dim3 rows((unsigned)(((int64_t)a.total_tokens * a.num_q_heads + kWaves - 1) / kWaves));
+      if (head_dim == 128) hipLaunchKernelGGL((prompt_join_kernel<128>), rows, block, 0, stream, a);
+      else hipLaunchKernelGGL((prompt_join_kernel<64>), rows, block, 0, stream, a);
+    }
     return hipGetLastError();
   }
   const int64_t waves = (int64_t)a.total_tokens * a.num_q_heads;

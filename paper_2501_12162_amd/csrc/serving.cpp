@@ -90,36 +90,90 @@ int32_t validate_prompt(int32_t num_requests, const int32_t *indptr, const int32
 // requests than it holds are found by a scan on the device, in their own order.
 // Several units per workgroup, each workgroup taking every kPromptGrid-th,
 // hide the loads that open a unit behind the end of the one before (16 ragged
-// prompts of 636-2012 tokens 420 -> XXX us); that needs units in descending
+// prompts of 636-2012 tokens 420 -> 411 us); that needs units in descending
 // order of keys, which the table gives where all rows have as many cached keys
 // before them.
-void plan_prompt(PagedAttnArgs &a, const int32_t *indptr, const int32_t *ctx) {
+struct PromptPlan {
   int64_t units = 0;
-  const bool fits = a.num_requests <= kPromptTable;
-  int32_t count = 0, least = INT32_MAX, most = 0;
-  for (int32_t r = 0; r < a.num_requests; ++r) {
+  int32_t chunks = 1, chunk_keys = INT32_MAX;
+  bool in_order = false;     // every row has about as many cached keys before its request's rows
+  size_t ml_bytes = 0, ws_bytes = 0;
+};
+
+// Few tiles over many keys (a small chunk of a long prompt) leave compute units
+// idle, so their keys are split and joined by a second launch.  Priced by a
+// tile's time over k keys, kTileUs + k * kKeyUs, in rounds of kPromptGrid tiles,
+// and by the join's traffic: tiles write and the join reads D + 2 floats per row.
+PromptPlan prompt_plan(int32_t num_requests, const int32_t *indptr, const int32_t *ctx, int32_t hq, int32_t hkv,
+                       int32_t head_dim, bool bf16) {
+  constexpr double kTileUs = 9.0, kJoinUs = 6.0, kJoinBytesPerUs = 4e6;
+  constexpr int32_t kLeastKeys = 256, kMostChunks = 64;
+  const double key_us = 0.022 * head_dim / 128;
+  PromptPlan p;
+  int32_t least = INT32_MAX, most = 0, keys = 0;
+  for (int32_t r = 0; r < num_requests; ++r) {
     const int32_t n = indptr[r + 1] - indptr[r];
     if (n == 0) continue;
-    units += (int64_t)prompt_tiles(n, a.group, kPromptTileRows) * a.num_kv_heads;
+    p.units += (int64_t)prompt_tiles(n, hq / hkv, kPromptTileRows) * hkv;
     least = std::min(least, ctx[r] - n);
     most = std::max(most, ctx[r] - n);
-    if (!fits) continue;
-    int32_t i = count++;
-    for (; i > 0 && (a.table[i - 1].n < n || (a.table[i - 1].n == n && a.table[i - 1].ctx < ctx[r])); --i)
-      a.table[i] = a.table[i - 1];
-    a.table[i] = {0, r, indptr[r], n, ctx[r]};
+    keys = std::max(keys, ctx[r]);
   }
+  p.in_order = most - least <= 128;
+  if (!bf16 || num_requests > kPromptTable || p.units == 0 || p.units >= 2 * kPromptGrid) return p;
+  const double row_bytes = 2.0 * (head_dim * 4 + 8) * indptr[num_requests] * hq;
+  double best = 0.95 * std::ceil((double)p.units / kPromptGrid) * (kTileUs + keys * key_us);
+  const int64_t units = p.units;
+  for (int32_t c = 2; c <= kMostChunks; ++c) {
+    const int32_t chunk = (ceil_div(keys, c) + 127) / 128 * 128;
+    if (chunk < kLeastKeys) break;
+    const int32_t chunks = ceil_div(keys, chunk);
+    const double us = std::ceil((double)(units * chunks) / kPromptGrid) * (kTileUs + chunk * key_us) + kJoinUs +
+                      row_bytes * chunks / kJoinBytesPerUs;
+    if (us < best) {
+      best = us;
+      p.chunks = chunks;
+      p.chunk_keys = chunk;
+    }
+  }
+  if (p.chunks > 1) {
+    p.units = units * p.chunks;
+    p.ml_bytes = round_up((size_t)p.units * kPromptTileRows * 8, 256);
+    p.ws_bytes = p.ml_bytes + (size_t)p.units * kPromptTileRows * head_dim * 4;
+  }
+  return p;
+}
+
+void fill_prompt(PagedAttnArgs &a, const PromptPlan &p, const int32_t *indptr, const int32_t *ctx, void *workspace) {
+  const bool split = p.chunks > 1;
+  int32_t count = 0;
+  if (a.num_requests <= kPromptTable)
+    for (int32_t r = 0; r < a.num_requests; ++r) {
+      const int32_t n = indptr[r + 1] - indptr[r];
+      if (n == 0) continue;
+      int32_t i = count++;
+      if (!split)
+        for (; i > 0 && (a.table[i - 1].n < n || (a.table[i - 1].n == n && a.table[i - 1].ctx < ctx[r])); --i)
+          a.table[i] = a.table[i - 1];
+      a.table[i] = {0, r, indptr[r], n, ctx[r]};
+    }
   int64_t end = 0;
   for (int32_t i = 0; i < count; ++i) {
     const int32_t tiles = prompt_tiles(a.table[i].n, a.group, kPromptTileRows);
     const int32_t below = i + 1 < count ? prompt_tiles(a.table[i + 1].n, a.group, kPromptTileRows) : 0;
-    end += (int64_t)(tiles - below) * (i + 1) * a.num_kv_heads;
+    end += (split ? (int64_t)tiles : (int64_t)(tiles - below) * (i + 1)) * a.num_kv_heads;
     a.table[i].unit_end = (int32_t)end;
   }
-  a.units = units;
   a.table_count = count;
-  a.grid = (int32_t)units;
-  if (count > 0 && units > kPromptGrid && most - least <= 128) a.grid = kPromptGrid;
+  a.units = p.units;
+  a.chunks = p.chunks;
+  a.chunk_keys = p.chunk_keys;
+  a.grid = (int32_t)p.units;
+  if (!split && count > 0 && p.units > kPromptGrid && p.in_order) a.grid = kPromptGrid;
+  if (split) {
+    a.ws_ml = (float *)workspace;
+    a.ws_o = (float *)((char *)workspace + p.ml_bytes);
+  }
 }
 
 int32_t validate_pages(bool any_key, const void *k_pages, const void *v_pages, int32_t num_pages, const int32_t *table) {
@@ -277,7 +331,9 @@ size_t adaserve_prompt_attn_workspace_bytes(int32_t num_requests, const int32_t 
   if (validate_paged(num_requests, 0, 0, num_q_heads, num_kv_heads, head_dim, page_size, 1.f, dtype) != ADASERVE_OK ||
       validate_prompt(num_requests, token_indptr_host, context_len_host, -1, num_q_heads, total, most) != ADASERVE_OK)
     return SIZE_MAX;
-  return 0;
+  return prompt_plan(num_requests, token_indptr_host, context_len_host, num_q_heads, num_kv_heads, head_dim,
+                     dtype == ADASERVE_BF16)
+      .ws_bytes;
 }
 
 int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, const int32_t *token_indptr_host,
@@ -286,8 +342,6 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
                              const int32_t *context_len, const int32_t *context_len_host, int32_t num_q_heads,
                              int32_t num_kv_heads, int32_t head_dim, int32_t page_size, float sm_scale, int32_t dtype,
                              void *out, void *workspace, size_t workspace_bytes, void *stream) {
-  (void)workspace;
-  (void)workspace_bytes;
   int32_t st = validate_paged(num_requests, num_pages, block_table_stride, num_q_heads, num_kv_heads, head_dim,
                               page_size, sm_scale, dtype);
   if (st != ADASERVE_OK) return st;
@@ -301,6 +355,10 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
   if (st != ADASERVE_OK) return st;
   if (!aligned(out, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "out must be 16-byte aligned");
   st = validate_pages(most > 0, k_pages, v_pages, num_pages, block_table);
+  if (st != ADASERVE_OK) return st;
+  const PromptPlan plan = prompt_plan(num_requests, token_indptr_host, context_len_host, num_q_heads, num_kv_heads,
+                                      head_dim, dtype == ADASERVE_BF16);
+  st = validate_workspace(workspace, workspace_bytes, plan.ws_bytes);
   if (st != ADASERVE_OK) return st;
   st = check_device();
   if (st != ADASERVE_OK) return st;
@@ -322,7 +380,7 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
   a.group = num_q_heads / num_kv_heads;
   a.sm_scale = sm_scale;
   a.scale_log2 = sm_scale * 1.4426950408889634f;
-  plan_prompt(a, token_indptr_host, context_len_host);
+  fill_prompt(a, plan, token_indptr_host, context_len_host, workspace);
   return launch_status(launch_prompt_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
                        "prompt attention launch");
 }

@@ -73,10 +73,13 @@ struct PagedAttnArgs {
   float sm_scale;
   float scale_log2;              // sm_scale * log2(e)
   // prompt attention
-  int64_t units;                 // tiles of all heads
+  int64_t units;                 // tiles of all heads, times chunks
+  int32_t chunks;                // most chunks of keys per tile: 1 unless there are few tiles
+  int32_t chunk_keys;            // keys per chunk (INT32_MAX: all)
   int32_t grid;                  // workgroups: one per unit, or kPromptGrid
   int32_t table_count;           // entries used in table[] (0: the device arrays are scanned)
-  // decode attention (DecodePlan)
+  // decode attention (DecodePlan); prompt attention with split keys: sums and
+  // references of [units, kPromptTileRows] rows in ws_o and ws_ml
   int32_t max_context;
   int32_t rows_per_group;
   int32_t row_groups;
