@@ -623,25 +623,249 @@ __global__ __launch_bounds__(kThreads) void prompt_join_kernel(PagedAttnArgs a) 
     attend_row<true, D>(a, a.table[e].request, t, h, seen);
     return;
   }
-  const float inv = l > 0.f ? 1.f / l : l == l ? 0.f : l;
+  const float inv = l == 0.f ? 0.f : 1.f / l;   // (a NaN stays one)
   __bf16 *dst = (__bf16 *)a.out + id * D + lane * EPL;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) dst[i] = (__bf16)(o[i] * inv);
 }
 
-template <int D>
+// fp32: one workgroup per tile of 16 RB rows, its four waves taking a quarter of
+// the tile's keys each and joining in LDS.  S^T = K Q^T and O^T = V^T P^T run on
+// v_mfma_f32_16x16x4_f32; both contractions may take their slots in any order,
+// so every lane loads 16 contiguous bytes of K and V straight into the operand
+// registers and P needs no exchange: slot q of QK step (c, e) is head-dim
+// element 16 c + 4 q + e, slot q of PV step e is key 4 q + e, and O^T tile (h, k)
+// holds the columns 64 h + 4 j + k.  Bound by the fp32 matrix rate (a sixteenth of
+// bf16's), so two row tiles share each operand only where there are enough tiles
+// to fill the device.
+template <int D, int RB>
 __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PagedAttnArgs a) {
-  const int wave = threadIdx.x >> 6;
-  const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + wave;
-  const int64_t t = id / a.num_q_heads;
-  const int h = (int)(id - t * a.num_q_heads);
-  if (t >= a.total_tokens) return;
-  int r = 0;
-  while (r < a.num_requests && a.token_indptr[r + 1] <= t) ++r;
-  if (r >= a.num_requests || a.token_indptr[r] > t) return;
-  const int32_t n = a.token_indptr[r + 1] - a.token_indptr[r];
-  const int64_t pos = (int64_t)a.context_len[r] - n + (t - a.token_indptr[r]);
-  attend_row<false, D>(a, r, t, h, pos + 1);
+  constexpr int RT = 16 * RB;
+  constexpr int NC = D / 16;      // 16-byte K loads per lane and page
+  constexpr int NH = D / 64;      // 16-byte V loads per lane and key
+  constexpr int LDO = D + 4;
+  __shared__ __align__(16) float mo[kWaves * RT * LDO];
+  __shared__ float mw[kWaves][RT], lw[kWaves][RT];
+  __shared__ int taken[RT];
+  const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, j = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.group;
+
+  // the unit: request by request, the last tile first
+  int r = -1;
+  int32_t local = 0;
+  int64_t base = 0;
+  for (int r0 = 0; r0 < a.num_requests; r0 += 64) {
+    const int i = r0 + lane;
+    int64_t units = 0;
+    if (i < a.num_requests)
+      units = (int64_t)prompt_tiles(max(a.token_indptr[i + 1] - a.token_indptr[i], 0), G, RT) * a.num_kv_heads;
+    const int64_t upto = wave_inclusive_scan(units);
+    const unsigned long long hit = __ballot(base + upto > (int64_t)blockIdx.x);
+    if (hit) {
+      const int f = __ffsll(hit) - 1;
+      r = r0 + f;
+      local = (int32_t)(blockIdx.x - base - __shfl(upto - units, f, 64));
+      break;
+    }
+    base += __shfl(upto, 63, 64);
+  }
+  r = __builtin_amdgcn_readfirstlane(r);
+  if (r < 0) return;
+  local = __builtin_amdgcn_readfirstlane(local);
+  const int32_t token0 = a.token_indptr[r], n = a.token_indptr[r + 1] - token0, ctx = a.context_len[r];
+  const int32_t tile = prompt_tiles(n, G, RT) - 1 - local / a.num_kv_heads, g = local % a.num_kv_heads;
+  if (tile < 0 || token0 < 0 || token0 + n > a.total_tokens) return;
+  const int32_t row0 = tile * RT, row_end = min(n * G, row0 + RT);
+  const int32_t first = ctx - n + 1;
+  const int32_t k_end = max(0, first + (row_end - 1) / G);
+  const int32_t n_full = max(0, first + row0 / G) / 16;   // pages that all rows see
+  const int32_t nb = (k_end + 15) / 16;
+  const int32_t b0 = (int32_t)((int64_t)nb * wave / kWaves), b1 = (int32_t)((int64_t)nb * (wave + 1) / kWaves);
+
+  f32x4 qf[RB][NC];
+  int32_t vis[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int32_t row = min(row0 + rb * 16 + j, row_end - 1), tok = row / G, head = g * G + row - tok * G;
+    vis[rb] = first + tok;
+    const float *qp = (const float *)a.q + (int64_t)(token0 + tok) * a.q_stride + (int64_t)head * D + q * 4;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) qf[rb][c] = *(const f32x4 *)(qp + c * 16);
+  }
+  // lane i holds the id of page page_base + i (-1: none)
+  int32_t page_base = b0, pages = -1;
+  auto load_pages = [&]() {
+    const int b = page_base + lane;
+    pages = -1;
+    if (b < nb && b < a.bt_stride) {
+      const int32_t p = a.block_table[(int64_t)r * a.bt_stride + b];
+      if (p >= 0 && p < a.num_pages) pages = p;
+    }
+  };
+  load_pages();
+  auto page_of = [&](int b) -> int32_t {
+    if (b >= page_base + 64) {
+      page_base = b;
+      load_pages();
+    }
+    return __builtin_amdgcn_readlane(pages, b - page_base);
+  };
+  // a missing page reads page 0, whose scores and values are not used
+  f32x4 kr[NC], vr[4][NH];
+  auto load_k = [&](int32_t page) {
+    const float *p = (const float *)a.k_pages + (((int64_t)max(page, 0) * a.num_kv_heads + g) * kPageSize + j) * D + q * 4;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) kr[c] = *(const f32x4 *)(p + c * 16);
+  };
+  auto load_v = [&](int32_t page) {
+    const float *p = (const float *)a.v_pages + (((int64_t)max(page, 0) * a.num_kv_heads + g) * kPageSize + q * 4) * D + j * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int h = 0; h < NH; ++h) vr[e][h] = *(const f32x4 *)(p + e * D + h * 64);
+  };
+  f32x4 o[RB][NH][4];
+  float m[RB], l[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    m[rb] = -1e30f;
+    l[rb] = 0.f;
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[rb][h][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  auto is_nan = [&](int rb) {
+    float x = l[rb];
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x = __builtin_elementwise_maximum(x, o[rb][h][k][i]);
+    x = max_over_lane_rows(x);
+    return x != x;
+  };
+  bool had_nan[RB] = {};
+  int32_t page = -1;
+  if (b0 < b1) {
+    page = page_of(b0);
+    load_k(page);
+    load_v(page);
+  }
+  for (int b = b0; b < b1; ++b) {
+    if (b == n_full || (b == b0 && b > n_full))
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) had_nan[rb] = is_nan(rb);
+    const int32_t next = page_of(min(b + 1, b1 - 1));
+    f32x4 s[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) s[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+          s[rb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[c][e], qf[rb][c][e], s[rb], 0, 0, 0);
+    load_k(next);
+    // s[rb][e]: key 4 q + e of the page, row j; in log2 units from here on
+    const bool masked = b >= n_full, none = page < 0;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = none ? 0.f : s[rb][e] * a.scale_log2;
+        s[rb][e] = !masked || b * 16 + q * 4 + e < vis[rb] ? x : -INFINITY;
+      }
+      const float bm = max_over_lane_rows(fmax3(s[rb][0], s[rb][1], __builtin_elementwise_maximum(s[rb][2], s[rb][3])));
+      if (__any(bm > m[rb])) {
+        const float mn = bm > m[rb] ? bm : m[rb], al = __builtin_amdgcn_exp2f(m[rb] - mn);
+        m[rb] = mn;
+        l[rb] *= al;
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[rb][h][k] *= al;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[rb][e] = __builtin_amdgcn_exp2f(s[rb][e] - m[rb]);
+        l[rb] += s[rb][e];
+      }
+    }
+    // a slot past the tile's keys may hold anything
+    if (none || b * 16 + 16 > k_end) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+          if (none || b * 16 + q * 4 + e >= k_end) vr[e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+            o[rb][h][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[e][h][k], s[rb][e], o[rb][h][k], 0, 0, 0);
+    load_v(next);
+    page = next;
+  }
+  if (tid < RT) taken[tid] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int rl = rb * 16 + j;
+    const float ls = sum_over_lane_rows(l[rb]);
+    // a key that the row does not see has weight 0, and 0 times an infinite value
+    // is NaN: such rows are taken again, key by key
+    if (b1 > n_full && is_nan(rb) && !had_nan[rb]) taken[rl] = 1;
+    if (q == 0) {
+      mw[wave][rl] = m[rb];
+      lw[wave][rl] = ls;
+    }
+    float *dst = mo + (wave * RT + rl) * LDO;
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(f32x4 *)(dst + h * 64 + q * 16 + i * 4) = f32x4{o[rb][h][0][i], o[rb][h][1][i], o[rb][h][2][i], o[rb][h][3][i]};
+  }
+  __syncthreads();
+  for (int it = tid; it < RT * (D / 4); it += kThreads) {
+    const int rl = it / (D / 4), col = it % (D / 4) * 4;
+    const int row = row0 + rl;
+    if (row >= row_end || taken[rl]) continue;
+    float mm = mw[0][rl];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, mw[w][rl]);
+    float den = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float wt = __builtin_amdgcn_exp2f(mw[w][rl] - mm);
+      den = __builtin_fmaf(wt, lw[w][rl], den);
+      acc += *(const f32x4 *)(mo + (w * RT + rl) * LDO + col) * wt;
+    }
+    const int tok = row / G, head = g * G + row - tok * G;
+    f32x4 res = {0.f, 0.f, 0.f, 0.f};
+    if (den != 0.f) res = acc / den;   // (a NaN stays one)
+    *(f32x4 *)((float *)a.out + ((int64_t)(token0 + tok) * a.num_q_heads + head) * D + col) = res;
+  }
+  for (int rl = wave; rl < RT && row0 + rl < row_end; rl += kWaves)
+    if (taken[rl]) {
+      const int tok = (row0 + rl) / G, head = g * G + row0 + rl - tok * G;
+      attend_row<false, D>(a, r, token0 + tok, head, first + tok);
+    }
+}
+
+template <int D, int RB>
+void launch_prompt_f32(const PagedAttnArgs &a, int64_t units, hipStream_t stream) {
+  hipLaunchKernelGGL((prompt_attn_f32_kernel<D, RB>), dim3((unsigned)units), dim3(kThreads), 0, stream, a);
 }
 
 }  // namespace
@@ -661,10 +885,13 @@ hipError_t launch_prompt_attn(const PagedAttnArgs &a, int head_dim, bool bf16, h
     }
     return hipGetLastError();
   }
-  const int64_t waves = (int64_t)a.total_tokens * a.num_q_heads;
-  const dim3 grid((unsigned)((waves + 3) / 4));
-  if (head_dim == 128) hipLaunchKernelGGL((prompt_attn_f32_kernel<128>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((prompt_attn_f32_kernel<64>), grid, block, 0, stream, a);
+  if (head_dim == 128) {
+    if (a.f32_rows == 32) launch_prompt_f32<128, 2>(a, a.units, stream);
+    else launch_prompt_f32<128, 1>(a, a.units, stream);
+  } else {
+    if (a.f32_rows == 32) launch_prompt_f32<64, 2>(a, a.units, stream);
+    else launch_prompt_f32<64, 1>(a, a.units, stream);
+  }
   return hipGetLastError();
 }
 

@@ -380,7 +380,19 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
   a.group = num_q_heads / num_kv_heads;
   a.sm_scale = sm_scale;
   a.scale_log2 = sm_scale * 1.4426950408889634f;
-  fill_prompt(a, plan, token_indptr_host, context_len_host, workspace);
+  if (dtype == ADASERVE_BF16) {
+    fill_prompt(a, plan, token_indptr_host, context_len_host, workspace);
+  } else {
+    // 32-row tiles read each key half as often; 16-row tiles put more units to work
+    for (a.f32_rows = 32;; a.f32_rows = 16) {
+      a.units = 0;
+      for (int32_t r = 0; r < num_requests; ++r)
+        a.units += (int64_t)prompt_tiles(token_indptr_host[r + 1] - token_indptr_host[r], a.group, a.f32_rows) * num_kv_heads;
+      if (a.units >= 1024 || a.f32_rows == 16) break;
+    }
+    a.chunk_keys = INT32_MAX;
+    a.chunks = 1;
+  }
   return launch_status(launch_prompt_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
                        "prompt attention launch");
 }

@@ -77,6 +77,7 @@ struct PagedAttnArgs {
   int32_t chunks;                // most chunks of keys per tile: 1 unless there are few tiles
   int32_t chunk_keys;            // keys per chunk (INT32_MAX: all)
   int32_t grid;                  // workgroups: one per unit, or kPromptGrid
+  int32_t f32_rows;              // rows per F32 tile: 16 or 32
   int32_t table_count;           // entries used in table[] (0: the device arrays are scanned)
   // decode attention (DecodePlan); prompt attention with split keys: sums and
   // references of [units, kPromptTileRows] rows in ws_o and ws_ml
