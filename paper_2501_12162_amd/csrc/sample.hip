@@ -11,6 +11,22 @@
 // exact and independent of its order (2^20 tokens of 2^32 are below 2^53, so
 // also as doubles); the units are fine enough (2.3e-10 of the likeliest
 // token's mass) that their rounding is far below that of fp32 sums.
+//
+// No sort: a row is cut into parts of 4096 to 32768 logits, so that a single row
+// runs on many compute units, and four launches go over them:
+//   1. maxima of the parts;
+//   2. per part a histogram of (count, mass) over 512 bins of -z log2 e: the one
+//      pass that takes an exponential per logit;
+//   3. from the row's histogram, the bins in which a filter may cut; every part
+//      lists its tokens of those bins, in index order (a bin is a sixteenth of a
+//      power of two wide: a few hundred tokens out of 10^5);
+//   4. one workgroup per row: the exact cuts among the listed tokens, the kept
+//      mass of each part (whole bins from its histogram, the rest from the
+//      list), and the draw within the one part that holds it.
+// The first three read the row (from HBM once, then out of the caches); pass 2
+// is bound by fp64 arithmetic and LDS atomics, the rest by memory and latency.
+// A row whose cut bins hold more tokens than the lists take (one of few distinct
+// values, or nearly flat) is searched as a whole in pass 4.
 #include <limits.h>
 
 #include "device_common.h"
@@ -20,203 +36,667 @@ namespace adaserve {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 256;          // of passes 1 to 3
+constexpr int kDrawThreads = 1024;
+constexpr int kBins = kSampleBins;
 constexpr double kUnit = 4294967296.0;
+// Bins 0 .. 510 cover -z log2 e in [0, 33.01), where masses can be 1 or more;
+// the last bin's tokens have none.
+constexpr float kBinsPerLog2 = 511.f / 33.01f;
+constexpr uint64_t kMassBits = 48, kMassMask = (1ull << kMassBits) - 1;   // a part's mass: at most 32768 2^32
 
-template <bool BF16>
-__device__ __forceinline__ float logit(const SampleArgs &a, int row, int v) {
-  const int64_t i = (int64_t)row * a.row_stride + v;
-  const float x = BF16 ? bf16_bits_to_float(((const uint16_t *)a.logits)[i]) : ((const float *)a.logits)[i];
-  return x + 0.f;   // -0 ranks with +0
-}
-
-// Unsigned order of the keys = order of the values.
+// Unsigned order of the keys = order of the values; -0 ranks with +0.
 __device__ __forceinline__ uint32_t order_key(float x) {
-  const uint32_t u = __float_as_uint(x);
+  const uint32_t u = __float_as_uint(x + 0.f);
   return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
 }
+constexpr uint32_t kKeyMinusInf = 0x007fffffu;   // order_key(-inf)
 
-__device__ __forceinline__ uint64_t mass_of(float x, float top, double t) {
-  return (uint64_t)__builtin_rint(exp(((double)x - (double)top) / t) * kUnit);
+// What a row asks for, and its logits' place.
+struct Row {
+  const char *base;        // its first logit
+  int off;                 // elements between the 16-byte line of the first logit and it
+  float top;               // largest logit
+  uint32_t top_key;
+  double rate;             // log2 e / T
+  int64_t k;               // 0: off
+  double p;                // >= 1: off
+  double least;            // least mass (0: off)
+  float u;
+  int state;               // 0: draw, 1: the first-ranked token, 2: no distribution
+};
+
+// -z log2 e of logit x (monotone in x, also in its roundings).
+__device__ __forceinline__ double depth_of(const Row &r, float x) {
+  return ((double)r.top - (double)x) * r.rate;
+}
+__device__ __forceinline__ int bin_of(double y) {
+  return y < 33.01 ? min((int)((float)y * kBinsPerLog2), kBins - 1) : kBins - 1;
+}
+// round(2^(32 - y)): 2^f, |f| <= 1/2, by its series to f^11 (error below 2^-44).
+__device__ __forceinline__ uint64_t mass_at(double y) {
+  if (!(y < 33.5)) return 0;
+  const double n = __builtin_rint(y), f = (n - y) * 0.693147180559945309417;
+  double s = 1.0 / 39916800;
+  s = __builtin_fma(s, f, 1.0 / 3628800);
+  s = __builtin_fma(s, f, 1.0 / 362880);
+  s = __builtin_fma(s, f, 1.0 / 40320);
+  s = __builtin_fma(s, f, 1.0 / 5040);
+  s = __builtin_fma(s, f, 1.0 / 720);
+  s = __builtin_fma(s, f, 1.0 / 120);
+  s = __builtin_fma(s, f, 1.0 / 24);
+  s = __builtin_fma(s, f, 1.0 / 6);
+  s = __builtin_fma(s, f, 0.5);
+  s = __builtin_fma(s, f, 1.0);
+  s = __builtin_fma(s, f, 1.0);
+  // adding 2^52 rounds to a whole number and leaves it in the mantissa
+  const double w = __builtin_ldexp(s, 32 - (int)n) + 4503599627370496.0;
+  return (uint64_t)__double_as_longlong(w) & ((1ull << 52) - 1);
+}
+__device__ __forceinline__ uint64_t mass_of(const Row &r, float x) { return mass_at(depth_of(r, x)); }
+
+// Logit vectors: vector v of a row holds elements v * EPV - off .. + EPV - 1, so
+// that whole ones are 16-byte lines; f(index, value) for those in the row.
+template <bool BF16>
+struct Vec {
+  static constexpr int EPV = BF16 ? 8 : 4;
+  float x[EPV];
+  int first;   // index of x[0], may lie before the row
+  __device__ __forceinline__ void load(const Row &r, int vocab, int v) {
+    first = v * EPV - r.off;
+    if (first >= 0 && first + EPV <= vocab) {
+      const u32x4 w = *(const u32x4 *)(r.base + (int64_t)first * (BF16 ? 2 : 4));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (BF16) {
+          x[2 * i] = __uint_as_float(w[i] << 16);
+          x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+          x[i] = __uint_as_float(w[i]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPV; ++i) {
+        const int e = first + i;
+        x[i] = -INFINITY;
+        if (e >= 0 && e < vocab)
+          x[i] = BF16 ? bf16_bits_to_float(((const uint16_t *)r.base)[e]) : ((const float *)r.base)[e];
+      }
+    }
+  }
+  __device__ __forceinline__ bool in(int i, int vocab) const { return (uint32_t)(first + i) < (uint32_t)vocab; }
+};
+
+template <bool BF16>
+__device__ __forceinline__ float logit_at(const Row &r, int i) {
+  return BF16 ? bf16_bits_to_float(((const uint16_t *)r.base)[i]) : ((const float *)r.base)[i];
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
-  __shared__ uint32_t hist_n[256];
-  __shared__ unsigned long long hist_w[256];
-  __shared__ unsigned long long scan[kThreads];
-  __shared__ uint32_t s_key;
-  __shared__ int32_t s_bad, s_token, s_cut;
-  __shared__ unsigned long long s_a, s_b, s_c;
-  const int row = blockIdx.x, tid = threadIdx.x;
-  const float temp = a.temperature ? a.temperature[row] : 1.f;
-  int64_t k = a.top_k ? a.top_k[row] : 0;
-  const float p = a.top_p ? a.top_p[row] : 1.f, least = a.min_p ? a.min_p[row] : 0.f, u = a.u[row];
-  if (tid == 0) {
-    s_key = 0;
-    s_bad = !(temp >= 0.f && temp < INFINITY) || p != p || least != least || u != u;
-    s_token = INT_MAX;
-    s_cut = INT_MAX;
-  }
-  __syncthreads();
+__device__ __forceinline__ Row row_place(const SampleArgs &a, int64_t row) {
+  Row r{};
+  r.base = (const char *)a.logits + row * a.row_stride * (BF16 ? 2 : 4);
+  r.off = (int)((uintptr_t)r.base & 15) / (BF16 ? 2 : 4);
+  return r;
+}
+
+// The row's parameters and maximum (by every wave of the workgroup).
+template <bool BF16>
+__device__ __forceinline__ Row load_row(const SampleArgs &a, int64_t row) {
+  Row r = row_place<BF16>(a, row);
+  const int lane = threadIdx.x & 63;
+  uint32_t key = lane < a.parts ? a.ws_max[row * a.parts + lane] : 0;
+  const float t = a.temperature ? a.temperature[row] : 1.f, p = a.top_p ? a.top_p[row] : 1.f;
+  const float m = a.min_p ? a.min_p[row] : 0.f;
+  const int32_t k = a.top_k ? a.top_k[row] : 0;
+  r.u = a.u[row];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) key = max(key, (uint32_t)__shfl_xor((int)key, o, 64));
+  r.top_key = key;
+  r.top = key_value(key);
+  const bool bad = key >= 0xff800000u || key <= kKeyMinusInf ||   // (a NaN's part has the largest key)
+                   !(t >= 0.f && t < INFINITY) || p != p || m != m || r.u != r.u;
+  r.state = bad ? 2 : t == 0.f || k == 1 || m > 1.f || p <= 0.f ? 1 : 0;
+  r.rate = 1.4426950408889634074 / (t == 0.f ? 1.0 : (double)t);
+  r.k = k >= 1 && k < a.vocab ? k : 0;
+  r.p = p;
+  r.least = m > 0.f ? (double)m * kUnit : 0.0;
+  if (r.least <= 0.5) r.least = 0.0;   // every mass of 1 passes, and a mass of 0 is never drawn
+  return r;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void sample_max_kernel(SampleArgs a) {
+  __shared__ uint32_t part_key[kThreads / 64];
+  const int64_t row = blockIdx.x / a.parts;
+  const int part = (int)(blockIdx.x - row * a.parts);
+  const Row r = row_place<BF16>(a, row);
+  const int v0 = part * a.part_vecs;
   uint32_t best = 0;
-  bool bad = false;
-  for (int v = tid; v < a.vocab; v += kThreads) {
-    const float x = logit<BF16>(a, row, v);
-    bad |= !(x < INFINITY);
-    best = max(best, order_key(x));
+  Vec<BF16> x[2];
+  for (int v = threadIdx.x; v < a.part_vecs; v += 2 * kThreads) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) x[h].load(r, v + h * kThreads < a.part_vecs ? a.vocab : 0, v0 + v + h * kThreads);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < Vec<BF16>::EPV; ++i)
+        best = max(best, x[h].x[i] < INFINITY ? order_key(x[h].x[i]) : 0xffffffffu);
   }
-  atomicMax(&s_key, best);
-  if (bad) s_bad = 1;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) best = max(best, (uint32_t)__shfl_xor((int)best, o, 64));
+  if ((threadIdx.x & 63) == 0) part_key[threadIdx.x >> 6] = best;
   __syncthreads();
-  const uint32_t top_key = s_key;
-  const float top = key_value(top_key);
-  if (s_bad || top == -INFINITY) {
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) best = max(best, part_key[w]);
+    a.ws_max[blockIdx.x] = best;
+  }
+}
+
+// A bin's word: mass | count << 48.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void sample_hist_kernel(SampleArgs a) {
+  __shared__ unsigned long long hist[kBins];
+  const int64_t row = blockIdx.x / a.parts;
+  const int part = (int)(blockIdx.x - row * a.parts);
+  const Row r = load_row<BF16>(a, row);
+  if (r.state) return;
+  for (int b = threadIdx.x; b < kBins; b += kThreads) hist[b] = 0;
+  __syncthreads();
+  const int v0 = part * a.part_vecs;
+  for (int v = threadIdx.x; v < a.part_vecs; v += kThreads) {
+    Vec<BF16> x;
+    x.load(r, a.vocab, v0 + v);
+#pragma unroll
+    for (int i = 0; i < Vec<BF16>::EPV; ++i) {
+      const double y = depth_of(r, x.x[i]);
+      const int b = bin_of(y);
+      if (b < kBins - 1) atomicAdd(&hist[b], (unsigned long long)(mass_at(y) | (1ull << kMassBits)));
+    }
+  }
+  __syncthreads();
+  uint64_t *out = a.ws_hist + (int64_t)blockIdx.x * kBins;
+  for (int b = threadIdx.x; b < kBins; b += kThreads) out[b] = hist[b];
+}
+
+// Exclusive prefix sum over the workgroup's threads, the total in `total`.
+template <int T>
+__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t *lds, uint64_t &total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint64_t s = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t x = __shfl_up((unsigned long long)s, o, 64);
+    if (lane >= o) s += x;
+  }
+  if (lane == 63) lds[wave] = s;
+  __syncthreads();
+  uint64_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < T / 64; ++w) {
+    if (w < wave) before += lds[w];
+    total += lds[w];
+  }
+  __syncthreads();
+  return before + s - v;
+}
+
+// Bins that min-p may cut in: those of tokens whose mass is within 1/2 of the
+// least one, and of the roundings beside them.
+__device__ __forceinline__ void least_bins(const Row &r, int &lo, int &hi) {
+  lo = hi = kBins;
+  if (r.least == 0.0) return;
+  const double a = 32.0 - log2(r.least + 0.500001), b = 32.0 - log2(fmax(r.least - 0.500001, 1e-9));
+  lo = bin_of(fmax(a - 1e-6, 0.0));
+  hi = bin_of(b + 1e-6);
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a) {
+  static_assert(kBins == 2 * kThreads, "two bins per thread");
+  __shared__ uint64_t scan[kThreads / 64];
+  __shared__ uint64_t cum_w[kBins + 1];
+  __shared__ uint32_t cum_n[kBins + 1];
+  __shared__ int cut_k, cut_lo, cut_hi;
+  const int64_t row = blockIdx.x / a.parts;
+  const int part = (int)(blockIdx.x - row * a.parts);
+  const Row r = load_row<BF16>(a, row);
+  if (r.state) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool filtered = r.k || r.p < 1.0 || r.least > 0.0;
+  if (!filtered && part > 0) {
+    if (tid == 0) a.ws_count[blockIdx.x] = 0;
+    return;
+  }
+  // the row's histogram and its running sums
+  uint64_t w[2] = {0, 0}, n[2] = {0, 0};
+  const uint64_t *h = a.ws_hist + row * a.parts * kBins + 2 * tid;
+#pragma unroll 4
+  for (int p = 0; p < a.parts; ++p) {
+    const uint64_t x0 = h[(int64_t)p * kBins], x1 = h[(int64_t)p * kBins + 1];
+    w[0] += x0 & kMassMask, n[0] += x0 >> kMassBits;
+    w[1] += x1 & kMassMask, n[1] += x1 >> kMassBits;
+  }
+  uint64_t all_w, all_n;
+  const uint64_t before_w = block_scan<kThreads>(w[0] + w[1], scan, all_w);
+  const uint64_t before_n = block_scan<kThreads>(n[0] + n[1], scan, all_n);
+  cum_w[2 * tid] = before_w, cum_w[2 * tid + 1] = before_w + w[0];
+  cum_n[2 * tid] = (uint32_t)before_n, cum_n[2 * tid + 1] = (uint32_t)(before_n + n[0]);
+  if (tid == 0) {
+    cum_w[kBins] = all_w, cum_n[kBins] = (uint32_t)all_n;
+    cut_k = kBins, cut_lo = kBins, cut_hi = -1;
+  }
+  __syncthreads();
+  if (part == 0)
+    for (int b = tid; b <= kBins; b += kThreads) {
+      a.ws_cum_w[row * (kBins + 1) + b] = cum_w[b];
+      a.ws_cum_n[row * (kBins + 1) + b] = cum_n[b];
+    }
+  // Top-k cuts in the bin that holds the k-th token (none: all tokens with mass
+  // are kept); the mass that it keeps lies between that of the bins before it and
+  // that with it, and so does where top-p cuts.
+  if (r.k)
+    for (int b = 2 * tid; b < 2 * tid + 2; ++b)
+      if ((int64_t)cum_n[b] < r.k && r.k <= (int64_t)cum_n[b + 1]) cut_k = b;
+  __syncthreads();
+  const int ck = cut_k;
+  if (r.p < 1.0) {
+    const double most = r.p * (double)(ck < kBins ? cum_w[ck + 1] : all_w), fewest = r.p * (double)(ck < kBins ? cum_w[ck] : all_w);
+    for (int b = 2 * tid; b < 2 * tid + 2; ++b) {
+      // the bins whose masses reach from below to at or above a wanted sum of the range
+      const double from = (double)cum_w[b], to = (double)cum_w[b + 1];
+      if (cum_n[b + 1] > cum_n[b] && from < fmax(most, 1.0) && to >= fewest) {
+        atomicMin(&cut_lo, b);
+        atomicMax(&cut_hi, b);
+      }
+    }
+  }
+  __syncthreads();
+  const int plo = cut_lo, phi = cut_hi;
+  int mlo, mhi;
+  least_bins(r, mlo, mhi);
+  // tokens of those bins, in index order
+  const int v0 = part * a.part_vecs;
+  uint16_t *list = a.ws_list + (int64_t)blockIdx.x * a.list_cap;
+  uint32_t have = 0;
+  if (filtered)
+    for (int v = tid; v < (a.part_vecs + kThreads - 1) / kThreads * kThreads; v += kThreads) {
+      Vec<BF16> x;
+      x.load(r, v < a.part_vecs ? a.vocab : 0, v0 + v);
+      uint32_t mine = 0;
+#pragma unroll
+      for (int i = 0; i < Vec<BF16>::EPV; ++i) {
+        const int b = bin_of(depth_of(r, x.x[i]));
+        const bool take = b < kBins - 1 && (b == ck || (b >= plo && b <= phi) || (b >= mlo && b <= mhi)) &&
+                          v < a.part_vecs && x.in(i, a.vocab);
+        mine |= (uint32_t)take << i;
+      }
+      const int count = __popc(mine);
+      int s = count;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(s, o, 64);
+        if (lane >= o) s += y;
+      }
+      if (lane == 63) scan[wave] = (uint64_t)s;
+      __syncthreads();
+      uint32_t at = have + s - count;
+      for (int q = 0; q < kThreads / 64; ++q) {
+        if (q < wave) at += (uint32_t)scan[q];
+        have += (uint32_t)scan[q];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < Vec<BF16>::EPV; ++i)
+        if (mine >> i & 1) {
+          if (at < (uint32_t)a.list_cap) list[at] = (uint16_t)(v * Vec<BF16>::EPV + i);
+          ++at;
+        }
+    }
+  if (tid == 0) a.ws_count[blockIdx.x] = have;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a) {
+  constexpr int T = kDrawThreads, EPV = Vec<BF16>::EPV;
+  __shared__ uint32_t list_key[kSampleList];
+  __shared__ int32_t list_idx[kSampleList];
+  __shared__ unsigned long long digit_w[256];
+  __shared__ uint32_t digit_n[256];
+  __shared__ unsigned long long part_w[kSampleMaxParts];
+  __shared__ uint32_t part_at[kSampleMaxParts + 1];
+  __shared__ uint64_t scan[T / 64];
+  __shared__ uint64_t s_before, s_sum;
+  __shared__ uint32_t s_digit;
+  __shared__ int s_bin, s_token;
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Row r = load_row<BF16>(a, row);
+  if (r.state == 2) {
     if (tid == 0) a.out_token[row] = -1;
     return;
   }
-  if (k <= 0 || k > a.vocab) k = a.vocab;
-  if (temp == 0.f || least > 1.f) k = 1;
-  const double t = temp == 0.f ? 1.0 : (double)temp;
+  if (tid == 0) s_token = INT_MAX, s_bin = kBins;
+  if (r.state == 1) {
+    // the first token of the row's largest logit, in the first part that has it
+    int first = a.parts - 1;
+    const bool has = lane < a.parts && a.ws_max[row * a.parts + lane] == r.top_key;
+    const unsigned long long hit = __ballot(has);
+    if (hit) first = __ffsll(hit) - 1;
+    __syncthreads();
+    int best = INT_MAX;
+    for (int v = tid; v < a.part_vecs; v += T) {
+      Vec<BF16> x;
+      x.load(r, a.vocab, first * a.part_vecs + v);
+#pragma unroll
+      for (int i = EPV - 1; i >= 0; --i)
+        if (x.in(i, a.vocab) && order_key(x.x[i]) == r.top_key) best = min(best, x.first + i);
+    }
+    if (best != INT_MAX) atomicMin(&s_token, best);
+    __syncthreads();
+    if (tid == 0) a.out_token[row] = s_token;
+    return;
+  }
+  const uint64_t *cum_w = a.ws_cum_w + row * (kBins + 1);
+  const uint32_t *cum_n = a.ws_cum_n + row * (kBins + 1);
+  int mlo, mhi;
+  least_bins(r, mlo, mhi);
 
-  // Radix descent over the keys, most significant byte first: by count to the
-  // k-th token, then by mass to the last token of the nucleus.
-  uint32_t cut = 0;          // keys above it are kept, and `ties` of those equal to it
-  int64_t ties = INT_MAX;
-  auto descend = [&](bool by_mass, unsigned long long want) {
-    // the first bins whose running total reaches `want`
+  // the listed tokens, in index order
+  if (tid < 64) {
+    uint32_t c = lane < a.parts ? a.ws_count[row * a.parts + lane] : 0;
+    const bool over = __any(c > (uint32_t)a.list_cap);
+    uint32_t s = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t y = (uint32_t)__shfl_up((int)s, o, 64);
+      if (lane >= o) s += y;
+    }
+    part_at[lane + 1] = s;
+    if (lane == 0) part_at[0] = 0;
+    part_w[lane] = 0;
+    if (lane == 63) s_digit = over || s > (uint32_t)kSampleList;
+  }
+  static_assert(kSampleMaxParts == 64, "one lane per part");
+  __syncthreads();
+  const bool whole = s_digit != 0;          // the lists do not hold them: the row is searched
+  const int listed = whole ? 0 : (int)part_at[kSampleMaxParts];
+  if (!whole)
+    for (int p = wave; p < a.parts; p += T / 64) {
+      const int at = (int)part_at[p], c = (int)part_at[p + 1] - at;
+      for (int j = lane; j < c; j += 64) {
+        const int i = p * a.part_vecs * EPV + a.ws_list[(row * a.parts + p) * a.list_cap + j] - r.off;
+        list_idx[at + j] = i;
+        list_key[at + j] = order_key(logit_at<BF16>(r, i));
+      }
+    }
+  __syncthreads();
+  // f(key, index) for every token that may be of interest (all of the row where
+  // there are no lists)
+  auto each = [&](auto f) {
+    if (!whole)
+      for (int i = tid; i < listed; i += T) f(list_key[i], list_idx[i]);
+    else
+      for (int v = tid; v < a.parts * a.part_vecs; v += T) {
+        Vec<BF16> x;
+        x.load(r, a.vocab, v);
+#pragma unroll
+        for (int i = 0; i < EPV; ++i)
+          if (x.in(i, a.vocab)) f(order_key(x.x[i]), x.first + i);
+      }
+  };
+  auto key_bin = [&](uint32_t key) { return bin_of(depth_of(r, key_value(key))); };
+
+  // Radix descent over the keys of the tokens of bin `bin`, most significant byte
+  // first: to the key at which their count (or mass) reaches `want`, `before`
+  // being what the larger keys have of it.  Ties of the cut key stand for `ties`
+  // tokens.
+  uint32_t cut = 0;              // keys above it are kept, and the first `ties` tokens of it
+  int64_t ties = 0;
+  auto descend = [&](bool by_mass, int bin, uint64_t want, uint64_t &before, uint32_t &found) {
     uint32_t prefix = 0;
-    unsigned long long before = 0, have = 0;
+    before = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kThreads) hist_n[i] = 0, hist_w[i] = 0;
+      if (tid < 256) digit_n[tid] = 0, digit_w[tid] = 0;
       __syncthreads();
-      for (int v = tid; v < a.vocab; v += kThreads) {
-        const float x = logit<BF16>(a, row, v);
-        const uint32_t key = order_key(x);
-        if (shift < 24 && (key >> (shift + 8)) != prefix) continue;
-        if (by_mass && key <= cut) continue;   // the ties at the cut are added below
-        atomicAdd(&hist_n[(key >> shift) & 255], 1u);
-        if (by_mass) atomicAdd(&hist_w[(key >> shift) & 255], (unsigned long long)mass_of(x, top, t));
-      }
+      each([&](uint32_t key, int) {
+        if (shift < 24 && (key >> (shift + 8)) != prefix) return;
+        if (key_bin(key) != bin) return;
+        if (!by_mass) atomicAdd(&digit_n[(key >> shift) & 255], 1u);
+        else if (key > cut) atomicAdd(&digit_w[(key >> shift) & 255], (unsigned long long)mass_of(r, key_value(key)));
+      });
       __syncthreads();
-      if (tid == 0) {
-        if (by_mass && (shift == 24 || (cut >> (shift + 8)) == prefix))
-          hist_w[(cut >> shift) & 255] += (unsigned long long)ties * mass_of(key_value(cut), top, t);
-        int b = 255;
-        unsigned long long here = by_mass ? hist_w[b] : hist_n[b];
-        while (b > 0 && before + here < want) {
-          before += here;
-          --b;
-          here = by_mass ? hist_w[b] : hist_n[b];
+      if (by_mass && tid == 0 && ties > 0 && key_bin(cut) == bin && (shift == 24 || (cut >> (shift + 8)) == prefix))
+        digit_w[(cut >> shift) & 255] += (unsigned long long)ties * mass_of(r, key_value(cut));
+      __syncthreads();
+      if (tid < 64) {
+        // lane l holds digits 255 - 4 l .. 252 - 4 l, the largest first
+        uint64_t d[4], sum = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          d[q] = by_mass ? digit_w[255 - 4 * lane - q] : digit_n[255 - 4 * lane - q];
+          sum += d[q];
         }
-        s_key = (prefix << 8) | (uint32_t)b;
-        s_a = before;
-        s_b = here;
+        uint64_t s = sum;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const uint64_t y = __shfl_up((unsigned long long)s, o, 64);
+          if (lane >= o) s += y;
+        }
+        // (the last digit that has anything, should the total fall short)
+        const unsigned long long reach = __ballot(before + s >= want), some = __ballot(sum > 0);
+        const int l = reach ? __ffsll(reach) - 1 : some ? 63 - __clzll(some) : 63;
+        if (lane == l) {
+          uint64_t at = before + s - sum;
+          int q = 0;
+          while (q < 3 && at + d[q] < want) at += d[q++];
+          s_digit = (uint32_t)(255 - 4 * lane - q);
+          s_before = at;
+        }
       }
       __syncthreads();
-      prefix = s_key;
-      before = s_a;
-      have = s_b;
+      prefix = (prefix << 8) | s_digit;
+      before = s_before;
       __syncthreads();
     }
-    s_c = have;
-    const unsigned long long left = want > before ? want - before : 0;
-    return make_ulonglong2(left, prefix);
+    found = prefix;
   };
-  if (k < a.vocab) {
-    const ulonglong2 d = descend(false, (unsigned long long)k);
-    cut = (uint32_t)d.y;
-    ties = (int64_t)d.x;
-  } else {
-    // every token: the cut lies below the smallest key
-    cut = 0;
-    ties = 0;
-  }
-  auto total_kept = [&](double w_least) {
-    unsigned long long sum = 0;
-    for (int v = tid; v < a.vocab; v += kThreads) {
-      const float x = logit<BF16>(a, row, v);
-      if (order_key(x) <= cut) continue;
-      const uint64_t w = mass_of(x, top, t);
-      if ((double)w >= w_least) sum += w;
-    }
-    if (tid == 0) s_a = 0;
-    __syncthreads();
-    atomicAdd(&s_a, sum);
-    __syncthreads();
-    unsigned long long all = s_a;
-    __syncthreads();
-    const uint64_t w = cut ? mass_of(key_value(cut), top, t) : 0;
-    if ((double)w >= w_least) all += (unsigned long long)ties * w;
-    return all;
+  // sum over the workgroup of f(key, index), over the tokens of interest
+  auto sum_of = [&](auto f) {
+    uint64_t v = 0, total;
+    each([&](uint32_t key, int i) { v += f(key, i); });
+    block_scan<T>(v, scan, total);
+    return total;
   };
-  if (p < 1.f) {
-    const double want = (double)p * (double)total_kept(0.0);
-    const unsigned long long w = want > 1.0 ? (unsigned long long)__builtin_ceil(want) : 1ull;
-    const ulonglong2 d = descend(true, w);
-    const uint32_t c = (uint32_t)d.y;
-    const uint64_t each = mass_of(key_value(c), top, t);
-    // each token at the cut whose predecessors' mass is below `want`
-    const uint64_t n = each ? (d.x + each - 1) / each : 0;
-    if (c != cut || (int64_t)n < ties) {
-      cut = c;
-      ties = (int64_t)n;
-    }
-  }
-  const double w_least = fmin((double)least, 1.0) * kUnit;
-  const unsigned long long kept = total_kept(w_least);
-  const double target = fmax((double)u, 0.0) * (double)kept;
 
-  // tokens in index order, kThreads at a time
-  unsigned long long run = 0;
-  int64_t tie_run = 0;
-  for (int v0 = 0; v0 < a.vocab; v0 += kThreads) {
-    const int v = v0 + tid;
-    const float x = v < a.vocab ? logit<BF16>(a, row, v) : -INFINITY;
-    const uint32_t key = order_key(x);
-    const bool tie = v < a.vocab && key == cut;
-    scan[tid] = tie;
+  uint64_t total = cum_w[kBins];
+  int bin_k = kBins;
+  if (r.k) {
+    for (int b = tid; b < kBins; b += T)
+      if ((int64_t)cum_n[b] < r.k && r.k <= (int64_t)cum_n[b + 1]) s_bin = b;
     __syncthreads();
-    for (int off = 1; off < kThreads; off <<= 1) {
-      const unsigned long long o = tid >= off ? scan[tid - off] : 0;
-      __syncthreads();
-      scan[tid] += o;
-      __syncthreads();
+    bin_k = s_bin;
+    __syncthreads();
+    if (bin_k < kBins) {
+      const uint64_t need = (uint64_t)r.k - cum_n[bin_k];
+      uint64_t before;
+      uint32_t found;
+      descend(false, bin_k, need, before, found);
+      cut = found;
+      ties = (int64_t)(need - before);
+      const uint64_t above = sum_of([&](uint32_t key, int) -> uint64_t {
+        return key > cut && key_bin(key) == bin_k ? mass_of(r, key_value(key)) : 0;
+      });
+      total = cum_w[bin_k] + above + (uint64_t)ties * mass_of(r, key_value(cut));
     }
-    const int64_t rank = tie_run + (int64_t)scan[tid] - 1;
-    tie_run += (int64_t)scan[kThreads - 1];
-    __syncthreads();
-    uint64_t w = v < a.vocab && (key > cut || (tie && rank < ties)) ? mass_of(x, top, t) : 0;
-    if ((double)w < w_least) w = 0;
-    scan[tid] = w;
-    __syncthreads();
-    for (int off = 1; off < kThreads; off <<= 1) {
-      const unsigned long long o = tid >= off ? scan[tid - off] : 0;
-      __syncthreads();
-      scan[tid] += o;
-      __syncthreads();
-    }
-    const unsigned long long upto = run + scan[tid];
-    // with u >= 1 nothing exceeds the target and the last kept token is drawn
-    if (w && ((double)upto > target || upto == kept)) atomicMin(&s_token, v);
-    run += scan[kThreads - 1];
-    __syncthreads();
-    if (s_token != INT_MAX) break;
   }
+  if (r.p < 1.0) {
+    const double wanted = r.p * (double)total;
+    const uint64_t want = wanted > 1.0 ? (uint64_t)__builtin_ceil(wanted) : 1;
+    if (tid == 0) s_bin = kBins - 1;
+    __syncthreads();
+    for (int b = tid; b < kBins; b += T)
+      if (cum_w[b] < want && want <= cum_w[b + 1]) s_bin = b;
+    __syncthreads();
+    const int bin_p = min(s_bin, bin_k);
+    __syncthreads();
+    uint64_t before;
+    uint32_t found;
+    descend(true, bin_p, want - cum_w[bin_p], before, found);
+    const uint64_t each_w = mass_of(r, key_value(found)), left = want - cum_w[bin_p] - before;
+    const int64_t n = each_w ? (int64_t)((left + each_w - 1) / each_w) : 0;   // tokens of that key it takes to get there
+    if (found > cut || n < ties) {
+      cut = found;
+      ties = n;
+    }
+  }
+  // the index of the last kept token of the cut's key
+  int last_tie = INT_MAX;
+  if (cut) {
+    const uint64_t equal = sum_of([&](uint32_t key, int) -> uint64_t { return key == cut; });
+    if (ties < (int64_t)equal) {
+      if (tid == 0) s_bin = -1;
+      __syncthreads();
+      int64_t run = 0;
+      const int items = whole ? a.vocab : listed;
+      for (int i0 = 0; i0 < items; i0 += T) {
+        const int i = i0 + tid;
+        bool tie = false;
+        int index = 0;
+        if (i < items) {
+          index = whole ? i : list_idx[i];
+          tie = (whole ? order_key(logit_at<BF16>(r, i)) : list_key[i]) == cut;
+        }
+        const unsigned long long b = __ballot(tie);
+        if (lane == 0) scan[wave] = (uint64_t)__popcll(b);
+        __syncthreads();
+        int64_t rank = run;
+        for (int q = 0; q < T / 64; ++q) {
+          if (q < wave) rank += (int64_t)scan[q];
+          run += (int64_t)scan[q];
+        }
+        rank += __popcll(b & ((1ull << lane) - 1));
+        if (tie && rank == ties - 1) s_bin = index;
+        __syncthreads();
+        if (run >= ties) break;
+      }
+      last_tie = s_bin;
+    }
+  }
+  auto kept = [&](uint32_t key, int i) -> uint64_t {
+    if (key < cut || (key == cut && i > last_tie)) return 0;
+    const uint64_t w = mass_of(r, key_value(key));
+    return (double)w >= r.least ? w : 0;
+  };
+
+  // kept mass by part: whole bins from its histogram, the rest token by token
+  const int whole_bins = min(cut ? key_bin(cut) : kBins, mlo);
+  if (!whole) {
+    for (int i = tid; i < listed; i += T) {
+      const uint32_t key = list_key[i];
+      if (key_bin(key) < whole_bins) continue;
+      const uint64_t w = kept(key, list_idx[i]);
+      if (w) atomicAdd(&part_w[(list_idx[i] + r.off) / (a.part_vecs * EPV)], (unsigned long long)w);
+    }
+    for (int p = wave; p < a.parts; p += T / 64) {
+      uint64_t w = 0;
+      const uint64_t *h = a.ws_hist + (row * a.parts + p) * kBins;
+      for (int b = lane; b < whole_bins; b += 64) w += h[b] & kMassMask;
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) w += __shfl_xor((unsigned long long)w, o, 64);
+      if (lane == 0) atomicAdd(&part_w[p], (unsigned long long)w);
+    }
+  } else {
+    for (int p = 0; p < a.parts; ++p) {
+      uint64_t w = 0;
+      for (int v = tid; v < a.part_vecs; v += T) {
+        Vec<BF16> x;
+        x.load(r, a.vocab, p * a.part_vecs + v);
+#pragma unroll
+        for (int i = 0; i < EPV; ++i)
+          if (x.in(i, a.vocab)) w += kept(order_key(x.x[i]), x.first + i);
+      }
+      atomicAdd(&part_w[p], (unsigned long long)w);
+    }
+  }
+  __syncthreads();
+  // the part that holds the target, then the token
+  if (tid < 64) {
+    const uint64_t w = part_w[lane];
+    uint64_t s = w;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint64_t y = __shfl_up((unsigned long long)s, o, 64);
+      if (lane >= o) s += y;
+    }
+    const uint64_t all = __shfl((unsigned long long)s, 63, 64);
+    // the first sum above the target; with u >= 1 there is none, and the last token with mass is drawn
+    const double target = fmax((double)r.u, 0.0) * (double)all;
+    const unsigned long long hit = __ballot(w > 0 && ((double)s > target || s == all));
+    const int l = __ffsll(hit) - 1;
+    if (lane == l) {
+      s_bin = l;
+      s_before = s - w;
+      s_sum = all;
+    }
+  }
+  __syncthreads();
+  const int part = s_bin;
+  const uint64_t all = s_sum;
+  uint64_t run = s_before;
+  const double target = fmax((double)r.u, 0.0) * (double)all;
+  const int per = (a.part_vecs + T - 1) / T;      // consecutive vectors per thread
+  uint64_t mine = 0;
+  for (int q = 0; q < per; ++q) {
+    const int v = tid * per + q;
+    if (v >= a.part_vecs) break;
+    Vec<BF16> x;
+    x.load(r, a.vocab, part * a.part_vecs + v);
+#pragma unroll
+    for (int i = 0; i < EPV; ++i)
+      if (x.in(i, a.vocab)) mine += kept(order_key(x.x[i]), x.first + i);
+  }
+  uint64_t part_total;
+  run += block_scan<T>(mine, scan, part_total);
+  if (mine && ((double)(run + mine) > target || run + mine == all)) {
+    // this thread's tokens, or a thread's before it, hold the first sum above the target
+    for (int q = 0; q < per; ++q) {
+      const int v = tid * per + q;
+      if (v >= a.part_vecs) break;
+      Vec<BF16> x;
+      x.load(r, a.vocab, part * a.part_vecs + v);
+#pragma unroll
+      for (int i = 0; i < EPV; ++i) {
+        const uint64_t w = x.in(i, a.vocab) ? kept(order_key(x.x[i]), x.first + i) : 0;
+        run += w;
+        if (w && ((double)run > target || run == all)) atomicMin(&s_token, x.first + i);
+      }
+    }
+  }
+  __syncthreads();
   if (tid == 0) a.out_token[row] = s_token == INT_MAX ? -1 : s_token;
+}
+
+template <bool BF16>
+hipError_t launch(const SampleArgs &a, hipStream_t stream) {
+  const dim3 parts((unsigned)((int64_t)a.rows * a.parts)), block(kThreads);
+  hipLaunchKernelGGL(sample_max_kernel<BF16>, parts, block, 0, stream, a);
+  hipLaunchKernelGGL(sample_hist_kernel<BF16>, parts, block, 0, stream, a);
+  hipLaunchKernelGGL(sample_list_kernel<BF16>, parts, block, 0, stream, a);
+  hipLaunchKernelGGL(sample_draw_kernel<BF16>, dim3((unsigned)a.rows), dim3(kDrawThreads), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t stream) {
-  if (bf16)
-    hipLaunchKernelGGL(sample_kernel<true>, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL(sample_kernel<false>, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
-  return hipGetLastError();
+  return bf16 ? launch<true>(a, stream) : launch<false>(a, stream);
 }
 
 }  // namespace adaserve

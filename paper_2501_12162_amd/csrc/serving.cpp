@@ -207,6 +207,8 @@ int32_t validate_decode(int32_t num_requests, int32_t hq, int32_t max_context, i
 
 int32_t validate_sample(int32_t num_rows, int32_t vocab, int32_t dtype) {
   if (num_rows < 0) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "num_rows %d < 0", num_rows);
+  if (num_rows > INT32_MAX / kSampleMaxParts)
+    return fail(ADASERVE_ERR_UNSUPPORTED, "num_rows %d > %d", num_rows, INT32_MAX / kSampleMaxParts);
   if (vocab < 1 || vocab > kSampleMaxVocab)
     return fail(vocab < 1 ? ADASERVE_ERR_INVALID_ARGUMENT : ADASERVE_ERR_UNSUPPORTED, "vocab %d outside [1, %d]",
                 vocab, kSampleMaxVocab);
@@ -462,14 +464,12 @@ int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_
 
 size_t adaserve_sample_workspace_bytes(int32_t num_rows, int32_t vocab, int32_t dtype) {
   if (validate_sample(num_rows, vocab, dtype) != ADASERVE_OK) return SIZE_MAX;
-  return 0;
+  return sample_plan(num_rows, vocab, dtype == ADASERVE_BF16).bytes;
 }
 
 int32_t adaserve_sample(const void *logits, int64_t row_stride, int32_t num_rows, int32_t vocab, int32_t dtype,
                         const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
                         const float *u, int32_t *out_token, void *workspace, size_t workspace_bytes, void *stream) {
-  (void)workspace;
-  (void)workspace_bytes;
   int32_t st = validate_sample(num_rows, vocab, dtype);
   if (st != ADASERVE_OK) return st;
   if (row_stride < vocab)
@@ -479,6 +479,9 @@ int32_t adaserve_sample(const void *logits, int64_t row_stride, int32_t num_rows
   if (!aligned(logits, elem_size(dtype)) || !aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) ||
       !aligned(min_p, 4) || !aligned(u, 4) || !aligned(out_token, 4))
     return fail(ADASERVE_ERR_INVALID_ARGUMENT, "a pointer is not aligned to its elements");
+  const SamplePlan plan = sample_plan(num_rows, vocab, dtype == ADASERVE_BF16);
+  st = validate_workspace(workspace, workspace_bytes, plan.bytes);
+  if (st != ADASERVE_OK) return st;
   st = check_device();
   if (st != ADASERVE_OK) return st;
   SampleArgs a{};
@@ -492,6 +495,16 @@ int32_t adaserve_sample(const void *logits, int64_t row_stride, int32_t num_rows
   a.min_p = min_p;
   a.u = u;
   a.out_token = out_token;
+  a.parts = plan.parts;
+  a.part_vecs = plan.part_vecs;
+  a.list_cap = plan.list_cap;
+  char *ws = (char *)workspace;
+  a.ws_hist = (uint64_t *)ws;
+  a.ws_cum_w = (uint64_t *)(ws + plan.cum_w);
+  a.ws_cum_n = (uint32_t *)(ws + plan.cum_n);
+  a.ws_max = (uint32_t *)(ws + plan.max);
+  a.ws_count = (uint32_t *)(ws + plan.count);
+  a.ws_list = (uint16_t *)(ws + plan.list);
   return launch_status(launch_sample(a, dtype == ADASERVE_BF16, (hipStream_t)stream), "sampling launch");
 }
 
