@@ -29,6 +29,8 @@
 // values, or nearly flat) is searched as a whole in pass 4.
 #include <limits.h>
 
+#include <type_traits>
+
 #include "device_common.h"
 #include "serving.h"
 
@@ -103,6 +105,9 @@ __device__ __forceinline__ uint64_t mass_of(const Row &r, float x) { return mass
 template <bool BF16>
 struct Vec {
   static constexpr int EPV = BF16 ? 8 : 4;
+  // Loads in flight per thread in passes 1 to 3: 4096 elements, the smallest
+  // part, are 4 fp32 vectors per thread and 2 bf16 ones.
+  static constexpr int BATCH = BF16 ? 2 : 4;
   float x[EPV];
   int first;   // index of x[0], may lie before the row
   __device__ __forceinline__ void load(const Row &r, int vocab, int v) {
@@ -177,12 +182,12 @@ __global__ __launch_bounds__(kThreads) void sample_max_kernel(SampleArgs a) {
   const Row r = row_place<BF16>(a, row);
   const int v0 = part * a.part_vecs;
   uint32_t best = 0;
-  Vec<BF16> x[2];
-  for (int v = threadIdx.x; v < a.part_vecs; v += 2 * kThreads) {
+  Vec<BF16> x[Vec<BF16>::BATCH];
+  for (int v = threadIdx.x; v < a.part_vecs; v += Vec<BF16>::BATCH * kThreads) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) x[h].load(r, v + h * kThreads < a.part_vecs ? a.vocab : 0, v0 + v + h * kThreads);
+    for (int h = 0; h < Vec<BF16>::BATCH; ++h) x[h].load(r, v + h * kThreads < a.part_vecs ? a.vocab : 0, v0 + v + h * kThreads);
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < Vec<BF16>::BATCH; ++h)
 #pragma unroll
       for (int i = 0; i < Vec<BF16>::EPV; ++i)
         best = max(best, x[h].x[i] < INFINITY ? order_key(x[h].x[i]) : 0xffffffffu);
@@ -209,15 +214,18 @@ __global__ __launch_bounds__(kThreads) void sample_hist_kernel(SampleArgs a) {
   for (int b = threadIdx.x; b < kBins; b += kThreads) hist[b] = 0;
   __syncthreads();
   const int v0 = part * a.part_vecs;
-  for (int v = threadIdx.x; v < a.part_vecs; v += kThreads) {
-    Vec<BF16> x;
-    x.load(r, a.vocab, v0 + v);
+  Vec<BF16> x[Vec<BF16>::BATCH];
+  for (int v = threadIdx.x; v < a.part_vecs; v += Vec<BF16>::BATCH * kThreads) {
 #pragma unroll
-    for (int i = 0; i < Vec<BF16>::EPV; ++i) {
-      const double y = depth_of(r, x.x[i]);
-      const int b = bin_of(y);
-      if (b < kBins - 1) atomicAdd(&hist[b], (unsigned long long)(mass_at(y) | (1ull << kMassBits)));
-    }
+    for (int h = 0; h < Vec<BF16>::BATCH; ++h) x[h].load(r, v + h * kThreads < a.part_vecs ? a.vocab : 0, v0 + v + h * kThreads);
+#pragma unroll
+    for (int h = 0; h < Vec<BF16>::BATCH; ++h)
+#pragma unroll
+      for (int i = 0; i < Vec<BF16>::EPV; ++i) {
+        const double y = depth_of(r, x[h].x[i]);
+        const int b = bin_of(y);
+        if (b < kBins - 1) atomicAdd(&hist[b], (unsigned long long)(mass_at(y) | (1ull << kMassBits)));
+      }
   }
   __syncthreads();
   uint64_t *out = a.ws_hist + (int64_t)blockIdx.x * kBins;
@@ -257,6 +265,8 @@ __device__ __forceinline__ void least_bins(const Row &r, int &lo, int &hi) {
   hi = bin_of(b + 1e-6);
 }
 
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a) {
   static_assert(kBins == 2 * kThreads, "two bins per thread");
@@ -271,18 +281,27 @@ __global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool filtered = r.k || r.p < 1.0 || r.least > 0.0;
   if (!filtered && part > 0) {
-    if (tid == 0) a.ws_count[blockIdx.x] = 0;
+    if (lane == 0) a.ws_count[(int64_t)blockIdx.x * (kThreads / 64) + wave] = 0;
     return;
   }
   // the row's histogram and its running sums
   uint64_t w[2] = {0, 0}, n[2] = {0, 0};
   const uint64_t *h = a.ws_hist + row * a.parts * kBins + 2 * tid;
-#pragma unroll 4
-  for (int p = 0; p < a.parts; ++p) {
-    const uint64_t x0 = h[(int64_t)p * kBins], x1 = h[(int64_t)p * kBins + 1];
-    w[0] += x0 & kMassMask, n[0] += x0 >> kMassBits;
-    w[1] += x1 & kMassMask, n[1] += x1 >> kMassBits;
-  }
+  auto add_parts = [&](int p, auto count) {   // this many loads in flight
+    constexpr int C = decltype(count)::value;
+    u64x2 x[C];
+#pragma unroll
+    for (int q = 0; q < C; ++q) x[q] = *(const u64x2 *)(h + (int64_t)(p + q) * kBins);
+#pragma unroll
+    for (int q = 0; q < C; ++q) {
+      w[0] += x[q][0] & kMassMask, n[0] += x[q][0] >> kMassBits;
+      w[1] += x[q][1] & kMassMask, n[1] += x[q][1] >> kMassBits;
+    }
+  };
+  int done = 0;
+  for (; done + 16 <= a.parts; done += 16) add_parts(done, std::integral_constant<int, 16>{});
+  for (; done + 4 <= a.parts; done += 4) add_parts(done, std::integral_constant<int, 4>{});
+  for (; done < a.parts; ++done) add_parts(done, std::integral_constant<int, 1>{});
   uint64_t all_w, all_n;
   const uint64_t before_w = block_scan<kThreads>(w[0] + w[1], scan, all_w);
   const uint64_t before_n = block_scan<kThreads>(n[0] + n[1], scan, all_n);
@@ -321,45 +340,47 @@ __global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a) {
   const int plo = cut_lo, phi = cut_hi;
   int mlo, mhi;
   least_bins(r, mlo, mhi);
-  // tokens of those bins, in index order
-  const int v0 = part * a.part_vecs;
-  uint16_t *list = a.ws_list + (int64_t)blockIdx.x * a.list_cap;
+  // tokens of those bins, in index order; each wave lists those of its quarter
+  const int quarter = a.part_vecs / (kThreads / 64);
+  const int v0 = part * a.part_vecs + wave * quarter;
+  const int64_t slot = (int64_t)blockIdx.x * (kThreads / 64) + wave;
+  uint64_t *list = a.ws_list + slot * kSampleListCap;
   uint32_t have = 0;
   if (filtered)
-    for (int v = tid; v < (a.part_vecs + kThreads - 1) / kThreads * kThreads; v += kThreads) {
-      Vec<BF16> x;
-      x.load(r, v < a.part_vecs ? a.vocab : 0, v0 + v);
-      uint32_t mine = 0;
+    for (int vb = 0; vb < quarter; vb += 64 * Vec<BF16>::BATCH) {
+      Vec<BF16> x[Vec<BF16>::BATCH];
 #pragma unroll
-      for (int i = 0; i < Vec<BF16>::EPV; ++i) {
-        const int b = bin_of(depth_of(r, x.x[i]));
-        const bool take = b < kBins - 1 && (b == ck || (b >= plo && b <= phi) || (b >= mlo && b <= mhi)) &&
-                          v < a.part_vecs && x.in(i, a.vocab);
-        mine |= (uint32_t)take << i;
+      for (int h = 0; h < Vec<BF16>::BATCH; ++h) {
+        const int v = vb + h * 64 + lane;
+        x[h].load(r, v < quarter ? a.vocab : 0, v0 + v);
       }
-      const int count = __popc(mine);
-      int s = count;
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(s, o, 64);
-        if (lane >= o) s += y;
-      }
-      if (lane == 63) scan[wave] = (uint64_t)s;
-      __syncthreads();
-      uint32_t at = have + s - count;
-      for (int q = 0; q < kThreads / 64; ++q) {
-        if (q < wave) at += (uint32_t)scan[q];
-        have += (uint32_t)scan[q];
-      }
-      __syncthreads();
+      for (int h = 0; h < Vec<BF16>::BATCH; ++h) {
+        uint32_t mine = 0;
 #pragma unroll
-      for (int i = 0; i < Vec<BF16>::EPV; ++i)
-        if (mine >> i & 1) {
-          if (at < (uint32_t)a.list_cap) list[at] = (uint16_t)(v * Vec<BF16>::EPV + i);
-          ++at;
+        for (int i = 0; i < Vec<BF16>::EPV; ++i) {
+          const int b = bin_of(depth_of(r, x[h].x[i]));
+          mine |= (uint32_t)(b < kBins - 1 && (b == ck || (b >= plo && b <= phi) || (b >= mlo && b <= mhi))) << i;
         }
+        if (!__any(mine != 0)) continue;
+        const int count = __popc(mine);
+        int s = count;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const int y = __shfl_up(s, o, 64);
+          if (lane >= o) s += y;
+        }
+        uint32_t at = have + s - count;
+        have += (uint32_t)__shfl(s, 63, 64);
+#pragma unroll
+        for (int i = 0; i < Vec<BF16>::EPV; ++i)
+          if (mine >> i & 1) {
+            if (at < (uint32_t)kSampleListCap) list[at] = (uint64_t)order_key(x[h].x[i]) << 32 | (uint32_t)(x[h].first + i);
+            ++at;
+          }
+      }
     }
-  if (tid == 0) a.ws_count[blockIdx.x] = have;
+  if (lane == 0) a.ws_count[slot] = have;
 }
 
 template <bool BF16>
@@ -370,7 +391,9 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
   __shared__ unsigned long long digit_w[256];
   __shared__ uint32_t digit_n[256];
   __shared__ unsigned long long part_w[kSampleMaxParts];
-  __shared__ uint32_t part_at[kSampleMaxParts + 1];
+  __shared__ uint32_t list_at[kSampleMaxParts * 4 + 1];
+  __shared__ uint64_t cum_w[kBins + 1];
+  __shared__ uint32_t cum_n[kBins + 1];
   __shared__ uint64_t scan[T / 64];
   __shared__ uint64_t s_before, s_sum;
   __shared__ uint32_t s_digit;
@@ -403,39 +426,41 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
     if (tid == 0) a.out_token[row] = s_token;
     return;
   }
-  const uint64_t *cum_w = a.ws_cum_w + row * (kBins + 1);
-  const uint32_t *cum_n = a.ws_cum_n + row * (kBins + 1);
   int mlo, mhi;
   least_bins(r, mlo, mhi);
 
-  // the listed tokens, in index order
-  if (tid < 64) {
-    uint32_t c = lane < a.parts ? a.ws_count[row * a.parts + lane] : 0;
-    const bool over = __any(c > (uint32_t)a.list_cap);
-    uint32_t s = c;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t y = (uint32_t)__shfl_up((int)s, o, 64);
-      if (lane >= o) s += y;
-    }
-    part_at[lane + 1] = s;
-    if (lane == 0) part_at[0] = 0;
-    part_w[lane] = 0;
-    if (lane == 63) s_digit = over || s > (uint32_t)kSampleList;
+  // the row's running sums, and the listed tokens in index order
+  for (int b = tid; b <= kBins; b += T) {
+    cum_w[b] = a.ws_cum_w[row * (kBins + 1) + b];
+    cum_n[b] = a.ws_cum_n[row * (kBins + 1) + b];
   }
-  static_assert(kSampleMaxParts == 64, "one lane per part");
+  const int lists = a.parts * 4;
+  {
+    const uint32_t c = tid < lists ? a.ws_count[row * lists + tid] : 0;
+    uint64_t all;
+    const uint64_t before = block_scan<T>(c, scan, all);
+    const uint64_t over = __any(c > (uint32_t)kSampleListCap);
+    if (tid <= lists) list_at[tid] = (uint32_t)before;
+    if (tid < kSampleMaxParts) part_w[tid] = 0;
+    if (tid == 0) s_digit = all > (uint64_t)kSampleList;
+    __syncthreads();
+    if (over && lane == 0) s_digit = 1;
+  }
+  static_assert(kSampleMaxParts * 4 < T, "one thread per list");
   __syncthreads();
   const bool whole = s_digit != 0;          // the lists do not hold them: the row is searched
-  const int listed = whole ? 0 : (int)part_at[kSampleMaxParts];
-  if (!whole)
-    for (int p = wave; p < a.parts; p += T / 64) {
-      const int at = (int)part_at[p], c = (int)part_at[p + 1] - at;
-      for (int j = lane; j < c; j += 64) {
-        const int i = p * a.part_vecs * EPV + a.ws_list[(row * a.parts + p) * a.list_cap + j] - r.off;
-        list_idx[at + j] = i;
-        list_key[at + j] = order_key(logit_at<BF16>(r, i));
-      }
+  const int listed = whole ? 0 : (int)list_at[lists];
+  for (int i = tid; i < listed; i += T) {
+    int lo = 0, n = lists;                  // the list that entry i is in
+    while (n > 1) {
+      const int half = n / 2;
+      if ((int)list_at[lo + half] <= i) lo += half, n -= half;
+      else n = half;
     }
+    const uint64_t e = a.ws_list[(row * lists + lo) * kSampleListCap + (i - (int)list_at[lo])];
+    list_key[i] = (uint32_t)(e >> 32);
+    list_idx[i] = (int32_t)(uint32_t)e;
+  }
   __syncthreads();
   // f(key, index) for every token that may be of interest (all of the row where
   // there are no lists)
@@ -664,9 +689,15 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
   }
   uint64_t part_total;
   run += block_scan<T>(mine, scan, part_total);
-  if (mine && ((double)(run + mine) > target || run + mine == all)) {
-    // this thread's tokens, or a thread's before it, hold the first sum above the target
-    for (int q = 0; q < per; ++q) {
+  // the first thread whose tokens take the sum beyond the target looks for the one
+  if (tid == 0) s_bin = T;
+  __syncthreads();
+  const bool here = mine && ((double)(run + mine) > target || run + mine == all);
+  const unsigned long long hit = __ballot(here);
+  if (hit && lane == __ffsll(hit) - 1) atomicMin(&s_bin, tid);
+  __syncthreads();
+  if (tid == s_bin) {
+    for (int q = 0; q < per && s_token == INT_MAX; ++q) {
       const int v = tid * per + q;
       if (v >= a.part_vecs) break;
       Vec<BF16> x;
@@ -675,7 +706,7 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
       for (int i = 0; i < EPV; ++i) {
         const uint64_t w = x.in(i, a.vocab) ? kept(order_key(x.x[i]), x.first + i) : 0;
         run += w;
-        if (w && ((double)run > target || run == all)) atomicMin(&s_token, x.first + i);
+        if (w && s_token == INT_MAX && ((double)run > target || run == all)) s_token = x.first + i;
       }
     }
   }

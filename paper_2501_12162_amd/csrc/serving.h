@@ -141,6 +141,7 @@ constexpr int kSampleMaxVocab = 1 << 20;   // sums of 2^32 per token stay below 
 constexpr int kSampleBins = 512;
 constexpr int kSampleMaxParts = 64;
 constexpr int kSampleList = 8192;           // listed tokens of a row that pass 4 holds in LDS
+constexpr int kSampleListCap = 512;         // tokens in the list of a quarter of a part
 
 struct SampleArgs {
   const void *logits;            // [rows, row_stride]
@@ -155,20 +156,19 @@ struct SampleArgs {
   int32_t *out_token;            // [rows]
   int32_t parts;                 // parts of a row (SamplePlan)
   int32_t part_vecs;             // 16-byte vectors per part
-  int32_t list_cap;              // tokens that a part can list
   uint32_t *ws_max;              // [rows, parts] largest key (all ones: a NaN or +inf)
   uint64_t *ws_hist;             // [rows, parts, bins] mass | count << 48
   uint64_t *ws_cum_w;            // [rows, bins + 1] mass of the bins before
   uint32_t *ws_cum_n;            // [rows, bins + 1] tokens of the bins before
-  uint32_t *ws_count;            // [rows, parts] listed tokens
-  uint16_t *ws_list;             // [rows, parts, list_cap] their places in the part
+  uint32_t *ws_count;            // [rows, parts, 4] listed tokens
+  uint64_t *ws_list;             // [rows, parts, 4, kSampleListCap] key << 32 | index
 };
 
 // Parts of 4096 to 32768 logits: a few rows are cut finely, to run on many
 // compute units; many rows coarsely, since pass 3 adds up a row's histograms in
 // every part.  At most 64 parts (2^20 logits and up to 7 before the row).
 struct SamplePlan {
-  int32_t parts, part_vecs, list_cap;
+  int32_t parts, part_vecs;
   size_t cum_w, cum_n, max, count, list, bytes;   // offsets; the histograms come first
 };
 
@@ -179,15 +179,14 @@ inline SamplePlan sample_plan(int32_t rows, int32_t vocab, bool bf16) {
   SamplePlan p;
   p.part_vecs = elements / epv;
   p.parts = (vocab + epv - 1 + elements - 1) / elements;
-  p.list_cap = elements < kSampleList ? elements : kSampleList;
   const size_t all = (size_t)rows * p.parts;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   p.cum_w = up(all * kSampleBins * 8);
   p.cum_n = p.cum_w + up((size_t)rows * (kSampleBins + 1) * 8);
   p.max = p.cum_n + up((size_t)rows * (kSampleBins + 1) * 4);
   p.count = p.max + up(all * 4);
-  p.list = p.count + up(all * 4);
-  p.bytes = rows ? p.list + up(all * p.list_cap * 2) : 0;
+  p.list = p.count + up(all * 4 * 4);
+  p.bytes = rows ? p.list + up(all * 4 * kSampleListCap * 8) : 0;
   return p;
 }
 
