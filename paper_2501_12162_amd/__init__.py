@@ -307,22 +307,24 @@ def _device_call(name: str, tensors, stream, *args) -> None:
     """Calls entry point ``name`` on the tensors' device: its current stream where none is given, and
     the device made current for the call where it is not."""
     import torch
-    device = None
+    device = -1
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
+        at = t.get_device()
+        if at < 0:
             raise ValueError("expected a device tensor")
-        if device is None:
-            device = t.device.index
-        elif t.device.index != device:
+        if device < 0:
+            device = at
+        elif at != device:
             raise ValueError("tensors are on different devices")
     fn = getattr(load_library(), name)
-    if device is None or device == torch.cuda.current_device():
-        st = fn(*args, _stream(stream))
+    s = (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+    if device == torch.cuda.current_device():
+        st = fn(*args, s)
     else:
         with torch.cuda.device(device):
-            st = fn(*args, _stream(stream))
+            st = fn(*args, s)
     if st != ADASERVE_OK:
         _check(st)
 

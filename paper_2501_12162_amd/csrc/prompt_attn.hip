@@ -39,7 +39,7 @@ struct PromptUnit {
 // where the search starts and stays.  With split keys the table holds the
 // requests one after another, and a tile's heads come once per chunk.  Without a
 // table: request by request, the last tile first.
-__device__ __forceinline__ bool find_prompt_unit(const PagedAttnArgs &a, int64_t u, int32_t &e, PromptUnit &un) {
+__device__ __forceinline__ bool find_prompt_unit(const PromptAttnArgs &a, int64_t u, int32_t &e, PromptUnit &un) {
   if (u >= a.units) return false;
   int32_t r = -1, token0 = 0, n = 0, ctx = 0, tile = 0, g = 0, k0 = 0;
   if (a.chunks > 1) {
@@ -117,7 +117,7 @@ __device__ __forceinline__ int64_t prompt_round_unit(int64_t b, int64_t k, int64
 // Both halves take the same K and V fragments from registers; the next ones
 // are read in phase B as the current ones are used up.
 template <int D>
-__global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAttnArgs a) {
   constexpr int KS = D / 16, DT = D / 32, KB = 32, ROWB = D * 2, NCH = D / 8;
   constexpr int BLK = KB * ROWB;
   constexpr int WI = BLK / 1024 / kWaves;
@@ -582,7 +582,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PagedAttn
 // Joins the chunks of split keys: with m the largest reference of the row's
 // chunks, out = sum 2^(m_c - m) o_c / sum 2^(m_c - m) l_c.  One wave per row.
 template <int D>
-__global__ __launch_bounds__(kThreads) void prompt_join_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(kThreads) void prompt_join_kernel(PromptAttnArgs a) {
   constexpr int EPL = D / 64;
   const int lane = threadIdx.x & 63;
   const int64_t id = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
@@ -639,7 +639,7 @@ __global__ __launch_bounds__(kThreads) void prompt_join_kernel(PagedAttnArgs a) 
 // bf16's), so two row tiles share each operand only where there are enough tiles
 // to fill the device.
 template <int D, int RB>
-__global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArgs a) {
   constexpr int RT = 16 * RB;
   constexpr int NC = D / 16;      // 16-byte K loads per lane and page
   constexpr int NH = D / 64;      // 16-byte V loads per lane and key
@@ -864,13 +864,13 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PagedAttnArgs
 }
 
 template <int D, int RB>
-void launch_prompt_f32(const PagedAttnArgs &a, int64_t units, hipStream_t stream) {
+void launch_prompt_f32(const PromptAttnArgs &a, int64_t units, hipStream_t stream) {
   hipLaunchKernelGGL((prompt_attn_f32_kernel<D, RB>), dim3((unsigned)units), dim3(kThreads), 0, stream, a);
 }
 
 }  // namespace
 
-hipError_t launch_prompt_attn(const PagedAttnArgs &a, int head_dim, bool bf16, hipStream_t stream) {
+hipError_t launch_prompt_attn(const PromptAttnArgs &a, int head_dim, bool bf16, hipStream_t stream) {
   const dim3 block(kThreads);
   if (bf16) {
     const dim3 grid((unsigned)a.grid);

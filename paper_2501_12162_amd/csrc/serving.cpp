@@ -144,7 +144,7 @@ PromptPlan prompt_plan(int32_t num_requests, const int32_t *indptr, const int32_
   return p;
 }
 
-void fill_prompt(PagedAttnArgs &a, const PromptPlan &p, const int32_t *indptr, const int32_t *ctx, void *workspace) {
+void fill_prompt(PromptAttnArgs &a, const PromptPlan &p, const int32_t *indptr, const int32_t *ctx, void *workspace) {
   const bool split = p.chunks > 1;
   int32_t count = 0;
   if (a.num_requests <= kPromptTable)
@@ -364,7 +364,7 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
   if (st != ADASERVE_OK) return st;
   st = check_device();
   if (st != ADASERVE_OK) return st;
-  PagedAttnArgs a{};
+  PromptAttnArgs a{};
   a.num_requests = num_requests;
   a.token_indptr = token_indptr;
   a.context_len = context_len;

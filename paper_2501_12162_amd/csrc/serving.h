@@ -90,6 +90,10 @@ struct PagedAttnArgs {
   int32_t *ws_request;           // [B, 2] first unit, units; null: nothing is split
   float *ws_ml;                  // [units, heads, row groups, kDecodeRows, 2] reference, sum
   float *ws_o;                   // [units, heads, row groups, kDecodeRows, D] weighted sums of V
+};
+
+// (apart, since the launches of decode attention need not carry its 2.5 KB)
+struct PromptAttnArgs : PagedAttnArgs {
   PromptEntry table[kPromptTable];
 };
 
@@ -133,7 +137,7 @@ inline DecodePlan decode_plan(int32_t B, int32_t hq, int32_t hkv, int32_t head_d
   return p;
 }
 
-hipError_t launch_prompt_attn(const PagedAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
+hipError_t launch_prompt_attn(const PromptAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
 hipError_t launch_decode_attn(const PagedAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
 
 constexpr int kSampleMaxVocab = 1 << 20;   // sums of 2^32 per token stay below 2^53
