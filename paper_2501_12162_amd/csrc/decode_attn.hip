@@ -1,11 +1,11 @@
 // Attention of one new token per request over its paged cache on gfx950.
 //
-// A unit of work is (request, kv-head, up to 8 of its query heads, a run of
-// 32-key blocks); the requests' caches are cut into runs so that the batch
-// fills the device whatever its lengths, and the runs of one request are
-// joined by a second launch.  The lengths are read on the device only: every
-// workgroup finds its unit from all of them (schedule()), so a captured launch
-// follows them.
+// A unit of work is (request, kv-head, a run of 32-key blocks), with all query
+// heads of the kv-head as its rows; the requests' caches are cut into runs so
+// that the batch fills the device whatever its lengths, and the runs of one
+// request are joined by a second launch.  The lengths are read on the device
+// only: every workgroup finds its unit from all of them (schedule()), so a
+// captured launch follows them.
 //
 // Bound by memory: 2 c Hkv D s bytes per request against 4 c Hq D flops.  So
 // everything serves to keep loads in flight: no LDS in the loop and no
@@ -13,17 +13,21 @@
 // straight in registers, 16 KB of them in flight per wave.
 //  * S^T = K Q^T on the matrix cores (16 keys x 16 rows; K as it lies in
 //    memory is the A operand, lanes without a row multiply zeros).  A lane then
-//    holds 4 keys of one row.
-//  * O += P V on the vector ALUs: the matrix cores would want V transposed,
-//    which only LDS could give.  The 16 lanes that hold the weights of 4 keys
-//    also load the V rows of those 4 keys, a slice of columns each, so a weight
-//    reaches them by a broadcast within 16 lanes (DPP), and a row's output is
-//    spread over columns; the four groups of lanes are summed once at the end.
-//    Weights stay fp32.
+//    holds 4 keys of each 16 and one row: what P^T as a B operand wants.
+//  * O^T += V^T P^T on the matrix cores, too.  A contraction may take its slots
+//    in any order and a tile its rows: the lane that holds the weights of 4 keys
+//    loads D / 16 columns of those keys' values, and tile c of O^T is column c
+//    of each lane's.  fp32 values are operands as they are loaded; of bf16 ones
+//    two neighbouring keys are put into a word (one v_perm per pair).  (On the
+//    vector ALUs, with a broadcast of every weight, 8 rows took longer than
+//    their loads: 64 requests of up to 4096 tokens, 8 rows, 141 us.)
+//  * bf16 weights are rounded to bf16 for the product, like the output after it;
+//    their sum is of the unrounded ones.
 //  * exponentials are 2^x of scores in log2 units; the running maximum moves
 //    only when it is exceeded by 2^8, which spares the rescaling of the output.
+#include <float.h>
+
 #include <type_traits>
-#include <utility>
 
 #include "device_common.h"
 #include "plan.h"
@@ -35,20 +39,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr float kLowest = -1e30f;      // running maximum before any key
+constexpr float kLowest = -FLT_MAX;     // running maximum before any key
 constexpr float kRescaleLog2 = 8.f;
-
-// The value of lane L of each 16 lanes.
-template <int L>
-__device__ __forceinline__ float row_bcast(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + L, 0xf, 0xf, false));
-}
-
-// f(row) for every row, the row a constant.
-template <class F, int... I>
-__device__ __forceinline__ void each_row(F &&f, std::integer_sequence<int, I...>) {
-  (f(std::integral_constant<int, I>{}), ...);
-}
 
 struct DecodeUnit {
   int32_t r;        // request, or -1: no such unit
@@ -120,25 +112,19 @@ __device__ __forceinline__ DecodeUnit schedule(const PagedAttnArgs &a, int32_t u
   return found;
 }
 
-template <bool BF16, int D, int R, bool NT>
-__global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs a) {
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads, 3) void decode_attn_kernel(PagedAttnArgs a) {
   constexpr int T = BF16 ? 2 : 1;          // 16-key tiles (pages) per block of a wave
   constexpr int KB = T * 16;
-  constexpr int EPL = D / 16;              // columns of a lane
+  constexpr int EPL = D / 16;              // columns of a lane, tiles of O^T
   constexpr int ESZ = BF16 ? 2 : 4;
   constexpr int NK = D * ESZ / 64;         // 16-byte K loads per lane and tile
-  __shared__ float mo[kWaves][R][D];
-  __shared__ float mw[kWaves][R], lw[kWaves][R];
+  constexpr int LDO = D + 4;
+  __shared__ __align__(16) float mo[kWaves][kDecodeRows][LDO];
+  __shared__ float mw[kWaves][kDecodeRows], lw[kWaves][kDecodeRows];
 
-  // blocks of 8 neighbouring (unit, head) pairs, their row groups 8 ids apart:
-  // those read the same keys and run on one XCD
-  const int64_t id = blockIdx.x;
-  const int64_t octet = id / (8 * a.row_groups);
-  const int rg = (int)(id - octet * (8 * a.row_groups)) / 8;
-  const int64_t pair = octet * 8 + (id & 7);
-  const int32_t u = (int32_t)(pair / a.num_kv_heads);
-  const int g = (int)(pair - (int64_t)u * a.num_kv_heads);
-  if (u >= a.units_per_head) return;
+  const int32_t u = (int32_t)(blockIdx.x / a.num_kv_heads);
+  const int g = (int)(blockIdx.x - (int64_t)u * a.num_kv_heads);
   const DecodeUnit un = schedule(a, u);
   const int r = __builtin_amdgcn_readfirstlane(un.r);
   if (r < 0) return;
@@ -147,10 +133,10 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
   const int32_t per = __builtin_amdgcn_readfirstlane(un.per);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int quad = lane >> 4, j = lane & 15;
-  const int row0 = rg * R, rows = min(R, a.group - row0);
-  const int64_t out_row = (int64_t)r * a.num_q_heads + (int64_t)g * a.group + row0;
+  const int rows = a.group;
+  const int64_t out_row = (int64_t)r * a.num_q_heads + (int64_t)g * rows;
   // the request's units, for the join
-  if (a.ws_request && chunk == 0 && g == 0 && rg == 0 && tid == 0) {
+  if (a.ws_request && chunk == 0 && g == 0 && tid == 0) {
     a.ws_request[2 * r] = un.first;
     a.ws_request[2 * r + 1] = chunks;
   }
@@ -187,7 +173,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
   // query rows as the B operand: lane holds row j (none: zeros)
   u32x4 qf[NK];
   {
-    const char *qp = (const char *)a.q + ((int64_t)r * a.q_stride + ((int64_t)g * a.group + row0 + (j < rows ? j : 0)) * D) * ESZ;
+    const char *qp = (const char *)a.q + ((int64_t)r * a.q_stride + ((int64_t)g * rows + (j < rows ? j : 0)) * D) * ESZ;
 #pragma unroll
     for (int c = 0; c < NK; ++c) {
       u32x4 v = *(const u32x4 *)(qp + c * 64 + quad * 16);
@@ -203,14 +189,9 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
   bool have[T];                            // the tile's page exists (of the tiles in kr)
   bool have_v[T];
   auto page_of = [&](int i, int t) { return __builtin_amdgcn_readlane(pages, i * T + t - page_base); };
-  auto load16 = [&](const char *p) -> u32x4 {
-    if constexpr (NT) return __builtin_nontemporal_load((const u32x4 *)p);
-    else return *(const u32x4 *)p;
-  };
-  auto load8 = [&](const char *p) -> u32x2 {
-    if constexpr (NT) return __builtin_nontemporal_load((const u32x2 *)p);
-    else return *(const u32x2 *)p;
-  };
+  // (nothing reads them again: past the caches)
+  auto load16 = [&](const char *p) -> u32x4 { return __builtin_nontemporal_load((const u32x4 *)p); };
+  auto load8 = [&](const char *p) -> u32x2 { return __builtin_nontemporal_load((const u32x2 *)p); };
   // A missing page reads page 0 (its values are not used): no branch around the loads.
   auto load_k = [&](int i) {
 #pragma unroll
@@ -227,7 +208,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
     for (int t = 0; t < T; ++t) {
       const int32_t p = page_of(i, t);
       have_v[t] = p >= 0;
-      const char *base = (const char *)a.v_pages + max(p, 0) * page_bytes + head_bytes + (quad * 4) * D * ESZ + j * EPL * ESZ;
+      const char *base = (const char *)a.v_pages + max(p, 0) * page_bytes + head_bytes + (quad * 4) * D * ESZ + j * (BF16 ? EPL * 2 : 16);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if constexpr (NV == 2) {
@@ -236,7 +217,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
         } else {
 #pragma unroll
           for (int w = 0; w < NV; w += 4) {
-            const u32x4 x = load16(base + e * D * ESZ + w * 4);
+            const u32x4 x = load16(base + e * D * ESZ + (w / 4) * 256);
             vr[t][e][w] = x[0], vr[t][e][w + 1] = x[1], vr[t][e][w + 2] = x[2], vr[t][e][w + 3] = x[3];
           }
         }
@@ -244,21 +225,21 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
     }
   };
 
-  float o[R][EPL];
+  // O^T, row j of the queries: bf16: tile c, element i is column (4 quad + i) EPL + c;
+  // fp32: tile 4 h + k, element i is column 64 h + 16 quad + 4 i + k
+  f32x4 o[EPL];
 #pragma unroll
-  for (int i = 0; i < R; ++i)
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) o[i][e] = 0.f;
+  for (int c = 0; c < EPL; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = kLowest, l = 0.f;   // of row j: the reference in log2 units; this lane's part of the sum
 
   if (mine > 0) {
     load_k(0);
     load_v(0);
   }
-  for (int i = 0; i < mine; ++i) {
-    const int nxt = min(i + 1, mine - 1);
+  auto block = [&](int i, auto last) __attribute__((always_inline)) {
+    constexpr bool kMore = !decltype(last)::value;
     f32x4 s[T];
-    bool hk[T], hv[T];
+    bool hk[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -275,8 +256,10 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
         }
       }
     }
-    if ((nxt + 1) * T - page_base > 64) load_pages(nxt * T);
-    load_k(nxt);
+    if constexpr (kMore) {
+      if ((i + 2) * T - page_base > 64) load_pages((i + 1) * T);
+      load_k(i + 1);
+    }
     // s[t][e]: key 16 t + 4 quad + e of the block, row j
     const int32_t left = k1 - (k0 + (wave + i * kWaves) * KB);   // keys of the block and after
     float p[T][4];
@@ -298,13 +281,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
       const float al = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       l *= al;
-      auto scale_row = [&](auto row) {
-        constexpr int I = decltype(row)::value;
-        const float f = row_bcast<I>(al);
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) o[I][e] *= f;
-      };
-      each_row(scale_row, std::make_integer_sequence<int, R>{});
+      for (int c = 0; c < EPL; ++c) o[c] *= al;
     }
 #pragma unroll
     for (int t = 0; t < T; ++t)
@@ -313,51 +291,59 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
         p[t][e] = __builtin_amdgcn_exp2f(p[t][e] - m);
         l += p[t][e];
       }
+    // a slot past the run's keys may hold anything
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      hv[t] = have_v[t];
+    for (int t = 0; t < T; ++t)
+      if (edge || !have_v[t]) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        // a slot past the run's keys may hold anything
-        const bool use = hv[t] && (!edge || t * 16 + quad * 4 + e < left);
-        float v[EPL];
+        for (int e = 0; e < 4; ++e)
+          if (!have_v[t] || t * 16 + quad * 4 + e >= left)
 #pragma unroll
-        for (int w = 0; w < NV; ++w) {
-          const uint32_t x = use ? vr[t][e][w] : 0u;
-          if constexpr (BF16) {
-            v[2 * w] = __uint_as_float(x << 16);
-            v[2 * w + 1] = __uint_as_float(x & 0xffff0000u);
-          } else {
-            v[w] = __uint_as_float(x);
-          }
-        }
-        auto add_row = [&](auto row) {
-          constexpr int I = decltype(row)::value;
-          const float f = row_bcast<I>(p[t][e]);
-#pragma unroll
-          for (int c = 0; c < EPL; ++c) o[I][c] = __builtin_fmaf(f, v[c], o[I][c]);
-        };
-        each_row(add_row, std::make_integer_sequence<int, R>{});
+            for (int w = 0; w < NV; ++w) vr[t][e][w] = 0;
       }
+    if constexpr (BF16) {
+      const bf16x8 pb = __builtin_bit_cast(
+          bf16x8, u32x4{pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[T - 1][0], p[T - 1][1]),
+                        pack_bf16x2(p[T - 1][2], p[T - 1][3])});
+#pragma unroll
+      for (int w = 0; w < NV; ++w) {
+        u32x4 lo, hi;
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            lo[t * 2 + e / 2] = __builtin_amdgcn_perm(vr[t][e + 1][w], vr[t][e][w], 0x05040100u);
+            hi[t * 2 + e / 2] = __builtin_amdgcn_perm(vr[t][e + 1][w], vr[t][e][w], 0x07060302u);
+          }
+        o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pb, o[2 * w], 0, 0, 0);
+        o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pb, o[2 * w + 1], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int w = 0; w < NV; ++w)
+          o[w] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[0][e][w]), p[0][e], o[w], 0, 0, 0);
     }
-    load_v(nxt);
-  }
+    if constexpr (kMore) load_v(i + 1);
+  };
+  for (int i = 0; i < mine - 1; ++i) block(i, std::false_type{});
+  if (mine > 0) block(mine - 1, std::true_type{});
 
-  // the four groups of lanes, then the four waves
+  // the four waves
   l = sum_over_lane_rows(l);
 #pragma unroll
-  for (int i = 0; i < R; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) {
-      const float x = sum_over_lane_rows(o[i][e]);
-      if (quad == (i & 3)) mo[wave][i][j * EPL + e] = x;
-    }
-  if (quad == 0 && j < R) {
+    for (int c = 0; c < EPL; c += 4)
+      *(f32x4 *)&mo[wave][j][BF16 ? (4 * quad + i) * EPL + c : c * 16 + 16 * quad + 4 * i] =
+          f32x4{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
+  if (quad == 0) {
     mw[wave][j] = m;
     lw[wave][j] = l;
   }
   __syncthreads();
-  const int64_t slot = ((int64_t)u * a.num_kv_heads + g) * a.row_groups + rg;
+  const int64_t slot = ((int64_t)u * a.num_kv_heads + g) * rows;   // the unit's first row of the workspace
   for (int it = tid; it < rows * D; it += kThreads) {
     const int i = it / D, c = it % D;
     float mm = mw[0][i];
@@ -371,12 +357,12 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
       num = __builtin_fmaf(f, mo[w][i][c], num);
     }
     if (chunks == 1) {
-      const float x = den != 0.f ? num / den : 0.f;
+      const float x = num / den;
       if (BF16) ((__bf16 *)a.out)[out_row * D + it] = (__bf16)x;
       else ((float *)a.out)[out_row * D + it] = x;
     } else {
-      a.ws_o[(slot * kDecodeRows + i) * D + c] = num;
-      if (c == 0) *(f32x2 *)(a.ws_ml + (slot * kDecodeRows + i) * 2) = f32x2{mm, den};
+      a.ws_o[(slot + i) * D + c] = num;
+      if (c == 0) *(f32x2 *)(a.ws_ml + (slot + i) * 2) = f32x2{mm, den};
     }
   }
 }
@@ -393,12 +379,10 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(PagedAttnArgs a) 
   const int32_t chunks = a.ws_request[2 * r + 1];
   if (chunks <= 1) return;
   const int32_t first = a.ws_request[2 * r];
-  const int g = h / a.group, in = h - g * a.group, rows_per = a.rows_per_group;
-  const int rg = in / rows_per, i = in - rg * rows_per;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float m = kLowest, l = 0.f, o[EPL] = {};
   for (int c = wave; c < chunks; c += kWaves) {
-    const int64_t slot = (((int64_t)(first + c) * a.num_kv_heads + g) * a.row_groups + rg) * kDecodeRows + i;
+    const int64_t slot = (int64_t)(first + c) * a.num_q_heads + h;
     const f32x2 ml = *(const f32x2 *)(a.ws_ml + slot * 2);
     float x[EPL];
 #pragma unroll
@@ -426,20 +410,16 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(PagedAttnArgs a) 
     den = __builtin_fmaf(f, sl[w], den);
     num = __builtin_fmaf(f, so[w][c], num);
   }
-  const float x = den != 0.f ? num / den : 0.f;
+  const float x = num / den;
   if (BF16) ((__bf16 *)a.out)[row * D + c] = (__bf16)x;
   else ((float *)a.out)[row * D + c] = x;
 }
 
-template <bool BF16, int D, int R>
+template <bool BF16, int D>
 hipError_t launch(const PagedAttnArgs &a, hipStream_t stream) {
-  const int64_t pairs = (int64_t)a.units_per_head * a.num_kv_heads;
-  const int64_t blocks = (pairs + 7) / 8 * 8 * a.row_groups;
+  const int64_t blocks = (int64_t)a.units_per_head * a.num_kv_heads;
   if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
-  if (a.row_groups == 1)
-    hipLaunchKernelGGL((decode_attn_kernel<BF16, D, R, true>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((decode_attn_kernel<BF16, D, R, false>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((decode_attn_kernel<BF16, D>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.ws_request) return e;
   hipLaunchKernelGGL((decode_join_kernel<BF16, D>), dim3((unsigned)((int64_t)a.num_requests * a.num_q_heads)),
@@ -447,21 +427,11 @@ hipError_t launch(const PagedAttnArgs &a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <bool BF16, int D>
-hipError_t launch_rows(const PagedAttnArgs &a, hipStream_t stream) {
-  switch (a.rows_per_group) {
-    case 1: return launch<BF16, D, 1>(a, stream);
-    case 2: return launch<BF16, D, 2>(a, stream);
-    case 4: return launch<BF16, D, 4>(a, stream);
-    default: return launch<BF16, D, 8>(a, stream);
-  }
-}
-
 }  // namespace
 
 hipError_t launch_decode_attn(const PagedAttnArgs &a, int head_dim, bool bf16, hipStream_t stream) {
-  if (bf16) return head_dim == 128 ? launch_rows<true, 128>(a, stream) : launch_rows<true, 64>(a, stream);
-  return head_dim == 128 ? launch_rows<false, 128>(a, stream) : launch_rows<false, 64>(a, stream);
+  if (bf16) return head_dim == 128 ? launch<true, 128>(a, stream) : launch<true, 64>(a, stream);
+  return head_dim == 128 ? launch<false, 128>(a, stream) : launch<false, 64>(a, stream);
 }
 
 }  // namespace adaserve

@@ -446,8 +446,6 @@ int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_
   a.num_kv_heads = num_kv_heads;
   a.group = num_q_heads / num_kv_heads;
   a.max_context = max_context;
-  a.rows_per_group = plan.rows_per_group;
-  a.row_groups = plan.row_groups;
   a.units_per_head = plan.units_per_head;
   a.target = plan.target;
   a.min_blocks = kDecodeMinBlocks;

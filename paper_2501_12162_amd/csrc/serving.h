@@ -82,14 +82,12 @@ struct PagedAttnArgs {
   // decode attention (DecodePlan); prompt attention with split keys: sums and
   // references of [units, kPromptTileRows] rows in ws_o and ws_ml
   int32_t max_context;
-  int32_t rows_per_group;
-  int32_t row_groups;
   int32_t units_per_head;
   int32_t target;
   int32_t min_blocks;
   int32_t *ws_request;           // [B, 2] first unit, units; null: nothing is split
-  float *ws_ml;                  // [units, heads, row groups, kDecodeRows, 2] reference, sum
-  float *ws_o;                   // [units, heads, row groups, kDecodeRows, D] weighted sums of V
+  float *ws_ml;                  // [units, Hq, 2] reference, sum
+  float *ws_o;                   // [units, Hq, D] weighted sums of V
 };
 
 // (apart, since the launches of decode attention need not carry its 2.5 KB)
@@ -97,19 +95,17 @@ struct PromptAttnArgs : PagedAttnArgs {
   PromptEntry table[kPromptTable];
 };
 
-// Decode attention's work, from sizes alone.  Query heads that share a kv-head
-// go in groups of 1, 2, 4 or 8 rows (a group of 8 reads the keys once for all;
-// more than 8 read them once per 8, the second time out of L2).  Per kv-head
-// and row group the batch's 32-key blocks are cut into about `target` runs of
-// at least kDecodeMinBlocks: a batch that fills the device with whole requests
-// (or that has more of them than the workgroups' scan takes) is not cut.
-constexpr int kDecodeRows = 8;
+// Decode attention's work, from sizes alone.  Per kv-head the batch's 32-key
+// blocks are cut into about `target` runs of at least kDecodeMinBlocks: a batch
+// that fills the device with whole requests (or that has more of them than the
+// workgroups' scan takes) is not cut.
+constexpr int kDecodeRows = 16;              // most query heads per kv-head: the columns of a matrix tile
 constexpr int kDecodeMinBlocks = 4;          // one block per wave
-constexpr int kDecodeUnits = 1024;           // on the device: two rounds of two workgroups per CU
+constexpr int kDecodeUnits = 1024;           // on the device
 constexpr int kDecodeSplitRequests = 1024;
 
 struct DecodePlan {
-  int32_t rows_per_group, row_groups, units_per_head, target;
+  int32_t units_per_head, target;
   bool split;
   int64_t ml_offset, o_offset;
   size_t ws_bytes;
@@ -117,11 +113,7 @@ struct DecodePlan {
 
 inline DecodePlan decode_plan(int32_t B, int32_t hq, int32_t hkv, int32_t head_dim, int32_t max_context) {
   DecodePlan p{};
-  const int32_t group = hq / hkv;
-  p.rows_per_group = group > 4 ? 8 : group > 2 ? 4 : group;
-  p.row_groups = (group + p.rows_per_group - 1) / p.rows_per_group;
-  const int64_t heads = (int64_t)hkv * p.row_groups;
-  p.target = (int32_t)((kDecodeUnits + heads - 1) / heads);
+  p.target = (kDecodeUnits + hkv - 1) / hkv;
   const int64_t blocks = (max_context + 31) / 32;
   const int64_t most = (blocks + kDecodeMinBlocks - 1) / kDecodeMinBlocks;   // runs of one request
   int64_t units = (int64_t)p.target + B;
@@ -129,7 +121,7 @@ inline DecodePlan decode_plan(int32_t B, int32_t hq, int32_t hkv, int32_t head_d
   p.split = most > 1 && B <= kDecodeSplitRequests && B < p.target * 4 && units > B;
   p.units_per_head = (int32_t)(p.split ? units : B);
   if (p.split) {
-    const size_t slots = (size_t)(units * heads) * kDecodeRows;
+    const size_t slots = (size_t)units * hq;
     p.ml_offset = ((int64_t)B * 8 + 255) / 256 * 256;
     p.o_offset = p.ml_offset + (int64_t)((slots * 8 + 255) / 256 * 256);
     p.ws_bytes = (size_t)p.o_offset + slots * head_dim * 4;
