@@ -1,11 +1,12 @@
 // Attention of one new token per request over its paged cache on gfx950.
 //
-// A unit of work is (request, kv-head, a run of 32-key blocks), with all query
-// heads of the kv-head as its rows; the requests' caches are cut into runs so
-// that the batch fills the device whatever its lengths, and the runs of one
-// request are joined by a second launch.  The lengths are read on the device
-// only: every workgroup finds its unit from all of them (schedule()), so a
-// captured launch follows them.
+// The batch's 32-key blocks, request after request, are dealt in equal and
+// contiguous shares to as many workgroups per kv-head as the device holds, so
+// that all end together whatever the lengths; a workgroup goes from request to
+// request, with all query heads of its kv-head as rows, and the runs of a request
+// that lies in several shares are joined by a second launch.  The lengths are
+// read on the device only: every workgroup finds its share from all of them
+// (schedule()), so a captured launch follows them.
 //
 // Bound by memory: 2 c Hkv D s bytes per request against 4 c Hq D flops.  So
 // everything serves to keep loads in flight: no LDS in the loop and no
@@ -19,12 +20,20 @@
 //    loads D / 16 columns of those keys' values, and tile c of O^T is column c
 //    of each lane's.  fp32 values are operands as they are loaded; of bf16 ones
 //    two neighbouring keys are put into a word (one v_perm per pair).  (On the
-//    vector ALUs, with a broadcast of every weight, 8 rows took longer than
-//    their loads: 64 requests of up to 4096 tokens, 8 rows, 141 us.)
+//    vector ALUs, with a broadcast of every weight, 8 rows took as long as their
+//    loads.)
 //  * bf16 weights are rounded to bf16 for the product, like the output after it;
 //    their sum is of the unrounded ones.
 //  * exponentials are 2^x of scores in log2 units; the running maximum moves
 //    only when it is exceeded by 2^8, which spares the rescaling of the output.
+//
+// Measured, bf16, D = 128 (a kernel that only reads gets 7.0 TB/s): 64 requests
+// of up to 4096 tokens, 64 on 8 heads, 668 MB: 110 us, 6.0 TB/s; 8 requests of
+// 32768 tokens, 32 on 8 heads, 1074 MB: 163 us, 6.6 TB/s; one of 1500 tokens: 7.5
+// us and 3.4 for the join.  With a unit per run of a request, two rounds of them,
+// the first two took 124 and 169 us; with three workgroups per CU (168 registers,
+// 8 of them spilled) 130 and 185.  Loading a run's first block before the end of
+// the run before gains nothing: 111 and 166.
 #include <float.h>
 
 #include <type_traits>
@@ -42,55 +51,37 @@ constexpr int kWaves = kThreads / 64;
 constexpr float kLowest = -FLT_MAX;     // running maximum before any key
 constexpr float kRescaleLog2 = 8.f;
 
+// The batch's 32-key blocks in one line, request after request; unit u takes
+// blocks [lo, hi) of it.
 struct DecodeUnit {
-  int32_t r;        // request, or -1: no such unit
-  int32_t len;      // its length (-1: out of range)
-  int32_t chunk;    // run of blocks
-  int32_t chunks;   // runs of the request
-  int32_t per;      // blocks per run
-  int32_t first;    // the request's first unit
+  int32_t lo, hi;
+  int32_t first;    // first request with a block in it, or an empty one that it owns
+  int32_t per;      // blocks per unit
+  bool last;        // of the units with work: it owns the empty requests at the end
 };
 
-__device__ __forceinline__ int32_t decode_blocks(int32_t len) { return (len + kKeysPerBlock - 1) / kKeysPerBlock; }
+__device__ __forceinline__ int32_t decode_blocks(int32_t len) { return len > 0 ? (len + kKeysPerBlock - 1) / kKeysPerBlock : 0; }
 
-// Unit u of the batch.  The batch's blocks are dealt into `target` equal runs,
-// none shorter than min_blocks; a request takes as many as cover it, and one
-// if it is empty.  Each thread takes 1 to 4 neighbouring requests (at most
-// kDecodeSplitRequests in all); every thread ends with the same answer.
-__device__ __forceinline__ DecodeUnit schedule(const PagedAttnArgs &a, int32_t u) {
-  __shared__ int32_t part[2][kWaves];
-  __shared__ DecodeUnit found;
+// Unit u, from all lengths: every unit has `per` blocks but for the last one.
+// Each thread takes 1 to 4 neighbouring requests (at most kDecodeSplitRequests
+// in all); start[] gets each request's first block, len[] its length (-1: out of
+// range).  False: no such unit.
+__device__ __forceinline__ bool schedule(const PagedAttnArgs &a, int32_t u, int32_t *start, int32_t *len, DecodeUnit &un) {
+  __shared__ int32_t part[kWaves];
+  __shared__ int32_t first;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  DecodeUnit d;
-  auto valid = [&](int32_t len) { return len >= 0 && len <= a.max_context ? len : -1; };
-  if (a.units_per_head == a.num_requests) {   // nothing is split
-    d = {u < a.num_requests ? u : -1, 0, 0, 1, 1 << 20, u};
-    if (d.r >= 0) d.len = valid(a.context_len[d.r]);
-    return d;
-  }
   const int per_thread = (a.num_requests + kThreads - 1) / kThreads;
-  int32_t len[4], nb[4], blocks = 0;
+  int32_t nb[4], mine = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = tid * per_thread + i;
-    len[i] = i < per_thread && r < a.num_requests ? valid(a.context_len[r]) : -2;
-    nb[i] = len[i] > 0 ? decode_blocks(len[i]) : 0;
-    blocks += nb[i];
-  }
-  // sum over the workgroup, then the scan of the runs
-  int32_t sum = blocks;
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
-  if (lane == 0) part[0][wave] = sum;
-  if (tid == 0) found.r = -1;
-  __syncthreads();
-  const int32_t total = part[0][0] + part[0][1] + part[0][2] + part[0][3];
-  const int32_t per = max(a.min_blocks, (total + a.target - 1) / a.target);
-  int32_t chunks[4], mine = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    chunks[i] = len[i] == -2 ? 0 : max(1, (nb[i] + per - 1) / per);
-    mine += chunks[i];
+    nb[i] = 0;
+    if (i < per_thread && r < a.num_requests) {
+      const int32_t x = a.context_len[r], ok = x >= 0 && x <= a.max_context ? x : -1;
+      len[r] = ok;
+      nb[i] = decode_blocks(ok);
+    }
+    mine += nb[i];
   }
   int32_t upto = mine;
 #pragma unroll
@@ -98,22 +89,57 @@ __device__ __forceinline__ DecodeUnit schedule(const PagedAttnArgs &a, int32_t u
     const int32_t o = __shfl_up(upto, off, 64);
     if (lane >= off) upto += o;
   }
-  if (lane == 63) part[1][wave] = upto;
+  if (lane == 63) part[wave] = upto;
   __syncthreads();
-  for (int w = 0; w < wave; ++w) upto += part[1][w];
-  int32_t before = upto - mine;
+  int32_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) upto += part[w];
+    total += part[w];
+  }
+  un.per = max(a.min_blocks, (total + a.units_per_head - 1) / a.units_per_head);
+  const int32_t units = max(1, (total + un.per - 1) / un.per);
+  if (u >= units) return false;
+  un.lo = u * un.per;
+  un.hi = min(total, un.lo + un.per);
+  un.last = u == units - 1;
+  int32_t at = upto - mine;
+  // `first`: the one request that is the unit's where the one before is not.  A
+  // request with blocks is if it ends behind lo, an empty one from lo on.
+  auto is_in = [&](int32_t from, int32_t n) { return n > 0 ? from + n > un.lo : from >= un.lo; };
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (u >= before && u < before + chunks[i])
-      found = {tid * per_thread + i, len[i], u - before, chunks[i], per, before};
-    before += chunks[i];
+    const int r = tid * per_thread + i;
+    if (i < per_thread && r < a.num_requests) {
+      start[r] = at;
+      if (is_in(at, nb[i])) {
+        // (the request before: its blocks end at `at`)
+        bool before = false;
+        if (i > 0) before = is_in(at - nb[i - 1], nb[i - 1]);
+        else if (r > 0) {
+          const int32_t x = a.context_len[r - 1], n = decode_blocks(x <= a.max_context ? x : -1);
+          before = is_in(at - n, n);
+        }
+        if (!before) first = r;
+      }
+      at += nb[i];
+    }
   }
   __syncthreads();
-  return found;
+  un.first = __builtin_amdgcn_readfirstlane(first);
+  return true;
 }
 
+// A run of a request's keys.
+struct Run {
+  int32_t r;
+  int32_t k0, k1;     // its keys
+  int32_t nb, mine;   // blocks of the wave's size; this wave's: wave, wave + 4, ...
+  int32_t slot;       // of the workspace: 2 u + 1 where it begins a request, 2 u where it goes on with one; -1: all of it
+};
+
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, 3) void decode_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs a) {
   constexpr int T = BF16 ? 2 : 1;          // 16-key tiles (pages) per block of a wave
   constexpr int KB = T * 16;
   constexpr int EPL = D / 16;              // columns of a lane, tiles of O^T
@@ -123,63 +149,85 @@ __global__ __launch_bounds__(kThreads, 3) void decode_attn_kernel(PagedAttnArgs 
   __shared__ __align__(16) float mo[kWaves][kDecodeRows][LDO];
   __shared__ float mw[kWaves][kDecodeRows], lw[kWaves][kDecodeRows];
 
+  __shared__ int32_t start[kDecodeSplitRequests], lens[kDecodeSplitRequests];
   const int32_t u = (int32_t)(blockIdx.x / a.num_kv_heads);
   const int g = (int)(blockIdx.x - (int64_t)u * a.num_kv_heads);
-  const DecodeUnit un = schedule(a, u);
-  const int r = __builtin_amdgcn_readfirstlane(un.r);
-  if (r < 0) return;
-  const int32_t len = __builtin_amdgcn_readfirstlane(un.len);
-  const int32_t chunk = __builtin_amdgcn_readfirstlane(un.chunk), chunks = __builtin_amdgcn_readfirstlane(un.chunks);
-  const int32_t per = __builtin_amdgcn_readfirstlane(un.per);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int quad = lane >> 4, j = lane & 15;
   const int rows = a.group;
-  const int64_t out_row = (int64_t)r * a.num_q_heads + (int64_t)g * rows;
-  // the request's units, for the join
-  if (a.ws_request && chunk == 0 && g == 0 && tid == 0) {
-    a.ws_request[2 * r] = un.first;
-    a.ws_request[2 * r + 1] = chunks;
-  }
-  if (len <= 0) {   // empty: zeros; out of range: NaN
-    const float x = len < 0 ? __builtin_nanf("") : 0.f;
-    for (int i = tid; i < rows * D; i += kThreads) {
-      if (BF16) ((__bf16 *)a.out)[out_row * D + i] = (__bf16)x;
-      else ((float *)a.out)[out_row * D + i] = x;
+  const bool split = a.ws_request != nullptr;
+  DecodeUnit un{0, INT32_MAX, u, 0, false};
+  if (split && !schedule(a, u, start, lens, un)) return;
+
+  // The unit's run of request r or of the first one after it that has keys
+  // there; the rows of the empty requests on the way become zeros, of lengths
+  // out of range NaN.  False: no more.
+  auto find_run = [&](int32_t r, Run &run) {
+    for (; r < (split ? a.num_requests : u + 1); ++r) {
+      int32_t len, from = 0;
+      if (split) {
+        from = __builtin_amdgcn_readfirstlane(start[r]);
+        len = __builtin_amdgcn_readfirstlane(lens[r]);
+        if (from >= un.hi && !un.last) return false;
+      } else {
+        len = a.context_len[r];
+        if (len > a.max_context) len = -1;
+      }
+      if (len <= 0) {
+        const float x = len < 0 ? __builtin_nanf("") : 0.f;
+        const int64_t at = ((int64_t)r * a.num_q_heads + (int64_t)g * rows) * D;
+        for (int i = tid; i < rows * D; i += kThreads) {
+          if (BF16) ((__bf16 *)a.out)[at + i] = (__bf16)x;
+          else ((float *)a.out)[at + i] = x;
+        }
+        continue;
+      }
+      const int32_t end = from + decode_blocks(len);
+      const int32_t b0 = max(from, un.lo), b1 = min(end, un.hi);
+      run.r = r;
+      run.k0 = (b0 - from) * kKeysPerBlock;
+      run.k1 = min(len, (b1 - from) * kKeysPerBlock);
+      run.nb = (run.k1 - run.k0 + KB - 1) / KB;
+      run.mine = run.nb > wave ? (run.nb - wave + kWaves - 1) / kWaves : 0;
+      run.slot = b0 > from ? 2 * u : b1 < end ? 2 * u + 1 : -1;
+      // the request's units, for the join
+      if (split && b0 == from && g == 0 && tid == 0) {
+        a.ws_request[2 * r] = u;
+        a.ws_request[2 * r + 1] = (end - 1) / un.per - u + 1;
+      }
+      return true;
     }
-    return;
-  }
-  // keys of the run, in blocks of KB; this wave takes blocks wave, wave + 4, ...
-  const int32_t k0 = chunk * per * kKeysPerBlock;
-  const int32_t k1 = min(len, k0 + per * kKeysPerBlock);
-  const int32_t nb = k1 > k0 ? (k1 - k0 + KB - 1) / KB : 0;
-  const int32_t mine = nb > wave ? (nb - wave + kWaves - 1) / kWaves : 0;
+    return false;
+  };
+  Run run, next;
+  if (!find_run(un.first, run)) return;
 
   // page ids: lane i holds that of tile i of this wave's blocks, 64 tiles at a time
-  int32_t pages = -1, page_base = 0;
-  auto load_pages = [&](int base) {
+  int32_t pages, page_base = 0;
+  auto page_ids = [&](const Run &w, int base) -> int32_t {
     const int i = base + lane;                       // tile of the wave
     const int32_t b = wave + (i / T) * kWaves;
-    const int32_t e = (k0 + b * KB) / kPageSize + i % T;
+    const int32_t e = (w.k0 + b * KB) / kPageSize + i % T;
     int32_t p = -1;
-    if (b < nb && e < a.bt_stride && e * kPageSize < k1) {
-      p = a.block_table[(int64_t)r * a.bt_stride + e];
+    if (b < w.nb && e < a.bt_stride && e * kPageSize < w.k1) {
+      p = a.block_table[(int64_t)w.r * a.bt_stride + e];
       if (p < 0 || p >= a.num_pages) p = -1;
     }
-    pages = p;
-    page_base = base;
+    return p;
   };
-  load_pages(0);
+  pages = page_ids(run, 0);
 
   // query rows as the B operand: lane holds row j (none: zeros)
   u32x4 qf[NK];
-  {
+  auto load_q = [&](int32_t r) {
     const char *qp = (const char *)a.q + ((int64_t)r * a.q_stride + ((int64_t)g * rows + (j < rows ? j : 0)) * D) * ESZ;
 #pragma unroll
     for (int c = 0; c < NK; ++c) {
       u32x4 v = *(const u32x4 *)(qp + c * 64 + quad * 16);
       qf[c] = j < rows ? v : u32x4{0, 0, 0, 0};
     }
-  }
+  };
+  load_q(run.r);
 
   const int64_t page_bytes = (int64_t)a.num_kv_heads * kPageSize * D * ESZ;
   const int64_t head_bytes = (int64_t)g * kPageSize * D * ESZ;
@@ -228,14 +276,7 @@ __global__ __launch_bounds__(kThreads, 3) void decode_attn_kernel(PagedAttnArgs 
   // O^T, row j of the queries: bf16: tile c, element i is column (4 quad + i) EPL + c;
   // fp32: tile 4 h + k, element i is column 64 h + 16 quad + 4 i + k
   f32x4 o[EPL];
-#pragma unroll
-  for (int c = 0; c < EPL; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = kLowest, l = 0.f;   // of row j: the reference in log2 units; this lane's part of the sum
-
-  if (mine > 0) {
-    load_k(0);
-    load_v(0);
-  }
+  float m, l;   // of row j: the reference in log2 units; this lane's part of the sum
   auto block = [&](int i, auto last) __attribute__((always_inline)) {
     constexpr bool kMore = !decltype(last)::value;
     f32x4 s[T];
@@ -257,11 +298,14 @@ __global__ __launch_bounds__(kThreads, 3) void decode_attn_kernel(PagedAttnArgs 
       }
     }
     if constexpr (kMore) {
-      if ((i + 2) * T - page_base > 64) load_pages((i + 1) * T);
+      if ((i + 2) * T - page_base > 64) {
+        page_base = (i + 1) * T;
+        pages = page_ids(run, page_base);
+      }
       load_k(i + 1);
     }
     // s[t][e]: key 16 t + 4 quad + e of the block, row j
-    const int32_t left = k1 - (k0 + (wave + i * kWaves) * KB);   // keys of the block and after
+    const int32_t left = run.k1 - (run.k0 + (wave + i * kWaves) * KB);   // keys of the block and after
     float p[T][4];
     float bm = kLowest;
     const bool edge = left < KB;
@@ -327,43 +371,68 @@ __global__ __launch_bounds__(kThreads, 3) void decode_attn_kernel(PagedAttnArgs 
     }
     if constexpr (kMore) load_v(i + 1);
   };
-  for (int i = 0; i < mine - 1; ++i) block(i, std::false_type{});
-  if (mine > 0) block(mine - 1, std::true_type{});
 
-  // the four waves
-  l = sum_over_lane_rows(l);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int c = 0; c < EPL; c += 4)
-      *(f32x4 *)&mo[wave][j][BF16 ? (4 * quad + i) * EPL + c : c * 16 + 16 * quad + 4 * i] =
-          f32x4{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
-  if (quad == 0) {
-    mw[wave][j] = m;
-    lw[wave][j] = l;
-  }
-  __syncthreads();
-  const int64_t slot = ((int64_t)u * a.num_kv_heads + g) * rows;   // the unit's first row of the workspace
-  for (int it = tid; it < rows * D; it += kThreads) {
-    const int i = it / D, c = it % D;
-    float mm = mw[0][i];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, mw[w][i]);
-    float den = 0.f, num = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(mw[w][i] - mm);
-      den = __builtin_fmaf(f, lw[w][i], den);
-      num = __builtin_fmaf(f, mo[w][i][c], num);
+#pragma unroll 1
+  for (;;) {
+    if (run.mine > 0) {
+      load_k(0);
+      load_v(0);
     }
-    if (chunks == 1) {
-      const float x = num / den;
-      if (BF16) ((__bf16 *)a.out)[out_row * D + it] = (__bf16)x;
-      else ((float *)a.out)[out_row * D + it] = x;
-    } else {
-      a.ws_o[(slot + i) * D + c] = num;
-      if (c == 0) *(f32x2 *)(a.ws_ml + (slot + i) * 2) = f32x2{mm, den};
+    // the next run and its page ids, before they are used
+    const bool more = split && find_run(run.r + 1, next);
+    int32_t next_pages = -1;
+    if (more) next_pages = page_ids(next, 0);
+    m = kLowest;
+    l = 0.f;
+#pragma unroll
+    for (int c = 0; c < EPL; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int i = 0; i < run.mine - 1; ++i) block(i, std::false_type{});
+    if (run.mine > 0) block(run.mine - 1, std::true_type{});
+
+    // the four waves
+    l = sum_over_lane_rows(l);
+    __syncthreads();   // (the run before is read)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < EPL; c += 4)
+        *(f32x4 *)&mo[wave][j][BF16 ? (4 * quad + i) * EPL + c : c * 16 + 16 * quad + 4 * i] =
+            f32x4{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
+    if (quad == 0) {
+      mw[wave][j] = m;
+      lw[wave][j] = l;
     }
+    __syncthreads();
+    const int64_t out_row = (int64_t)run.r * a.num_q_heads + (int64_t)g * rows;
+    const int64_t slot = (int64_t)run.slot * a.num_q_heads + (int64_t)g * rows;
+#pragma unroll 1
+    for (int it = tid; it < rows * D; it += kThreads) {
+      const int i = it / D, c = it % D;
+      float mm = mw[0][i];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, mw[w][i]);
+      float den = 0.f, num = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(mw[w][i] - mm);
+        den = __builtin_fmaf(f, lw[w][i], den);
+        num = __builtin_fmaf(f, mo[w][i][c], num);
+      }
+      if (run.slot < 0) {
+        const float x = num / den;
+        if (BF16) ((__bf16 *)a.out)[out_row * D + it] = (__bf16)x;
+        else ((float *)a.out)[out_row * D + it] = x;
+      } else {
+        a.ws_o[(slot + i) * D + c] = num;
+        if (c == 0) *(f32x2 *)(a.ws_ml + (slot + i) * 2) = f32x2{mm, den};
+      }
+    }
+    if (!more) return;
+    run = next;
+    pages = next_pages;
+    page_base = 0;
+    load_q(run.r);
   }
 }
 
@@ -376,13 +445,14 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(PagedAttnArgs a) 
   __shared__ float so[kWaves][D], sm[kWaves], sl[kWaves];
   const int64_t row = blockIdx.x;
   const int r = (int)(row / a.num_q_heads), h = (int)(row - (int64_t)r * a.num_q_heads);
-  const int32_t chunks = a.ws_request[2 * r + 1];
+  const int32_t len = a.context_len[r];
+  if (len <= 0 || len > a.max_context) return;
+  const int32_t first = a.ws_request[2 * r], chunks = a.ws_request[2 * r + 1];
   if (chunks <= 1) return;
-  const int32_t first = a.ws_request[2 * r];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float m = kLowest, l = 0.f, o[EPL] = {};
   for (int c = wave; c < chunks; c += kWaves) {
-    const int64_t slot = (int64_t)(first + c) * a.num_q_heads + h;
+    const int64_t slot = (int64_t)(2 * (first + c) + (c == 0)) * a.num_q_heads + h;
     const f32x2 ml = *(const f32x2 *)(a.ws_ml + slot * 2);
     float x[EPL];
 #pragma unroll

@@ -447,7 +447,6 @@ int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_
   a.group = num_q_heads / num_kv_heads;
   a.max_context = max_context;
   a.units_per_head = plan.units_per_head;
-  a.target = plan.target;
   a.min_blocks = kDecodeMinBlocks;
   if (plan.split) {
     a.ws_request = (int32_t *)workspace;

@@ -83,11 +83,10 @@ struct PagedAttnArgs {
   // references of [units, kPromptTileRows] rows in ws_o and ws_ml
   int32_t max_context;
   int32_t units_per_head;
-  int32_t target;
   int32_t min_blocks;
-  int32_t *ws_request;           // [B, 2] first unit, units; null: nothing is split
-  float *ws_ml;                  // [units, Hq, 2] reference, sum
-  float *ws_o;                   // [units, Hq, D] weighted sums of V
+  int32_t *ws_request;           // [B, 2] first unit, units; null: a unit is a request
+  float *ws_ml;                  // [units, 2, Hq, 2] reference, sum
+  float *ws_o;                   // [units, 2, Hq, D] weighted sums of V
 };
 
 // (apart, since the launches of decode attention need not carry its 2.5 KB)
@@ -96,16 +95,18 @@ struct PromptAttnArgs : PagedAttnArgs {
 };
 
 // Decode attention's work, from sizes alone.  Per kv-head the batch's 32-key
-// blocks are cut into about `target` runs of at least kDecodeMinBlocks: a batch
-// that fills the device with whole requests (or that has more of them than the
-// workgroups' scan takes) is not cut.
+// blocks are dealt in equal, contiguous shares to as many units as the device
+// holds at a time, so that all end together whatever the lengths; a unit goes
+// from request to request, and a request in several units is joined by a second
+// launch.  Requests of one short run each, and more of them than the scan takes,
+// are units themselves.
 constexpr int kDecodeRows = 16;              // most query heads per kv-head: the columns of a matrix tile
 constexpr int kDecodeMinBlocks = 4;          // one block per wave
-constexpr int kDecodeUnits = 1024;           // on the device
+constexpr int kDecodeUnits = 512;            // on the device: two workgroups per CU
 constexpr int kDecodeSplitRequests = 1024;
 
 struct DecodePlan {
-  int32_t units_per_head, target;
+  int32_t units_per_head;
   bool split;
   int64_t ml_offset, o_offset;
   size_t ws_bytes;
@@ -113,15 +114,16 @@ struct DecodePlan {
 
 inline DecodePlan decode_plan(int32_t B, int32_t hq, int32_t hkv, int32_t head_dim, int32_t max_context) {
   DecodePlan p{};
-  p.target = (kDecodeUnits + hkv - 1) / hkv;
   const int64_t blocks = (max_context + 31) / 32;
-  const int64_t most = (blocks + kDecodeMinBlocks - 1) / kDecodeMinBlocks;   // runs of one request
-  int64_t units = (int64_t)p.target + B;
-  if (units > B * most) units = B * most;
-  p.split = most > 1 && B <= kDecodeSplitRequests && B < p.target * 4 && units > B;
-  p.units_per_head = (int32_t)(p.split ? units : B);
+  p.split = blocks > kDecodeMinBlocks && B <= kDecodeSplitRequests;
+  p.units_per_head = B;
   if (p.split) {
-    const size_t slots = (size_t)units * hq;
+    int64_t units = kDecodeUnits / hkv;
+    const int64_t most = (B * blocks + kDecodeMinBlocks - 1) / kDecodeMinBlocks;
+    if (units > most) units = most;
+    if (units < 1) units = 1;
+    p.units_per_head = (int32_t)units;
+    const size_t slots = (size_t)units * 2 * hq;
     p.ml_offset = ((int64_t)B * 8 + 255) / 256 * 256;
     p.o_offset = p.ml_offset + (int64_t)((slots * 8 + 255) / 256 * 256);
     p.ws_bytes = (size_t)p.o_offset + slots * head_dim * 4;
