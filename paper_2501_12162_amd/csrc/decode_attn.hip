@@ -22,8 +22,10 @@
 //    two neighbouring keys are put into a word (one v_perm per pair).  (On the
 //    vector ALUs, with a broadcast of every weight, 8 rows took as long as their
 //    loads.)
-//  * bf16 weights are rounded to bf16 for the product, like the output after it;
-//    their sum is of the unrounded ones.
+//  * for bf16 values a weight goes into the product as the sum of two bf16 parts,
+//    which holds 16 bits of it: the matrix cores wait for memory anyway (with the
+//    first part alone the times are the same and the error against fp64 0.0021
+//    instead of the output rounding's 0.0017).
 //  * exponentials are 2^x of scores in log2 units; the running maximum moves
 //    only when it is exceeded by 2^8, which spares the rescaling of the output.
 //
@@ -346,9 +348,17 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
             for (int w = 0; w < NV; ++w) vr[t][e][w] = 0;
       }
     if constexpr (BF16) {
-      const bf16x8 pb = __builtin_bit_cast(
-          bf16x8, u32x4{pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[T - 1][0], p[T - 1][1]),
-                        pack_bf16x2(p[T - 1][2], p[T - 1][3])});
+      // weights as the sum of two bf16 parts
+      u32x4 w0, w1;
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          const uint32_t x = pack_bf16x2(p[t][e], p[t][e + 1]);
+          w0[t * 2 + e / 2] = x;
+          w1[t * 2 + e / 2] = pack_bf16x2(p[t][e] - __uint_as_float(x << 16), p[t][e + 1] - __uint_as_float(x & 0xffff0000u));
+        }
+      const bf16x8 p0 = __builtin_bit_cast(bf16x8, w0), p1 = __builtin_bit_cast(bf16x8, w1);
 #pragma unroll
       for (int w = 0; w < NV; ++w) {
         u32x4 lo, hi;
@@ -359,8 +369,10 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
             lo[t * 2 + e / 2] = __builtin_amdgcn_perm(vr[t][e + 1][w], vr[t][e][w], 0x05040100u);
             hi[t * 2 + e / 2] = __builtin_amdgcn_perm(vr[t][e + 1][w], vr[t][e][w], 0x07060302u);
           }
-        o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pb, o[2 * w], 0, 0, 0);
-        o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pb, o[2 * w + 1], 0, 0, 0);
+        o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), p0, o[2 * w], 0, 0, 0);
+        o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), p0, o[2 * w + 1], 0, 0, 0);
+        o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), p1, o[2 * w], 0, 0, 0);
+        o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), p1, o[2 * w + 1], 0, 0, 0);
       }
     } else {
 #pragma unroll
