@@ -303,21 +303,31 @@ def adaserve_tree_accept_sampled(*, node_indptr, parent, draft_tokens, target_lo
     _check(st)
 
 
-def _device_call(name: str, tensors, stream, *args) -> None:
-    """Calls entry point ``name`` on the tensors' device: its current stream where none is given, and
-    the device made current for the call where it is not."""
-    import torch
-    device = -1
-    for t in tensors:
+def _pointers(dense, strided=()):
+    """The tensors' device, and the pointers of the dense ones (None -> NULL)."""
+    device, pointers = -1, []
+    for t in dense:
         if t is None:
+            pointers.append(None)
             continue
         at = t.get_device()
-        if at < 0:
-            raise ValueError("expected a device tensor")
-        if device < 0:
+        if at != device:
+            if at < 0 or device >= 0:
+                raise ValueError("expected a device tensor" if at < 0 else "tensors are on different devices")
             device = at
-        elif at != device:
-            raise ValueError("tensors are on different devices")
+        if not t.is_contiguous():
+            raise ValueError("expected a contiguous tensor")
+        pointers.append(t.data_ptr())
+    for t in strided:
+        if t is not None and t.get_device() != device:
+            raise ValueError("expected a device tensor" if t.get_device() < 0 else "tensors are on different devices")
+    return device, pointers
+
+
+def _device_call(name: str, device: int, stream, *args) -> None:
+    """Calls entry point ``name`` on a device: its current stream where none is given, and the device made
+    current for the call where it is not."""
+    import torch
     fn = getattr(load_library(), name)
     s = (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
     if device == torch.cuda.current_device():
@@ -333,10 +343,10 @@ def _rows(t, name: str):
     """(pointer, elements between rows) of a [rows, heads, dim] tensor whose rows are dense."""
     if t is None:
         return None, 0
-    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
-        if t.shape[1] * t.shape[2] > 1 and t.numel():
-            raise ValueError("%s must have dense heads" % name)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    (rows, heads, dim), (step, head_step, one) = t.shape, t.stride()
+    if (one != 1 or head_step != dim) and heads * dim > 1 and rows:
+        raise ValueError("%s must have dense heads" % name)
+    return t.data_ptr(), step if rows > 1 else heads * dim
 
 
 def _typed(t, dtype, name: str) -> None:
@@ -358,15 +368,17 @@ def adaserve_rope_append_kv(*, token_indptr, prefix_len, q=None, k=None, v=None,
     if main is None:
         raise ValueError("neither q nor k is given")
     B = token_indptr.shape[0] - 1
-    T, _, D = main.shape
+    T, heads, D = main.shape
     hq = 0 if q is None else q.shape[1]
-    hkv = 1 if k is None else k.shape[1]
-    if k_pages is not None and (k is None or k_pages.shape[1] != hkv or k_pages.shape[3] != D
-                                or v_pages is None or v_pages.shape != k_pages.shape):
-        raise ValueError("k_pages and v_pages must be [pages, %d, page_size, %d]" % (hkv, D))
-    for t, name, like in ((q, "q", main), (v, "v", k), (q_out, "q_out", q), (k_out, "k_out", k)):
+    hkv = 1 if k is None else heads
+    pages, ps = 0, 1
+    if k_pages is not None:
+        pages, page_heads, ps, page_dim = k_pages.shape
+        if k is None or page_heads != hkv or page_dim != D or v_pages is None or v_pages.shape != k_pages.shape:
+            raise ValueError("k_pages and v_pages must be [pages, %d, page_size, %d]" % (hkv, D))
+    for t, name, like, h in ((q, "q", main, hq), (v, "v", k, hkv), (q_out, "q_out", q, hq), (k_out, "k_out", k, hkv)):
         if t is not None:
-            if like is None or t.shape[0] != T or t.shape[2] != D or (t is not q and t.shape[1] != like.shape[1]):
+            if like is None or t.shape != (T, h, D):
                 raise ValueError("%s does not fit the tokens, heads and head dim of the other rows" % name)
             _typed(t, main.dtype, name)
     for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
@@ -378,13 +390,12 @@ def adaserve_rope_append_kv(*, token_indptr, prefix_len, q=None, k=None, v=None,
             raise ValueError("%s has %d rows, expected %d" % (name, t.shape[0], n))
     _typed(inv_freq, torch.float32, "inv_freq")
     (qp, qs), (kp, ks), (vp, vs) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
-    pages, ps = (0, 1) if k_pages is None else (k_pages.shape[0], k_pages.shape[2])
-    _device_call("adaserve_rope_append_kv", (main, q, v, token_indptr, prefix_len, positions, inv_freq, q_out, k_out,
-                                             k_pages, v_pages, block_table, new_prefix_len), stream,
-                 B, T, _dptr(token_indptr), _dptr(prefix_len), _dptr(positions), qp, qs, kp, ks, vp, vs,
-                 _dptr(inv_freq), 0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved), hq, hkv, D, ps,
-                 _dtype_code(main), _dptr(q_out), _dptr(k_out), _dptr(k_pages), _dptr(v_pages), pages,
-                 _dptr(block_table), 0 if block_table is None else block_table.shape[1], _dptr(new_prefix_len))
+    device, (ip, pl, pos, inv, qo, ko, kpg, vpg, bt, new) = _pointers(
+        (token_indptr, prefix_len, positions, inv_freq, q_out, k_out, k_pages, v_pages, block_table, new_prefix_len),
+        (q, k, v))
+    _device_call("adaserve_rope_append_kv", device, stream, B, T, ip, pl, pos, qp, qs, kp, ks, vp, vs, inv,
+                 0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved), hq, hkv, D, ps, _dtype_code(main),
+                 qo, ko, kpg, vpg, pages, bt, 0 if block_table is None else block_table.shape[1], new)
 
 
 def _check_paged(q, k_pages, v_pages, block_table, context_len, out, requests) -> None:
@@ -424,11 +435,11 @@ def adaserve_prompt_attn(*, token_indptr, token_indptr_host, q, k_pages, v_pages
     _check_paged(q, k_pages, v_pages, block_table, context_len, out, B)
     _typed(token_indptr, torch.int32, "token_indptr")
     qp, qs = _rows(q, "q")
-    _device_call("adaserve_prompt_attn", (q, token_indptr, k_pages, v_pages, block_table, context_len, out, workspace),
-                 stream, B, _dptr(token_indptr), ip.ctypes.data, qp, qs, _dptr(k_pages), _dptr(v_pages),
-                 k_pages.shape[0], _dptr(block_table), block_table.shape[1], _dptr(context_len), cl.ctypes.data, Hq,
-                 k_pages.shape[1], D, k_pages.shape[2], sm_scale, _dtype_code(q), _dptr(out), _dptr(workspace),
-                 _bytes(workspace))
+    device, (tip, kp, vp, bt, clen, o, ws) = _pointers(
+        (token_indptr, k_pages, v_pages, block_table, context_len, out, workspace), (q,))
+    _device_call("adaserve_prompt_attn", device, stream, B, tip, ip.ctypes.data, qp, qs, kp, vp, k_pages.shape[0], bt,
+                 block_table.shape[1], clen, cl.ctypes.data, Hq, k_pages.shape[1], D, k_pages.shape[2], sm_scale,
+                 _dtype_code(q), o, ws, _bytes(workspace))
 
 
 def adaserve_decode_attn_workspace_bytes(num_requests: int, max_context: int, num_q_heads: int, num_kv_heads: int,
@@ -446,10 +457,10 @@ def adaserve_decode_attn(*, q, k_pages, v_pages, block_table, context_len, max_c
     B, Hq, D = q.shape
     _check_paged(q, k_pages, v_pages, block_table, context_len, out, B)
     qp, qs = _rows(q, "q")
-    _device_call("adaserve_decode_attn", (q, k_pages, v_pages, block_table, context_len, out, workspace), stream, B,
-                 qp, qs, _dptr(k_pages), _dptr(v_pages), k_pages.shape[0], _dptr(block_table), block_table.shape[1],
-                 _dptr(context_len), max_context, Hq, k_pages.shape[1], D, k_pages.shape[2], sm_scale,
-                 _dtype_code(q), _dptr(out), _dptr(workspace), _bytes(workspace))
+    device, (kp, vp, bt, clen, o, ws) = _pointers((k_pages, v_pages, block_table, context_len, out, workspace), (q,))
+    _device_call("adaserve_decode_attn", device, stream, B, qp, qs, kp, vp, k_pages.shape[0], bt, block_table.shape[1],
+                 clen, max_context, Hq, k_pages.shape[1], D, k_pages.shape[2], sm_scale, _dtype_code(q), o, ws,
+                 _bytes(workspace))
 
 
 def adaserve_sample_workspace_bytes(num_rows: int, vocab: int, dtype: int) -> int:
@@ -473,9 +484,8 @@ def adaserve_sample(*, logits, vocab: int, u, out_token, temperature=None, top_k
                            (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"), (u, torch.float32, "u"),
                            (out_token, torch.int32, "out_token")):
         _typed(t, dtype, name)
-        if t is not None and t.shape[0] != rows:
-            raise ValueError("%s has %d entries, expected %d" % (name, t.shape[0], rows))
-    _device_call("adaserve_sample", (logits, temperature, top_k, top_p, min_p, u, out_token, workspace), stream,
-                 logits.data_ptr(), logits.stride(0) if rows > 1 else width, rows, vocab, _dtype_code(logits),
-                 _dptr(temperature), _dptr(top_k), _dptr(top_p), _dptr(min_p), _dptr(u), _dptr(out_token),
-                 _dptr(workspace), _bytes(workspace))
+        if t is not None and t.numel() != rows:
+            raise ValueError("%s has %d entries, expected %d" % (name, t.numel(), rows))
+    device, (t, k, p, m, up, out, ws) = _pointers((temperature, top_k, top_p, min_p, u, out_token, workspace), (logits,))
+    _device_call("adaserve_sample", device, stream, logits.data_ptr(), logits.stride(0) if rows > 1 else width, rows,
+                 vocab, _dtype_code(logits), t, k, p, m, up, out, ws, _bytes(workspace))
