@@ -487,7 +487,8 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
   auto descend = [&](bool by_mass, int bin, uint64_t want, uint64_t &before, uint32_t &found) {
     uint32_t prefix = 0;
     before = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
+    // (of a bf16 key the high half says all)
+    for (int shift = 24; shift >= (BF16 ? 16 : 0); shift -= 8) {
       if (tid < 256) digit_n[tid] = 0, digit_w[tid] = 0;
       __syncthreads();
       each([&](uint32_t key, int) {
@@ -530,7 +531,8 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
       before = s_before;
       __syncthreads();
     }
-    found = prefix;
+    // low halves: those of u ^ 0x80000000 and of ~u with a zero low half
+    found = !BF16 ? prefix : prefix << 16 | (prefix >> 15 ? 0 : 0xffffu);
   };
   // sum over the workgroup of f(key, index), over the tokens of interest
   auto sum_of = [&](auto f) {
@@ -630,9 +632,13 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
       if (w) atomicAdd(&part_w[(list_idx[i] + r.off) / (a.part_vecs * EPV)], (unsigned long long)w);
     }
     for (int p = wave; p < a.parts; p += T / 64) {
-      uint64_t w = 0;
+      uint64_t w = 0, x[kBins / 64];
       const uint64_t *h = a.ws_hist + (row * a.parts + p) * kBins;
-      for (int b = lane; b < whole_bins; b += 64) w += h[b] & kMassMask;
+#pragma unroll
+      for (int i = 0; i < kBins / 64; ++i) x[i] = h[i * 64 + lane];
+#pragma unroll
+      for (int i = 0; i < kBins / 64; ++i)
+        if (i * 64 + lane < whole_bins) w += x[i] & kMassMask;
 #pragma unroll
       for (int o = 32; o >= 1; o >>= 1) w += __shfl_xor((unsigned long long)w, o, 64);
       if (lane == 0) atomicAdd(&part_w[p], (unsigned long long)w);
