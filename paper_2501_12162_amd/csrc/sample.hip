@@ -274,15 +274,43 @@ __device__ __forceinline__ void least_bins(const Row &r, int &lo, int &hi) {
   hi = bin_of(b + 1e-6);
 }
 
+// The least key whose token lies in bin `bin` or before it (the bins fall as the
+// logits rise), by the whole wave, six bits a step.
+__device__ __forceinline__ uint32_t least_key(const Row &r, int bin) {
+  const int lane = threadIdx.x & 63;
+  uint32_t key = 0;
+#pragma unroll
+  for (int shift = 30; shift >= 0; shift -= 6) {
+    // (the first step has two bits only)
+    const uint32_t at = key + ((uint32_t)lane << shift);
+    const bool in = (shift < 30 || lane < 4) && (at >= r.top_key || bin_of(depth_of(r, key_value(at))) <= bin);
+    const unsigned long long hit = __ballot(in);
+    // the last key of the step that is not in; the first key of all may be
+    const int first = hit ? __ffsll(hit) - 1 : shift < 30 ? 64 : 4;
+    if (shift == 0) return key + first;
+    key += (uint32_t)max(first - 1, 0) << shift;
+  }
+  return key;
+}
+
+// Logits from `lo` to below `hi`.
+struct Span {
+  float lo, hi;
+  __device__ __forceinline__ uint32_t has(float x) const { return x >= lo && x < hi; }
+};
+
 typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 
+// (eight workgroups per CU, so that the first steps of some hide behind the loads
+// of others: 250 rows of 128256 37 -> 34 us)
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a) {
+__global__ __launch_bounds__(kThreads, 8) void sample_list_kernel(SampleArgs a) {
   static_assert(kBins == 2 * kThreads, "two bins per thread");
   __shared__ uint64_t scan[kThreads / 64];
   __shared__ uint64_t cum_w[kBins + 1];
   __shared__ uint32_t cum_n[kBins + 1];
   __shared__ int cut_k, cut_lo, cut_hi;
+  __shared__ Span spans[3];
   const int64_t row = blockIdx.x / a.parts;
   const int part = (int)(blockIdx.x - row * a.parts);
   const Row r = load_row<BF16>(a, row);
@@ -308,8 +336,7 @@ __global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a) {
     }
   };
   int done = 0;
-  for (; done + 16 <= a.parts; done += 16) add_parts(done, std::integral_constant<int, 16>{});
-  for (; done + 4 <= a.parts; done += 4) add_parts(done, std::integral_constant<int, 4>{});
+  for (; done + 8 <= a.parts; done += 8) add_parts(done, std::integral_constant<int, 8>{});
   for (; done < a.parts; ++done) add_parts(done, std::integral_constant<int, 1>{});
   uint64_t all_w, all_n;
   const uint64_t before_w = block_scan<kThreads>(w[0] + w[1], scan, all_w);
@@ -349,6 +376,19 @@ __global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a) {
   const int plo = cut_lo, phi = cut_hi;
   int mlo, mhi;
   least_bins(r, mlo, mhi);
+  // The logits of those bins (of the last one none: it has no mass), so that a
+  // token costs comparisons instead of its bin (250 rows of 128256: 41 -> 37 us).
+  if (filtered && wave < 3) {
+    const int lo = wave == 0 ? ck : wave == 1 ? plo : mlo, hi = min(wave == 0 ? ck : wave == 1 ? phi : mhi, kBins - 2);
+    Span x{INFINITY, -INFINITY};
+    if (lo <= hi) {
+      x.lo = key_value(least_key(r, hi));
+      x.hi = lo > 0 ? key_value(least_key(r, lo - 1)) : INFINITY;
+    }
+    if (lane == 0) spans[wave] = x;
+  }
+  __syncthreads();
+  const Span sk = spans[0], sp = spans[1], sm = spans[2];
   // tokens of those bins, in index order; each wave lists those of its quarter
   const int quarter = a.part_vecs / (kThreads / 64);
   const int v0 = part * a.part_vecs + wave * quarter;
@@ -368,8 +408,8 @@ __global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a) {
         uint32_t mine = 0;
 #pragma unroll
         for (int i = 0; i < Vec<BF16>::EPV; ++i) {
-          const int b = bin_of(depth_of(r, x[h].x[i]));
-          mine |= (uint32_t)(b < kBins - 1 && (b == ck || (b >= plo && b <= phi) || (b >= mlo && b <= mhi))) << i;
+          const float v = x[h].x[i];
+          mine |= (sk.has(v) | sp.has(v) | sm.has(v)) << i;
         }
         if (!__any(mine != 0)) continue;
         const int count = __popc(mine);
