@@ -1,6 +1,24 @@
 // Causal attention of packed prompts over the paged cache on gfx950: row i of
 // a request's n tokens stands at position c - n + i of its c cached keys and
 // sees the keys up to itself.
+//
+//   o_i = sum_k w_ik v_k / sum_k w_ik,  w_ik = 2^(c (q_i k_k - m_i)),  c = scale log2 e
+// in one pass over the keys; m_i is any reference that keeps the weights in
+// range, and cancels.
+//
+// Bound by the matrix cores: 4 D flops per (row, key) pair, and a key is read
+// from memory once per 256 rows, from LDS once per 64.  The rows of a kv-head's
+// query heads share its keys, so a tile is 256 / G tokens with all G heads.  S is
+// taken transposed (keys by rows): a lane then holds 16 keys of one row, the sum
+// of its weights stays in the lane, and P^T is the B operand of O^T = V^T P^T
+// after one exchange of halves.  Weights are rounded to bf16 for that product (the
+// output is, too); their sum is of the unrounded ones.
+//
+// Measured, bf16, D = 128, 32 heads on 8: one prompt of 8191 tokens 455 - 467 us,
+// 1.18 - 1.21 PFLOP/s of the pairs seen (a library product of 8192 x 8192 x 8192
+// runs at 1.16); 16 ragged prompts of 512 - 2048 tokens 374 - 381 us, 0.81 PFLOP/s:
+// a tile's start, masked end and output take 19 thousand cycles, as long as 900
+// keys.  fp32, D = 64, 3 prompts of up to 700 tokens, 8 on 8 heads: 24 us.
 #include <type_traits>
 
 #include "device_common.h"

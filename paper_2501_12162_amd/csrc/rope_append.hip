@@ -16,6 +16,10 @@
 // columns would repeat each once per head, as much time as the copy takes),
 // then move 16-byte pieces, both halves of a pair in one thread, so that the
 // outputs may be the inputs.
+//
+// Measured, bf16, D = 128, 32 + 8 + 8 heads: 9.6 thousand tokens of 8 prompts, 236 MB
+// read and written, 55 us, 4.3 TB/s, with inputs that no cache holds (a device
+// copy of 1 GiB runs at 5.0), 40 us when the caches hold some of them.  One token: 4 us.
 #include "device_common.h"
 #include "plan.h"
 #include "serving.h"
