@@ -90,7 +90,7 @@ int32_t validate_prompt(int32_t num_requests, const int32_t *indptr, const int32
 // requests than it holds are found by a scan on the device, in their own order.
 // Several units per workgroup, each workgroup taking every kPromptGrid-th,
 // hide the loads that open a unit behind the end of the one before (16 ragged
-// prompts of 636-2012 tokens 420 -> 411 us); that needs units in descending
+// prompts of 636-2012 tokens 379 -> 375 us); that needs units in descending
 // order of keys, which the table gives where all rows have as many cached keys
 // before them.
 struct PromptPlan {
