@@ -460,7 +460,8 @@ int32_t adaserve_tree_accept_sampled(int32_t num_requests, int32_t total_nodes,
  *     as they are);
  *   q_out [num_tokens, Hq, D], k_out [num_tokens, Hkv, D]: dense rotated rows;
  *     q_out may be q and k_out may be k where those are dense.  q and q_out may
- *     both be NULL; k_out may be NULL when there are pages.
+ *     both be NULL; k_out may be NULL when there are pages, k (and k_out) when
+ *     there are none.
  *   k_pages, v_pages [num_pages, Hkv, page_size, D]: rotated keys, and values
  *     bit for bit, go to page block_table[r][place / page_size], slot
  *     place % page_size.  Both NULL: nothing is appended (nodes of draft trees:
@@ -503,6 +504,7 @@ int32_t adaserve_rope_append_kv(int32_t num_requests, int32_t num_tokens, const 
  * are never read into the result; a key that a row does not see adds nothing to
  * it, whatever key and value it holds.
  * Block-table entries outside [0, num_pages) are all-zero pages.
+ * Scores are to be below 2^29 in magnitude.
  * token_indptr_host and context_len_host mirror the device arrays.  T * Hq <
  * 2^31.  workspace: at least adaserve_prompt_attn_workspace_bytes(...) bytes
  * (0 for most batches; 256-byte aligned, no initialisation needed); calls that

@@ -312,7 +312,7 @@ int32_t adaserve_rope_append_kv(int32_t num_requests, int32_t num_tokens, const 
   a.rotary_dim = rotary_dim;
   a.interleaved = interleaved;
   a.num_q_heads = q ? num_q_heads : 0;
-  a.num_kv_heads = num_kv_heads;
+  a.num_kv_heads = k ? num_kv_heads : 0;
   a.head_dim = head_dim;
   a.page_size = page_size;
   a.q_out = q_out;

@@ -25,7 +25,7 @@ struct RopeAppendArgs {
   int32_t rotary_dim;
   int32_t interleaved;
   int32_t num_q_heads;           // 0 without q
-  int32_t num_kv_heads;
+  int32_t num_kv_heads;          // 0 without k
   int32_t head_dim;
   int32_t page_size;
   void *q_out;                   // [num_tokens, Hq, D]

@@ -163,3 +163,24 @@ def test_append_replayed_from_a_graph(ada):
         for a, b in zip(eager, graphed):
             assert back(a).tobytes() == back(b).tobytes(), rep
         assert eager[2].tolist() == (start + rep + 1).tolist()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("which", ["q", "k"])
+def test_queries_or_keys_alone(ada, dtype, which):
+    """Rows of one kind only: no pages, no other output."""
+    import torch
+    rng = np.random.default_rng(17)
+    new, prefix, h, d = [3, 0, 1200], [5, 2, 31], 6, 128
+    indptr = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    x = typed(rng.standard_normal((int(indptr[-1]) + 2, h, d)), dtype)
+    inv = inv_freq(d)
+    out = torch.full(x.shape, SENTINEL, dtype=to_dev(x[:1]).dtype, device="cuda")
+    print("alone", which, dtype, flush=True)
+    ada.adaserve_rope_append_kv(token_indptr=to_dev(indptr), prefix_len=to_dev(np.asarray(prefix, np.int32)),
+                                inv_freq=to_dev(inv), **{which: to_dev(x), which + "_out": out})
+    torch.cuda.synchronize()
+    req, place, _, _ = serving.append_places(indptr, prefix, np.zeros((3, 0), np.int32), 0, PS, len(x))
+    own = req >= 0
+    close(back(out)[own], serving.rope(x, place, inv)[own], x, dtype)
+    assert (serving.widen(back(out)[~own]) == SENTINEL).all()
