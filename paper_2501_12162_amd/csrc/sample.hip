@@ -21,8 +21,8 @@
 //      lists its tokens of those bins, in index order (a bin is a sixteenth of a
 //      power of two wide: a few hundred tokens out of 10^5);
 //   4. one workgroup per row: the exact cuts among the listed tokens, the kept
-//      mass of each part (whole bins from its histogram, the rest from the
-//      list), and the draw within the one part that holds it.
+//      mass of each part (that of the bins before all cuts from pass 3, the rest
+//      from the list), and the draw within the one part that holds it.
 // The first three read the row (from HBM once, then out of the caches); pass 2
 // is bound by fp64 arithmetic and LDS atomics, the rest by memory and latency.
 // Measured, fp32, 250 rows of 128256 (128 MB), all filters: 20 (6.3 TB/s), 41, 34
@@ -319,8 +319,15 @@ __global__ __launch_bounds__(kThreads, 8) void sample_list_kernel(SampleArgs a) 
   const Row r = load_row<BF16>(a, row);
   if (r.state) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const bool filtered = r.k || r.p < 1.0 || r.least > 0.0;
-  if (!filtered && part > 0) {
+  const u64x2 own = *(const u64x2 *)(a.ws_hist + (int64_t)blockIdx.x * kBins + 2 * tid);
+  // the part's mass in the bins before `floor`
+  auto part_mass = [&](int floor) {
+    uint64_t total;
+    block_scan<kThreads>((2 * tid < floor ? own[0] & kMassMask : 0) + (2 * tid + 1 < floor ? own[1] & kMassMask : 0), scan, total);
+    if (tid == 0) a.ws_part_w[blockIdx.x] = total;
+  };
+  if (!(r.k || r.p < 1.0 || r.least > 0.0)) {   // no filter: nothing to cut
+    part_mass(kBins);
     if (lane == 0) a.ws_count[(int64_t)blockIdx.x * (kThreads / 64) + wave] = 0;
     return;
   }
@@ -381,7 +388,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_list_kernel(SampleArgs a) 
   least_bins(r, mlo, mhi);
   // The logits of those bins (of the last one none: it has no mass), so that a
   // token costs comparisons instead of its bin (250 rows of 128256: 41 -> 37 us).
-  if (filtered && wave < 3) {
+  if (wave < 3) {
     const int lo = wave == 0 ? ck : wave == 1 ? plo : mlo, hi = min(wave == 0 ? ck : wave == 1 ? phi : mhi, kBins - 2);
     Span x{INFINITY, -INFINITY};
     if (lo <= hi) {
@@ -390,6 +397,9 @@ __global__ __launch_bounds__(kThreads, 8) void sample_list_kernel(SampleArgs a) 
     }
     if (lane == 0) spans[wave] = x;
   }
+  // (the bins from there on that are kept as a whole are listed, too: the cut of
+  // top-p lies in [plo, phi], that of top-k, where there is no top-p, in ck)
+  part_mass(min(ck, min(plo, mlo)));
   __syncthreads();
   const Span sk = spans[0], sp = spans[1], sm = spans[2];
   // tokens of those bins, in index order; each wave lists those of its quarter
@@ -398,8 +408,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_list_kernel(SampleArgs a) 
   const int64_t slot = (int64_t)blockIdx.x * (kThreads / 64) + wave;
   uint64_t *list = a.ws_list + slot * kSampleListCap;
   uint32_t have = 0;
-  if (filtered)
-    for (int vb = 0; vb < quarter; vb += 64 * Vec<BF16>::BATCH) {
+  for (int vb = 0; vb < quarter; vb += 64 * Vec<BF16>::BATCH) {
       Vec<BF16> x[Vec<BF16>::BATCH];
 #pragma unroll
       for (int h = 0; h < Vec<BF16>::BATCH; ++h) {
@@ -478,10 +487,7 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
     if (tid == 0) a.out_token[row] = s_token;
     return;
   }
-  int mlo, mhi;
-  least_bins(r, mlo, mhi);
-
-  // the row's running sums, and the listed tokens in index order
+  // the row's running sums (of a row with a filter), and the listed tokens in index order
   for (int b = tid; b <= kBins; b += T) {
     cum_w[b] = a.ws_cum_w[row * (kBins + 1) + b];
     cum_n[b] = a.ws_cum_n[row * (kBins + 1) + b];
@@ -493,7 +499,7 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
     const uint64_t before = block_scan<T>(c, scan, all);
     const uint64_t over = __any(c > (uint32_t)kSampleListCap);
     if (tid <= lists) list_at[tid] = (uint32_t)before;
-    if (tid < kSampleMaxParts) part_w[tid] = 0;
+    if (tid < kSampleMaxParts) part_w[tid] = tid < a.parts ? a.ws_part_w[row * a.parts + tid] : 0;
     if (tid == 0) s_digit = all > (uint64_t)kSampleList;
     __syncthreads();
     if (over && lane == 0) s_digit = 1;
@@ -674,28 +680,16 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
     return (double)w >= r.least ? w : 0;
   };
 
-  // kept mass by part: whole bins from its histogram, the rest token by token
-  const int whole_bins = min(cut ? key_bin(cut) : kBins, mlo);
+  // kept mass by part: the bins before all cuts (pass 3), the rest token by token
   if (!whole) {
     for (int i = tid; i < listed; i += T) {
-      const uint32_t key = list_key[i];
-      if (key_bin(key) < whole_bins) continue;
-      const uint64_t w = kept(key, list_idx[i]);
+      const uint64_t w = kept(list_key[i], list_idx[i]);
       if (w) atomicAdd(&part_w[(list_idx[i] + r.off) / (a.part_vecs * EPV)], (unsigned long long)w);
     }
-    for (int p = wave; p < a.parts; p += T / 64) {
-      uint64_t w = 0, x[kBins / 64];
-      const uint64_t *h = a.ws_hist + (row * a.parts + p) * kBins;
-#pragma unroll
-      for (int i = 0; i < kBins / 64; ++i) x[i] = h[i * 64 + lane];
-#pragma unroll
-      for (int i = 0; i < kBins / 64; ++i)
-        if (i * 64 + lane < whole_bins) w += x[i] & kMassMask;
-#pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) w += __shfl_xor((unsigned long long)w, o, 64);
-      if (lane == 0) atomicAdd(&part_w[p], (unsigned long long)w);
-    }
   } else {
+    __syncthreads();
+    if (tid < kSampleMaxParts) part_w[tid] = 0;
+    __syncthreads();
     for (int p = 0; p < a.parts; ++p) {
       uint64_t w = 0;
       for (int v = tid; v < a.part_vecs; v += T) {

@@ -499,6 +499,7 @@ int32_t adaserve_sample(const void *logits, int64_t row_stride, int32_t num_rows
   a.ws_cum_w = (uint64_t *)(ws + plan.cum_w);
   a.ws_cum_n = (uint32_t *)(ws + plan.cum_n);
   a.ws_max = (uint32_t *)(ws + plan.max);
+  a.ws_part_w = (uint64_t *)(ws + plan.part_w);
   a.ws_count = (uint32_t *)(ws + plan.count);
   a.ws_list = (uint64_t *)(ws + plan.list);
   return launch_status(launch_sample(a, dtype == ADASERVE_BF16, (hipStream_t)stream), "sampling launch");

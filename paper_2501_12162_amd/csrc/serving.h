@@ -158,6 +158,7 @@ struct SampleArgs {
   uint64_t *ws_hist;             // [rows, parts, bins] mass | count << 48
   uint64_t *ws_cum_w;            // [rows, bins + 1] mass of the bins before
   uint32_t *ws_cum_n;            // [rows, bins + 1] tokens of the bins before
+  uint64_t *ws_part_w;           // [rows, parts] mass of the bins before all cuts
   uint32_t *ws_count;            // [rows, parts, 4] listed tokens
   uint64_t *ws_list;             // [rows, parts, 4, kSampleListCap] key << 32 | index
 };
@@ -167,7 +168,7 @@ struct SampleArgs {
 // every part.  At most 64 parts (2^20 logits and up to 7 before the row).
 struct SamplePlan {
   int32_t parts, part_vecs;
-  size_t cum_w, cum_n, max, count, list, bytes;   // offsets; the histograms come first
+  size_t cum_w, cum_n, max, part_w, count, list, bytes;   // offsets; the histograms come first
 };
 
 inline SamplePlan sample_plan(int32_t rows, int32_t vocab, bool bf16) {
@@ -182,7 +183,8 @@ inline SamplePlan sample_plan(int32_t rows, int32_t vocab, bool bf16) {
   p.cum_w = up(all * kSampleBins * 8);
   p.cum_n = p.cum_w + up((size_t)rows * (kSampleBins + 1) * 8);
   p.max = p.cum_n + up((size_t)rows * (kSampleBins + 1) * 4);
-  p.count = p.max + up(all * 4);
+  p.part_w = p.max + up(all * 4);
+  p.count = p.part_w + up(all * 8);
   p.list = p.count + up(all * 4 * 4);
   p.bytes = rows ? p.list + up(all * 4 * kSampleListCap * 8) : 0;
   return p;
