@@ -449,8 +449,8 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
   constexpr int T = kDrawThreads, EPV = Vec<BF16>::EPV;
   __shared__ uint32_t list_key[kSampleList];
   __shared__ int32_t list_idx[kSampleList];
-  __shared__ unsigned long long digit_w[256];
-  __shared__ uint32_t digit_n[256];
+  __shared__ unsigned long long digit_w[2][256];
+  __shared__ uint32_t digit_n[2][256];
   __shared__ unsigned long long part_w[kSampleMaxParts];
   __shared__ uint32_t list_at[kSampleMaxParts * 4 + 1];
   __shared__ uint64_t cum_w[kBins + 1];
@@ -545,26 +545,28 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
   auto descend = [&](bool by_mass, int bin, uint64_t want, uint64_t &before, uint32_t &found) {
     uint32_t prefix = 0;
     before = 0;
+    const uint64_t tie_w = by_mass && ties > 0 && key_bin(cut) == bin ? (uint64_t)ties * mass_of(r, key_value(cut)) : 0;
+    if (tid < 256) digit_n[0][tid] = 0, digit_w[0][tid] = 0;
+    __syncthreads();
+    int at = 0;   // the sums of this digit; the others are cleared meanwhile
     // (of a bf16 key the high half says all)
-    for (int shift = 24; shift >= (BF16 ? 16 : 0); shift -= 8) {
-      if (tid < 256) digit_n[tid] = 0, digit_w[tid] = 0;
-      __syncthreads();
+    for (int shift = 24; shift >= (BF16 ? 16 : 0); shift -= 8, at ^= 1) {
       each([&](uint32_t key, int) {
         if (shift < 24 && (key >> (shift + 8)) != prefix) return;
         if (key_bin(key) != bin) return;
-        if (!by_mass) atomicAdd(&digit_n[(key >> shift) & 255], 1u);
-        else if (key > cut) atomicAdd(&digit_w[(key >> shift) & 255], (unsigned long long)mass_of(r, key_value(key)));
+        if (!by_mass) atomicAdd(&digit_n[at][(key >> shift) & 255], 1u);
+        else if (key > cut) atomicAdd(&digit_w[at][(key >> shift) & 255], (unsigned long long)mass_of(r, key_value(key)));
       });
-      __syncthreads();
-      if (by_mass && tid == 0 && ties > 0 && key_bin(cut) == bin && (shift == 24 || (cut >> (shift + 8)) == prefix))
-        digit_w[(cut >> shift) & 255] += (unsigned long long)ties * mass_of(r, key_value(cut));
       __syncthreads();
       if (tid < 64) {
         // lane l holds digits 255 - 4 l .. 252 - 4 l, the largest first
+        const int tie_digit = tie_w && (shift == 24 || (cut >> (shift + 8)) == prefix) ? (int)(cut >> shift) & 255 : -1;
         uint64_t d[4], sum = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          d[q] = by_mass ? digit_w[255 - 4 * lane - q] : digit_n[255 - 4 * lane - q];
+          const int digit = 255 - 4 * lane - q;
+          d[q] = by_mass ? digit_w[at][digit] : digit_n[at][digit];
+          if (digit == tie_digit) d[q] += tie_w;
           sum += d[q];
         }
         uint64_t s = sum;
@@ -577,17 +579,18 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
         const unsigned long long reach = __ballot(before + s >= want), some = __ballot(sum > 0);
         const int l = reach ? __ffsll(reach) - 1 : some ? 63 - __clzll(some) : 63;
         if (lane == l) {
-          uint64_t at = before + s - sum;
+          uint64_t upto = before + s - sum;
           int q = 0;
-          while (q < 3 && at + d[q] < want) at += d[q++];
+          while (q < 3 && upto + d[q] < want) upto += d[q++];
           s_digit = (uint32_t)(255 - 4 * lane - q);
-          s_before = at;
+          s_before = upto;
         }
+      } else if (tid >= 256 && tid < 512) {
+        digit_n[at ^ 1][tid - 256] = 0, digit_w[at ^ 1][tid - 256] = 0;
       }
       __syncthreads();
       prefix = (prefix << 8) | s_digit;
       before = s_before;
-      __syncthreads();
     }
     // low halves: those of u ^ 0x80000000 and of ~u with a zero low half
     found = !BF16 ? prefix : prefix << 16 | (prefix >> 15 ? 0 : 0xffffu);
