@@ -10,16 +10,18 @@
 // rounded once to the output type.
 //
 // Bound by memory: every row is read once and written once (keys a second
-// time where k_out is asked for).  A workgroup takes kTokens tokens, or one
-// where there are few: its threads first put the tokens' sines and cosines
-// into LDS, one angle per thread (every thread computing those of its own
-// columns would repeat each once per head, as much time as the copy takes),
-// then move 16-byte pieces, both halves of a pair in one thread, so that the
-// outputs may be the inputs.
+// time where k_out is asked for).  A workgroup takes one token: its first wave
+// puts the token's sines and cosines into LDS, one angle per lane (every thread
+// computing those of its own columns would repeat each once per head, as much
+// time as the copy takes), then all move 16-byte pieces, both halves of a pair in
+// one thread, so that the outputs may be the inputs.  (Four tokens to a workgroup,
+// a wave for the angles of each: 54.5 instead of 48 us on the 9611 tokens below, 9.1
+// instead of 6.7 on 1023.)
 //
 // Measured, bf16, D = 128, 32 + 8 + 8 heads: 9.6 thousand tokens of 8 prompts, 236 MB
-// read and written, 55 us, 4.3 TB/s, with inputs that no cache holds (a device
-// copy of 1 GiB runs at 5.0), 40 us when the caches hold some of them.  One token: 4 us.
+// read and written, 48 us, 4.9 TB/s, with inputs that no cache holds (a device
+// copy of 1 GiB runs at 5.0), 37 us when the caches hold some of them; 40 thousand
+// tokens 5.1 TB/s.  One token: 4.1 us in a graph.
 #include "device_common.h"
 #include "plan.h"
 #include "serving.h"
@@ -29,7 +31,6 @@ namespace adaserve {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 4;   // per workgroup
 
 // The request that owns token t: the last r with indptr[r] <= t, by the whole
 // wave (64 entries per round of loads).  -1 when t is in no request.
@@ -92,20 +93,20 @@ __device__ __forceinline__ void turn_neighbours(u32x4 &a, const float2 *cs) {
   }
 }
 
-// Workgroups 0 .. token_blocks - 1 take `tokens` tokens each, the others four
-// requests each, whose new lengths they write.
+// Workgroups 0 .. tokens - 1 take a token each, the others four requests each,
+// whose new lengths they write.
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeAppendArgs a, int32_t tokens, int64_t token_blocks) {
+__global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeAppendArgs a, int32_t tokens) {
   constexpr int EPV = BF16 ? 8 : 4;
   constexpr int ESZ = BF16 ? 2 : 4;
-  __shared__ float2 cs[kTokens][kRopeMaxHeadDim / 2];
-  __shared__ int64_t page_row[kTokens];   // row (page, head 0, slot) of the pools, or -1
-  __shared__ int32_t owner[kTokens];
+  __shared__ float2 cs[kRopeMaxHeadDim / 2];
+  __shared__ int64_t page_row;   // row (page, head 0, slot) of the pools, or -1
+  __shared__ int32_t owner;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
-  if ((int64_t)blockIdx.x >= token_blocks) {
+  if ((int64_t)blockIdx.x >= tokens) {
     // new lengths: a request grows by its leading rows whose page exists
-    const int64_t r = ((int64_t)blockIdx.x - token_blocks) * 4 + wave;
+    const int64_t r = ((int64_t)blockIdx.x - tokens) * 4 + wave;
     if (r >= a.num_requests) return;
     const int32_t L = a.prefix_len[r];
     const int64_t begin = max(a.token_indptr[r], 0), end = min(a.token_indptr[r + 1], a.num_tokens);
@@ -131,12 +132,10 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeAppendArgs a,
     return;
   }
 
-  const int64_t t0 = (int64_t)blockIdx.x * tokens;
-  const int here = (int)min((int64_t)tokens, a.num_tokens - t0);
-  // one wave per token: its request, position and page
-  if (wave < here) {
-    const int32_t t = (int32_t)(t0 + wave);
-    const int r = find_request(a.token_indptr, a.num_requests, t);
+  const int64_t t = blockIdx.x;
+  // its request, position and page
+  if (wave == 0) {
+    const int r = find_request(a.token_indptr, a.num_requests, (int32_t)t);
     int64_t place = 0, row = -1;
     if (r >= 0) {
       const int32_t L = a.prefix_len[r];
@@ -152,44 +151,42 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeAppendArgs a,
         const double turns = (double)pos * (double)a.inv_freq[i] * 0.15915494309189533577;
         float s, c;
         sincospif((float)(2.0 * (turns - __builtin_rint(turns))), &s, &c);
-        cs[wave][i] = make_float2(c, s);
+        cs[i] = make_float2(c, s);
       }
     }
     if (lane == 0) {
-      owner[wave] = r;
-      page_row[wave] = row;
+      owner = r;
+      page_row = row;
     }
   }
   __syncthreads();
+  if (owner < 0) return;
+  const int64_t place_row = page_row;
 
   // rotated heads: `pairs` pieces of two vectors each, then the vectors past
   // the rotated part, all of one head by neighbouring threads
   const int vecs = a.head_dim / EPV, half = a.rotary_dim / (2 * EPV);
   const int pieces = vecs - half;
   const int hk = a.num_q_heads + a.num_kv_heads;
-  const uint32_t items = (uint32_t)here * hk * pieces;
+  const uint32_t items = (uint32_t)hk * pieces;
   const int64_t D = a.head_dim;
   for (uint32_t w = tid; w < items; w += kThreads) {
-    const uint32_t row = w / (uint32_t)pieces;
-    const int j = (int)(w - row * pieces);
-    const int tk = (int)(row / (uint32_t)hk), h = (int)(row - (uint32_t)tk * hk);
-    if (owner[tk] < 0) continue;
-    const int64_t t = t0 + tk;
+    const int h = (int)(w / (uint32_t)pieces);
+    const int j = (int)w - h * pieces;
     const bool is_q = h < a.num_q_heads;
     const int g = is_q ? h : h - a.num_q_heads;
     const char *src = is_q ? (const char *)a.q + (t * a.q_stride + (int64_t)g * D) * ESZ
                            : (const char *)a.k + (t * a.k_stride + (int64_t)g * D) * ESZ;
     char *dst = is_q ? (char *)a.q_out : (char *)a.k_out;
     if (dst) dst += (t * (is_q ? a.num_q_heads : a.num_kv_heads) + g) * D * ESZ;
-    char *page = !is_q && page_row[tk] >= 0
-                     ? (char *)a.k_pages + (page_row[tk] + (int64_t)g * a.page_size) * D * ESZ : nullptr;
+    char *page = !is_q && place_row >= 0 ? (char *)a.k_pages + (place_row + (int64_t)g * a.page_size) * D * ESZ : nullptr;
     if (j < half) {
       u32x4 x = *(const u32x4 *)(src + j * 16), y = *(const u32x4 *)(src + (j + half) * 16);
       if (a.interleaved) {
-        turn_neighbours<BF16>(x, &cs[tk][j * (EPV / 2)]);
-        turn_neighbours<BF16>(y, &cs[tk][(j + half) * (EPV / 2)]);
+        turn_neighbours<BF16>(x, &cs[j * (EPV / 2)]);
+        turn_neighbours<BF16>(y, &cs[(j + half) * (EPV / 2)]);
       } else {
-        turn<BF16>(x, y, &cs[tk][j * EPV]);
+        turn<BF16>(x, y, &cs[j * EPV]);
       }
       if (dst) {
         *(u32x4 *)(dst + j * 16) = x;
@@ -205,37 +202,30 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeAppendArgs a,
       if (page) *(u32x4 *)(page + (j + half) * 16) = x;
     }
   }
-  if (!a.v_pages) return;
-  const uint32_t vitems = (uint32_t)here * a.num_kv_heads * vecs;
+  if (!a.v_pages || place_row < 0) return;
+  const uint32_t vitems = (uint32_t)a.num_kv_heads * vecs;
   for (uint32_t w = tid; w < vitems; w += kThreads) {
-    const uint32_t row = w / (uint32_t)vecs;
-    const int j = (int)(w - row * vecs);
-    const int tk = (int)(row / (uint32_t)a.num_kv_heads), g = (int)(row - (uint32_t)tk * a.num_kv_heads);
-    if (owner[tk] < 0 || page_row[tk] < 0) continue;
-    const char *src = (const char *)a.v + ((t0 + tk) * a.v_stride + (int64_t)g * D) * ESZ;
-    *(u32x4 *)((char *)a.v_pages + (page_row[tk] + (int64_t)g * a.page_size) * D * ESZ + j * 16) =
-        *(const u32x4 *)(src + j * 16);
+    const int g = (int)(w / (uint32_t)vecs);
+    const int j = (int)w - g * vecs;
+    const char *src = (const char *)a.v + (t * a.v_stride + (int64_t)g * D) * ESZ;
+    *(u32x4 *)((char *)a.v_pages + (place_row + (int64_t)g * a.page_size) * D * ESZ + j * 16) = *(const u32x4 *)(src + j * 16);
   }
 }
 
 }  // namespace
 
 hipError_t launch_rope_append(const RopeAppendArgs &a, bool bf16, hipStream_t stream) {
-  const int tokens = a.num_tokens >= 1024 ? kTokens : 1;
-  const int64_t token_blocks = ((int64_t)a.num_tokens + tokens - 1) / tokens;
   const int64_t length_blocks = a.new_prefix_len ? (a.num_requests + 3) / 4 : 0;
   const bool in_place = a.new_prefix_len && a.new_prefix_len == a.prefix_len;
-  auto run = [&](int64_t first, int64_t blocks) {
+  auto run = [&](int32_t tokens, int64_t blocks) {
     if (blocks == 0) return hipSuccess;
-    if (bf16)
-      hipLaunchKernelGGL(rope_append_kernel<true>, dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, tokens, first);
-    else
-      hipLaunchKernelGGL(rope_append_kernel<false>, dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, tokens, first);
+    if (bf16) hipLaunchKernelGGL(rope_append_kernel<true>, dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, tokens);
+    else hipLaunchKernelGGL(rope_append_kernel<false>, dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, tokens);
     return hipGetLastError();
   };
   // lengths written over those that the tokens read wait for a launch of their own
-  if (!in_place) return run(token_blocks, token_blocks + length_blocks);
-  const hipError_t e = run(token_blocks, token_blocks);
+  if (!in_place) return run(a.num_tokens, a.num_tokens + length_blocks);
+  const hipError_t e = run(a.num_tokens, a.num_tokens);
   return e != hipSuccess ? e : run(0, length_blocks);
 }
 

@@ -25,8 +25,8 @@
 //      from the list), and the draw within the one part that holds it.
 // The first three read the row (from HBM once, then out of the caches); pass 2
 // is bound by fp64 arithmetic and LDS atomics, the rest by memory and latency.
-// Measured, fp32, 250 rows of 128256 (128 MB), all filters: 20 (6.3 TB/s), 41, 34
-// and 26 us; one bf16 row: 3.3, 4.9, 9.7 and 17 us, of which 10 or so are launches
+// Measured, fp32, 250 rows of 128256 (128 MB), all filters: 20 (6.3 TB/s), 41, 33
+// and 25 us; one bf16 row: 3.3, 5.0, 10.0 and 15 us, of which 10 or so are launches
 // and the rest dependent steps.
 // A row whose cut bins hold more tokens than the lists take (one of few distinct
 // values, or nearly flat) is searched as a whole in pass 4.
