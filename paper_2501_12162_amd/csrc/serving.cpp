@@ -144,7 +144,8 @@ PromptPlan prompt_plan(int32_t num_requests, const int32_t *indptr, const int32_
   return p;
 }
 
-void fill_prompt(PromptAttnArgs &a, const PromptPlan &p, const int32_t *indptr, const int32_t *ctx, void *workspace) {
+void fill_prompt(PromptAttnArgs &a, const PromptPlan &p, const int32_t *indptr, const int32_t *ctx, int32_t tile_rows,
+                 void *workspace) {
   const bool split = p.chunks > 1;
   int32_t count = 0;
   if (a.num_requests <= kPromptTable)
@@ -159,8 +160,8 @@ void fill_prompt(PromptAttnArgs &a, const PromptPlan &p, const int32_t *indptr, 
     }
   int64_t end = 0;
   for (int32_t i = 0; i < count; ++i) {
-    const int32_t tiles = prompt_tiles(a.table[i].n, a.group, kPromptTileRows);
-    const int32_t below = i + 1 < count ? prompt_tiles(a.table[i + 1].n, a.group, kPromptTileRows) : 0;
+    const int32_t tiles = prompt_tiles(a.table[i].n, a.group, tile_rows);
+    const int32_t below = i + 1 < count ? prompt_tiles(a.table[i + 1].n, a.group, tile_rows) : 0;
     end += (split ? (int64_t)tiles : (int64_t)(tiles - below) * (i + 1)) * a.num_kv_heads;
     a.table[i].unit_end = (int32_t)end;
   }
@@ -383,7 +384,7 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
   a.sm_scale = sm_scale;
   a.scale_log2 = sm_scale * 1.4426950408889634f;
   if (dtype == ADASERVE_BF16) {
-    fill_prompt(a, plan, token_indptr_host, context_len_host, workspace);
+    fill_prompt(a, plan, token_indptr_host, context_len_host, kPromptTileRows, workspace);
   } else {
     // 32-row tiles read each key half as often; 16-row tiles put more units to work
     for (a.f32_rows = 32;; a.f32_rows = 16) {
@@ -392,8 +393,9 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
         a.units += (int64_t)prompt_tiles(token_indptr_host[r + 1] - token_indptr_host[r], a.group, a.f32_rows) * num_kv_heads;
       if (a.units >= 1024 || a.f32_rows == 16) break;
     }
-    a.chunk_keys = INT32_MAX;
-    a.chunks = 1;
+    PromptPlan tiles;
+    tiles.units = a.units;
+    fill_prompt(a, tiles, token_indptr_host, context_len_host, a.f32_rows, nullptr);
   }
   return launch_status(launch_prompt_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
                        "prompt attention launch");
