@@ -386,12 +386,13 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
   if (dtype == ADASERVE_BF16) {
     fill_prompt(a, plan, token_indptr_host, context_len_host, kPromptTileRows, workspace);
   } else {
-    // 32-row tiles read each key half as often; 16-row tiles put more units to work
+    // 32-row tiles read each key half as often, 16-row tiles put more units to work: 2250 tiles of 32
+    // (2 prompts of up to 1500 tokens, D = 128) 301 against 341 us, 1800 (8 of up to 300) 88 against 83
     for (a.f32_rows = 32;; a.f32_rows = 16) {
       a.units = 0;
       for (int32_t r = 0; r < num_requests; ++r)
         a.units += (int64_t)prompt_tiles(token_indptr_host[r + 1] - token_indptr_host[r], a.group, a.f32_rows) * num_kv_heads;
-      if (a.units >= 1024 || a.f32_rows == 16) break;
+      if (a.units >= 2048 || a.f32_rows == 16) break;
     }
     PromptPlan tiles;
     tiles.units = a.units;
