@@ -121,3 +121,55 @@ def test_decode_pages_missing_in_long_contexts(ada, dtype):
             t[1, e] = -1 if e % 2 else c.pages
         return t
     decode(ada, 17, [20, 9700, 300], hq=4, hkv=1, dtype=dtype, table=holes)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pools_beyond_4_gib(ada, dtype):
+    """Pages at the far end of pools of more than 2^32 bytes: what is appended there and read back by prompts and single
+    tokens equals the same on the first pages, bit for bit."""
+    import torch
+    hq, hkv, d, new, ctx = 16, 8, 128, [40, 1], [70, 33]
+    size = 2 if dtype == "bf16" else 4
+    pages = 2 ** 32 // (hkv * PS * d * size) + 2000
+    rng = np.random.default_rng(20)
+    before = np.asarray(ctx) - new
+    need = [-(-c // PS) for c in ctx]
+    indptr = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T = int(indptr[-1])
+    x = to_dev(typed(rng.standard_normal((T, hq + 2 * hkv, d)), dtype))
+    old = [to_dev(typed(rng.standard_normal((sum(need), hkv, PS, d)), dtype)) for _ in range(2)]
+    lens32, before32 = np.asarray(ctx, np.int32), before.astype(np.int32)
+    pools = [torch.empty((pages, hkv, PS, d), dtype=x.dtype, device="cuda") for _ in range(2)]
+    outs = []
+    for first in (0, pages - sum(need)):
+        table = np.full((2, max(need) + 1), -1, np.int32)
+        at = first
+        for r, n in enumerate(need):
+            table[r, :n] = np.arange(at, at + n)
+            at += n
+        for pool, rows in zip(pools, old):
+            pool[first:first + sum(need)] = rows
+        table = to_dev(table)
+        q = torch.empty((T, hq, d), dtype=x.dtype, device="cuda")
+        grown = torch.empty(2, dtype=torch.int32, device="cuda")
+        print("pools", dtype, "pages from", first, flush=True)
+        ada.adaserve_rope_append_kv(token_indptr=to_dev(indptr), prefix_len=to_dev(before32), q=x[:, :hq], k=x[:, hq:hq + hkv],
+                                    v=x[:, hq + hkv:], inv_freq=to_dev(np.ones(d // 2, np.float32)), q_out=q,
+                                    k_pages=pools[0], v_pages=pools[1], block_table=table, new_prefix_len=grown)
+        assert grown.tolist() == ctx
+        kind = ada.ADASERVE_BF16 if dtype == "bf16" else ada.ADASERVE_F32
+        prompts, singles = torch.empty_like(q), torch.empty_like(q[:2])
+        for bytes_, call in (
+                (ada.adaserve_prompt_attn_workspace_bytes(indptr, lens32, hq, hkv, d, PS, kind),
+                 lambda ws: ada.adaserve_prompt_attn(
+                     token_indptr=to_dev(indptr), token_indptr_host=indptr, q=q, k_pages=pools[0], v_pages=pools[1],
+                     block_table=table, context_len=grown, context_len_host=lens32, sm_scale=d ** -0.5, out=prompts, workspace=ws)),
+                (ada.adaserve_decode_attn_workspace_bytes(2, 96, hq, hkv, d, PS, kind),
+                 lambda ws: ada.adaserve_decode_attn(
+                     q=q[:2], k_pages=pools[0], v_pages=pools[1], block_table=torch.cat([table, table], 1), context_len=grown,
+                     max_context=96, sm_scale=d ** -0.5, out=singles, workspace=ws))):
+            call(torch.empty(max(bytes_, 1), dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        outs.append([test_gpu_paged_attention.back(t).tobytes() for t in
+                     (prompts, singles, pools[0][first:first + sum(need)], pools[1][first:first + sum(need)])])
+    assert outs[0] == outs[1]

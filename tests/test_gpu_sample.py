@@ -197,3 +197,20 @@ def test_sample_replayed_from_a_graph(ada):
         par = {n: np.asarray(a, np.int32 if n == "top_k" else np.float32) for n, a in par.items()}
         assert back(out).tolist() == serving.sample(host, v, u=uu, **par).tolist(), rep
         draw(ada, typed(rng.standard_normal((3, 4000)), "f32"), 4000, rng.random(3))
+
+
+def test_sample_rows_beyond_4_gib(ada):
+    """Rows 2^28 fp32 elements apart: the last begins 9 GiB after the first."""
+    import torch
+    rng = np.random.default_rng(23)
+    rows, vocab, step = 10, 5000, 2 ** 28
+    x = typed(rng.standard_normal((rows, vocab)) * 3, "f32")
+    far = torch.empty((rows - 1) * step + vocab, device="cuda").as_strided((rows, vocab), (step, 1))
+    far.copy_(to_dev(x))
+    u = rng.random(rows).astype(np.float32)
+    out = torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+    ws = torch.empty(ada.adaserve_sample_workspace_bytes(rows, vocab, ada.ADASERVE_F32), dtype=torch.uint8, device="cuda")
+    print("sample rows far apart", flush=True)
+    ada.adaserve_sample(logits=far, vocab=vocab, u=to_dev(u), out_token=out, workspace=ws)
+    torch.cuda.synchronize()
+    assert back(out).tolist() == serving.sample(x, vocab, u=u).tolist()
