@@ -451,7 +451,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
 // Joins the runs of a request's row: with reference m over the runs' m_c,
 // out = sum 2^(m_c - m) o_c / sum 2^(m_c - m) l_c.  One workgroup per row, its
 // four waves taking every fourth run, eight of them in flight (47 runs of a request
-// of 6000 tokens: 6.7 -> 4.0 us).
+// of 6000 tokens: 6.7 -> 3.7 us).
 template <bool BF16, int D>
 __global__ __launch_bounds__(kThreads) void decode_join_kernel(PagedAttnArgs a) {
   constexpr int EPL = D / 64;
@@ -469,17 +469,19 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(PagedAttnArgs a) 
     float x[kRuns][EPL];
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
-      const int c = min(c0 + i * kWaves, chunks - 1);
-      const int64_t slot = (int64_t)(2 * (first + c) + (c == 0)) * a.num_q_heads + h;
-      ml[i] = *(const f32x2 *)(a.ws_ml + slot * 2);
+      const int c = __builtin_amdgcn_readfirstlane(c0 + i * kWaves);
+      ml[i] = f32x2{kLowest, 0.f};
 #pragma unroll
-      for (int e = 0; e < EPL; ++e) x[i][e] = a.ws_o[slot * D + lane * EPL + e];
+      for (int e = 0; e < EPL; ++e) x[i][e] = 0.f;
+      if (c < chunks) {
+        const int64_t slot = (int64_t)(2 * (first + c) + (c == 0)) * a.num_q_heads + h;
+        ml[i] = *(const f32x2 *)(a.ws_ml + slot * 2);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) x[i][e] = a.ws_o[slot * D + lane * EPL + e];
+      }
     }
 #pragma unroll
-    for (int i = 0; i < kRuns; ++i) {
-      if (c0 + i * kWaves >= chunks) ml[i] = f32x2{kLowest, 0.f};
-      m = fmaxf(m, ml[i][0]);
-    }
+    for (int i = 0; i < kRuns; ++i) m = fmaxf(m, ml[i][0]);
     // (the sums so far have reference m_sum)
     const float f = __builtin_amdgcn_exp2f(m_sum - m);
     m_sum = m;
@@ -488,10 +490,10 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(PagedAttnArgs a) 
     for (int e = 0; e < EPL; ++e) o[e] *= f;
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
-      const float w = c0 + i * kWaves < chunks ? __builtin_amdgcn_exp2f(ml[i][0] - m) : 0.f;
+      const float w = __builtin_amdgcn_exp2f(ml[i][0] - m);
       l = __builtin_fmaf(w, ml[i][1], l);
 #pragma unroll
-      for (int e = 0; e < EPL; ++e) o[e] = c0 + i * kWaves < chunks ? __builtin_fmaf(w, x[i][e], o[e]) : o[e];
+      for (int e = 0; e < EPL; ++e) o[e] = __builtin_fmaf(w, x[i][e], o[e]);
     }
   }
   if (lane == 0) sm[wave] = m, sl[wave] = l;
