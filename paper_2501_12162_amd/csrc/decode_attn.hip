@@ -69,7 +69,7 @@ __device__ __forceinline__ int32_t decode_blocks(int32_t len) { return len > 0 ?
 // in all); start[] gets each request's first block, len[] its length (-1: out of
 // range).  False: no such unit.
 __device__ __forceinline__ bool schedule(const PagedAttnArgs &a, int32_t u, int32_t *start, int32_t *len, DecodeUnit &un) {
-  __shared__ int32_t part[kWaves];
+  __shared__ int32_t part[2][kWaves];
   __shared__ int32_t first;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per_thread = (a.num_requests + kThreads - 1) / kThreads;
@@ -85,27 +85,48 @@ __device__ __forceinline__ bool schedule(const PagedAttnArgs &a, int32_t u, int3
     }
     mine += nb[i];
   }
-  int32_t upto = mine;
+  // the sum over the threads before, and over all
+  auto scan = [&](int32_t *parts, int32_t x, int32_t &total) {
+    int32_t upto = x;
 #pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int32_t o = __shfl_up(upto, off, 64);
-    if (lane >= off) upto += o;
-  }
-  if (lane == 63) part[wave] = upto;
-  __syncthreads();
-  int32_t total = 0;
+    for (int off = 1; off < 64; off <<= 1) {
+      const int32_t o = __shfl_up(upto, off, 64);
+      if (lane >= off) upto += o;
+    }
+    if (lane == 63) parts[wave] = upto;
+    __syncthreads();
+    total = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) upto += part[w];
-    total += part[w];
-  }
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) upto += parts[w];
+      total += parts[w];
+    }
+    return upto - x;
+  };
+  int32_t total, at = scan(part[0], mine, total);
   un.per = max(a.min_blocks, (total + a.units_per_head - 1) / a.units_per_head);
+  // Where there are units for it every request begins with one of its own: a unit
+  // of two requests takes their runs one after the other (4 requests of 1500
+  // tokens, which do not fill the device: 14.3 -> 13.0 us; finding out costs 0.3
+  // to 0.5 us, so it is asked only where there are two units per request).
+  int32_t step = 1;   // requests begin at multiples of it
+  if (a.num_requests > 1 && 2 * a.num_requests <= a.units_per_head) {
+    int32_t apart = 0, all;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) apart += (nb[i] + un.per - 1) / un.per * un.per;
+    const int32_t from = scan(part[1], apart, all);
+    if (all <= a.units_per_head * un.per) {
+      step = un.per;
+      at = from;
+      total = all;
+    }
+  }
+  auto space = [&](int32_t n) { return (n + step - 1) / step * step; };
   const int32_t units = max(1, (total + un.per - 1) / un.per);
   if (u >= units) return false;
   un.lo = u * un.per;
   un.hi = min(total, un.lo + un.per);
   un.last = u == units - 1;
-  int32_t at = upto - mine;
   // `first`: the one request that is the unit's where the one before is not.  A
   // request with blocks is if it ends behind lo, an empty one from lo on.
   auto is_in = [&](int32_t from, int32_t n) { return n > 0 ? from + n > un.lo : from >= un.lo; };
@@ -115,16 +136,16 @@ __device__ __forceinline__ bool schedule(const PagedAttnArgs &a, int32_t u, int3
     if (i < per_thread && r < a.num_requests) {
       start[r] = at;
       if (is_in(at, nb[i])) {
-        // (the request before: its blocks end at `at`)
+        // (the request before: its space ends at `at`)
         bool before = false;
-        if (i > 0) before = is_in(at - nb[i - 1], nb[i - 1]);
+        if (i > 0) before = is_in(at - space(nb[i - 1]), nb[i - 1]);
         else if (r > 0) {
           const int32_t x = a.context_len[r - 1], n = decode_blocks(x <= a.max_context ? x : -1);
-          before = is_in(at - n, n);
+          before = is_in(at - space(n), n);
         }
         if (!before) first = r;
       }
-      at += nb[i];
+      at += space(nb[i]);
     }
   }
   __syncthreads();

@@ -121,7 +121,7 @@ inline DecodePlan decode_plan(int32_t B, int32_t hq, int32_t hkv, int32_t head_d
   p.units_per_head = B;
   if (p.split) {
     int64_t units = kDecodeUnits / hkv;
-    const int64_t most = (B * blocks + kDecodeMinBlocks - 1) / kDecodeMinBlocks;
+    const int64_t most = B * ((blocks + kDecodeMinBlocks - 1) / kDecodeMinBlocks);
     if (units > most) units = most;
     if (units < 1) units = 1;
     p.units_per_head = (int32_t)units;
