@@ -14,9 +14,9 @@
 // after one exchange of halves.  Weights are rounded to bf16 for that product (the
 // output is, too); their sum is of the unrounded ones.
 //
-// Measured, bf16, D = 128, 32 heads on 8: one prompt of 8191 tokens 455 - 468 us,
-// 1.18 - 1.21 PFLOP/s of the pairs seen (a library product of 8192 x 8192 x 8192
-// runs at 1.16); 16 ragged prompts of 512 - 2048 tokens 372 - 381 us, 0.81 PFLOP/s:
+// Measured, bf16, D = 128, 32 heads on 8: one prompt of 8191 tokens 454 - 473 us,
+// 1.16 - 1.21 PFLOP/s of the pairs seen (a library product of 8192 x 8192 x 8192
+// runs at 1.16); 16 ragged prompts of 512 - 2048 tokens 372 - 384 us, 0.81 PFLOP/s:
 // a tile's start, masked end and output take 19 thousand cycles, as long as 900
 // keys.  fp32, D = 64, 3 prompts of up to 700 tokens, 8 on 8 heads: 19.5 us.
 #include <type_traits>
