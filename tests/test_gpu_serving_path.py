@@ -236,3 +236,24 @@ def test_prompt_attention_from_a_graph(ada, new, ctx):
     ref, size, reach = serving.paged_attention(x, indptr, c.k, c.v, c.table, ctx, d ** -0.5)
     err = np.abs(serving.widen(back(out)) - ref)
     assert (err <= attention_bound("bf16", ref, size, reach, int(ctx.max()), d)).all()
+
+
+def test_stream_given_by_the_caller(ada):
+    """`stream=` puts the work on that stream, behind what waits there."""
+    import torch
+    s = Server(ada, 15, [200, 9], "bf16")
+    s.prefill()
+    s.step()
+    torch.cuda.synchronize()
+    out, token = torch.zeros_like(s.out), torch.full_like(s.token, -7)
+    side = torch.cuda.Stream()
+    q = torch.zeros_like(s.q)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2_000_000)   # about a millisecond
+        q.copy_(s.q)
+    ada.adaserve_decode_attn(q=q, k_pages=s.kp, v_pages=s.vp, block_table=s.table, context_len=s.lens, max_context=s.most,
+                             sm_scale=s.scale, out=out, workspace=s.ws_decode, stream=side)
+    ada.adaserve_sample(logits=out.reshape(s.B, -1), vocab=s.vocab, u=s.u, out_token=token, workspace=s.ws_sample, stream=side,
+                        **s.par_dev)
+    side.synchronize()
+    assert back(out).tobytes() == back(s.out).tobytes() and token.tolist() == s.token.tolist()
