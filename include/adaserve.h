@@ -504,7 +504,9 @@ int32_t adaserve_rope_append_kv(int32_t num_requests, int32_t num_tokens, const 
  * are never read into the result; a key that a row does not see adds nothing to
  * it, whatever key and value it holds.
  * Block-table entries outside [0, num_pages) are all-zero pages.
- * Scores are to be below 2^29 in magnitude.
+ * Scores are to be below 2^29 in magnitude, and the values that a row sees
+ * finite (0 * Inf is NaN), with |value| * c below 2^118: sums over the keys are
+ * taken in fp32, of weights up to 2^8.
  * token_indptr_host and context_len_host mirror the device arrays.  T * Hq <
  * 2^31.  workspace: at least adaserve_prompt_attn_workspace_bytes(...) bytes
  * (0 for most batches; 256-byte aligned, no initialisation needed); calls that

@@ -152,8 +152,11 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   // 32 keys: bf16 and fp32 are as precise at 2^60 as at 1, so no maximum is taken
   // per sub-block.  A row whose sum gets beyond kMost is one whose scores
   // rise by more than 44 nats over those of its first keys; its tile is done
-  // again with the maximum taken everywhere.
-  constexpr float kMost = 0x1p64f;
+  // again with the maximum taken everywhere.  So is that of a row whose weights
+  // reach further than with maxima (2^8 per key) and whose products with the values
+  // get beyond kMostOut: |value| * keys < 2^118 keeps both ways' sums, and those
+  // of their joined chunks, within fp32.
+  constexpr float kMost = 0x1p64f, kMostOut = 0x1p120f;
   __shared__ int redo;
   __shared__ __align__(1024) char ring[NST * STAGE];   // (K of sub-block 0: in the last stage at first)
 
@@ -526,8 +529,20 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
       }
       any_sub(i++);
     }
-    const bool beyond = !(lsum[0] < kMost) || !(lsum[1] < kMost);
-    if (!careful && __any(beyond) && lane == 0) redo = 1;
+    if (!careful) {
+      bool beyond = !(lsum[0] < kMost) || !(lsum[1] < kMost);
+      // (rarely: 2 x 16 DT comparisons)
+      const float fair = 0x1p8f * (float)k_end;
+      if (__any(fmaxf(lsum[0], lsum[1]) > fair)) {
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) beyond = beyond || !(fabsf(o[rt][dt][j]) < kMostOut);
+      }
+      if (__any(beyond) && lane == 0) redo = 1;
+    }
     __syncthreads();   // every wave is done with the ring, too
     if (redo) {
       __syncthreads();
