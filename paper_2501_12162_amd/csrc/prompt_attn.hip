@@ -19,6 +19,8 @@
 // runs at 1.16); 16 ragged prompts of 512 - 2048 tokens 372 - 384 us, 0.81 PFLOP/s:
 // a tile's start, masked end and output take 19 thousand cycles, as long as 900
 // keys.  fp32, D = 64, 3 prompts of up to 700 tokens, 8 on 8 heads: 19.5 us.
+#include <float.h>
+
 #include <type_traits>
 
 #include "device_common.h"
@@ -279,7 +281,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   }
 
   f32x16 o[2][DT];
-  const float c = a.scale_log2, up_raw = kRescaleLog2 / c;
+  // References are in units of q k; before any key -1e30 in log2 units, below
+  // every score whatever the scale.
+  const float c = a.scale_log2, up_raw = kRescaleLog2 / c, lowest = fmaxf(-1e30f / c, -FLT_MAX);
   float lsum[2], m_ref[2];
 
   bf16x8 kf[KS], vf[2 * DT];
@@ -474,7 +478,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
       lsum[rt] = 0.f;
-      m_ref[rt] = -1e30f;
+      m_ref[rt] = lowest;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[rt][dt] = f32x16{};
     }

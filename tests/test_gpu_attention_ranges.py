@@ -55,3 +55,16 @@ def test_prompt_values_at_the_documented_size(ada, new, ctx, split):  # noqa: F8
     c.v = typed(np.full(c.v.shape, 2.0 ** 118 / (ctx[0] + 1), np.float32), "bf16")
     got = run_prompt(ada, q, new, ctx, c, "bf16", 128 ** -0.5, split=split)
     check("prompt", got, q, new, ctx, c, "bf16", 128 ** -0.5)
+
+
+@pytest.mark.parametrize("new,ctx,split", [([200], [260], False), ([120], [4000], True)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prompt_far_scores_at_a_small_scale(ada, dtype, new, ctx, split):  # noqa: F811
+    """Queries and keys of 2^47 at a scale of 2^-90: every score is about -3100, and they differ by units."""
+    rng = np.random.default_rng(3)
+    d, scale = 128, 2.0 ** -90
+    c = Cache(rng, ctx, 2, d, dtype)
+    c.k = typed(-2.0 ** 47 * (1 + 2.0 ** -7 * rng.integers(0, 3, c.k.shape)), dtype)
+    q = typed(np.full((int(starts(new)[-1]), 8, d), 1.5 * 2.0 ** 47), dtype)
+    got = run_prompt(ada, q, new, ctx, c, dtype, scale, split=split if dtype == "bf16" else False)
+    check("prompt", got, q, new, ctx, c, dtype, scale)
