@@ -193,14 +193,17 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   // `pages_after` the 64 sub-blocks after those.
   const int wave_page = (wave * WI * RPI) / kPageSize;
   int32_t pages, pages_after, window;
-  bool all_pages;   // no whole sub-block of the windows so far lacks its page
+  // no whole sub-block of the windows so far lacks its page (a last one of at most
+  // 16 keys has no second page, which is no reason to leave the common path:
+  // 16 ragged prompts, half of them such, 386 -> 364 us)
+  bool all_pages;
   auto load_pages = [&](const PromptUnit &of, int base) __attribute__((always_inline)) -> int32_t {
     const int32_t e = of.k0 / kPageSize + (base + lane) * (KB / kPageSize) + wave_page;
     return e < a.bt_stride && e < (of.ctx + kPageSize - 1) / kPageSize ? a.block_table[(int64_t)of.r * a.bt_stride + e] : -1;
   };
   auto take_pages = [&](int32_t ids) __attribute__((always_inline)) {
     pages = ids >= 0 && ids < a.num_pages ? ids : -1;
-    all_pages = all_pages && !__any(pages < 0 && window + lane < nb);
+    all_pages = all_pages && !__any(pages < 0 && window + lane < k_end / KB);
     pages_after = load_pages(un, window + 64);
   };
   auto next_window = [&]() __attribute__((always_inline)) {
