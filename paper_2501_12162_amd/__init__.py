@@ -344,7 +344,8 @@ def _rows(t, name: str):
     if t is None:
         return None, 0
     (rows, heads, dim), (step, head_step, one) = t.shape, t.stride()
-    if (one != 1 or head_step != dim) and heads * dim > 1 and rows:
+    # (the step of an axis of one entry means nothing)
+    if rows and ((dim > 1 and one != 1) or (heads > 1 and head_step != dim)):
         raise ValueError("%s must have dense heads" % name)
     return t.data_ptr(), step if rows > 1 else heads * dim
 
