@@ -112,13 +112,14 @@ PromptPlan prompt_plan(int32_t num_requests, const int32_t *indptr, const int32_
   constexpr int32_t kLeastKeys = 256, kMostChunks = 64;
   const double key_us = 0.022 * head_dim / 128;
   PromptPlan p;
-  int32_t least = INT32_MAX, most = 0, keys = 0;
+  int32_t keys = 0;
+  int64_t least = INT32_MAX, most = 0;
   for (int32_t r = 0; r < num_requests; ++r) {
     const int32_t n = indptr[r + 1] - indptr[r];
     if (n == 0) continue;
     p.units += (int64_t)prompt_tiles(n, hq / hkv, kPromptTileRows) * hkv;
-    least = std::min(least, ctx[r] - n);
-    most = std::max(most, ctx[r] - n);
+    least = std::min<int64_t>(least, ctx[r] - n);
+    most = std::max<int64_t>(most, ctx[r] - n);
     keys = std::max(keys, ctx[r]);
   }
   p.in_order = most - least <= 128;

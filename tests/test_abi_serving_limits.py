@@ -1,0 +1,16 @@
+"""Sizes at the ends of what the serving operators take, on the host before any
+HIP call: workspaces that do not hold what the kernels write, and counts whose
+sums leave 32 bits or one launch."""
+import numpy as np
+import pytest
+
+import paper_2501_12162_amd as ada
+from test_abi_serving import BAD, FAKE, SIZE_MAX, UNSUP, WS, _append, _decode, _prompt, _sample, lib  # noqa: F401
+
+INT_MAX = 2 ** 31 - 1
+
+
+def test_prompt_workspace_query_of_the_most_rows(lib):  # noqa: F811
+    """2^31 - 1 rows, some of them far before their request's keys, others far behind."""
+    ip, ctx = np.asarray([0, INT_MAX - 1, INT_MAX], np.int32), np.asarray([0, 2 ** 23 - 1], np.int32)
+    assert lib.adaserve_prompt_attn_workspace_bytes(2, ip.ctypes.data, ctx.ctypes.data, 1, 1, 128, 16, ada.ADASERVE_BF16) == 0
