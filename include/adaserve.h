@@ -440,6 +440,7 @@ int32_t adaserve_tree_accept_sampled(int32_t num_requests, int32_t total_nodes,
  * Token packing: request r owns the token rows [token_indptr[r],
  * token_indptr[r+1]), of any number, 0 among them; rows past the last request's
  * (padding of a batch) are neither read nor written.
+ * Rows given with a stride span at most 2^48 elements.
  */
 
 /*

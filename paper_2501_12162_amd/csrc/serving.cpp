@@ -53,13 +53,22 @@ int32_t validate_paged(int32_t num_requests, int32_t num_pages, int32_t bt_strid
   return ADASERVE_OK;
 }
 
-// Query rows of `heads` heads, `stride` elements apart, readable in 16-byte pieces.
-int32_t validate_rows(const char *name, const void *p, int64_t stride, int64_t row, int32_t esz) {
+// `rows` rows `stride` elements apart stay within what a pointer reaches (and their byte count within 64 bits).
+int32_t validate_span(const char *name, int64_t rows, int64_t stride) {
+  constexpr int64_t kMostElements = (int64_t)1 << 48;
+  if (rows > 1 && stride > kMostElements / (rows - 1))
+    return fail(ADASERVE_ERR_UNSUPPORTED, "%s: %lld rows %lld elements apart span more than 2^48 elements", name,
+                (long long)rows, (long long)stride);
+  return ADASERVE_OK;
+}
+
+// `rows` rows of `row` elements, `stride` elements apart, readable in 16-byte pieces.
+int32_t validate_rows(const char *name, const void *p, int64_t rows, int64_t stride, int64_t row, int32_t esz) {
   if (stride < row) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "%s_row_stride %lld < %lld", name, (long long)stride, (long long)row);
   if (stride > (int64_t)1 << 40) return fail(ADASERVE_ERR_UNSUPPORTED, "%s_row_stride %lld > 2^40", name, (long long)stride);
   if (!aligned(p, 16) || (stride * esz) % 16 != 0)
     return fail(ADASERVE_ERR_INVALID_ARGUMENT, "%s must be 16-byte aligned with rows a multiple of 16 bytes apart", name);
-  return ADASERVE_OK;
+  return validate_span(name, rows, stride);
 }
 
 // Shape checks of prompt attention that the workspace query shares.
@@ -278,15 +287,15 @@ int32_t adaserve_rope_append_kv(int32_t num_requests, int32_t num_tokens, const 
     if (k_out && !k) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "k_out needs k");
     if (k && !k_out && !append) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "k has neither k_out nor pages to go to");
     if (q) {
-      const int32_t st = validate_rows("q", q, q_row_stride, q_row, esz);
+      const int32_t st = validate_rows("q", q, num_tokens, q_row_stride, q_row, esz);
       if (st != ADASERVE_OK) return st;
     }
     if (k) {
-      const int32_t st = validate_rows("k", k, k_row_stride, kv_row, esz);
+      const int32_t st = validate_rows("k", k, num_tokens, k_row_stride, kv_row, esz);
       if (st != ADASERVE_OK) return st;
     }
     if (append) {
-      const int32_t st = validate_rows("v", v, v_row_stride, kv_row, esz);
+      const int32_t st = validate_rows("v", v, num_tokens, v_row_stride, kv_row, esz);
       if (st != ADASERVE_OK) return st;
     }
     // an output is its own input or apart from every input
@@ -357,7 +366,7 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
   if (total == 0) return ADASERVE_OK;
   if (!token_indptr || !q || !out || !context_len)
     return fail(ADASERVE_ERR_INVALID_ARGUMENT, "a required device pointer is NULL");
-  st = validate_rows("q", q, q_row_stride, (int64_t)num_q_heads * head_dim, elem_size(dtype));
+  st = validate_rows("q", q, total, q_row_stride, (int64_t)num_q_heads * head_dim, elem_size(dtype));
   if (st != ADASERVE_OK) return st;
   if (!aligned(out, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "out must be 16-byte aligned");
   st = validate_pages(most > 0, k_pages, v_pages, num_pages, block_table);
@@ -426,7 +435,7 @@ int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_
   if (st != ADASERVE_OK) return st;
   if (num_requests == 0) return ADASERVE_OK;
   if (!q || !out || !context_len) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "a required device pointer is NULL");
-  st = validate_rows("q", q, q_row_stride, (int64_t)num_q_heads * head_dim, elem_size(dtype));
+  st = validate_rows("q", q, num_requests, q_row_stride, (int64_t)num_q_heads * head_dim, elem_size(dtype));
   if (st != ADASERVE_OK) return st;
   if (!aligned(out, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "out must be 16-byte aligned");
   st = validate_pages(max_context > 0, k_pages, v_pages, num_pages, block_table);
@@ -482,6 +491,8 @@ int32_t adaserve_sample(const void *logits, int64_t row_stride, int32_t num_rows
   if (!aligned(logits, elem_size(dtype)) || !aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) ||
       !aligned(min_p, 4) || !aligned(u, 4) || !aligned(out_token, 4))
     return fail(ADASERVE_ERR_INVALID_ARGUMENT, "a pointer is not aligned to its elements");
+  st = validate_span("logits", num_rows, row_stride);
+  if (st != ADASERVE_OK) return st;
   const SamplePlan plan = sample_plan(num_rows, vocab, dtype == ADASERVE_BF16);
   st = validate_workspace(workspace, workspace_bytes, plan.bytes);
   if (st != ADASERVE_OK) return st;

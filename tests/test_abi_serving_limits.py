@@ -14,3 +14,16 @@ def test_prompt_workspace_query_of_the_most_rows(lib):  # noqa: F811
     """2^31 - 1 rows, some of them far before their request's keys, others far behind."""
     ip, ctx = np.asarray([0, INT_MAX - 1, INT_MAX], np.int32), np.asarray([0, 2 ** 23 - 1], np.int32)
     assert lib.adaserve_prompt_attn_workspace_bytes(2, ip.ctypes.data, ctx.ctypes.data, 1, 1, 128, 16, ada.ADASERVE_BF16) == 0
+
+
+def test_rows_whose_span_leaves_the_address_space(lib):  # noqa: F811
+    """Spans of 2^31 rows at the largest stride, whose byte count is beyond 64 bits: refused, not wrapped into a range that
+    overlaps nothing (or something)."""
+    far = 2 ** 40
+    assert _append(lib, T=INT_MAX, qs=far) == UNSUP
+    assert _append(lib, T=INT_MAX, ks=far, q=None, qo=None) == UNSUP
+    assert _append(lib, T=INT_MAX, vs=far) == UNSUP
+    assert _append(lib, T=2 ** 9, qs=far) == UNSUP          # 2^49 elements
+    assert _prompt(lib, ip=[0, 2 ** 27, 2 ** 27], qs=far) == UNSUP
+    assert _decode(lib, B=2 ** 24, qs=far) == UNSUP
+    assert _sample(lib, rows=2 ** 20, stride=2 ** 62) == UNSUP
