@@ -440,7 +440,11 @@ int32_t adaserve_tree_accept_sampled(int32_t num_requests, int32_t total_nodes,
  * Token packing: request r owns the token rows [token_indptr[r],
  * token_indptr[r+1]), of any number, 0 among them; rows past the last request's
  * (padding of a batch) are neither read nor written.
- * Rows given with a stride span at most 2^48 elements.
+ * Rows given with a stride span at most 2^48 elements.  A launch has fewer than
+ * 2^32 threads, so num_tokens + num_requests / 4 of an append, num_requests * Hkv
+ * of single tokens, the tiles of prompts (a request's rows by 16 or more, per
+ * kv-head) and the row parts of sampling (4096 logits or more) stay below 2^24,
+ * sampled rows below 2^22; calls beyond are refused (ADASERVE_ERR_UNSUPPORTED).
  */
 
 /*

@@ -48,7 +48,7 @@ namespace adaserve {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kServingThreads;
 constexpr int kWaves = kThreads / 64;
 constexpr float kLowest = -FLT_MAX;     // running maximum before any key
 constexpr float kRescaleLog2 = 8.f;
@@ -541,7 +541,6 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(PagedAttnArgs a) 
 template <bool BF16, int D>
 hipError_t launch(const PagedAttnArgs &a, hipStream_t stream) {
   const int64_t blocks = (int64_t)a.units_per_head * a.num_kv_heads;
-  if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((decode_attn_kernel<BF16, D>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.ws_request) return e;

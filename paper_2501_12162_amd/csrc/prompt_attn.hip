@@ -33,7 +33,7 @@ namespace adaserve {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kServingThreads;
 constexpr int kWaves = 4;
 constexpr int kTileRows = kPromptTileRows;
 

@@ -30,7 +30,7 @@ namespace adaserve {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kServingThreads;
 
 // The request that owns token t: the last r with indptr[r] <= t, by the whole
 // wave (64 entries per round of loads).  -1 when t is in no request.
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeAppendArgs a,
 }  // namespace
 
 hipError_t launch_rope_append(const RopeAppendArgs &a, bool bf16, hipStream_t stream) {
-  const int64_t length_blocks = a.new_prefix_len ? (a.num_requests + 3) / 4 : 0;
+  const int64_t length_blocks = a.new_prefix_len ? rope_length_blocks(a.num_requests) : 0;
   const bool in_place = a.new_prefix_len && a.new_prefix_len == a.prefix_len;
   auto run = [&](int32_t tokens, int64_t blocks) {
     if (blocks == 0) return hipSuccess;

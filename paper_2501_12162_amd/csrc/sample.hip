@@ -41,8 +41,8 @@ namespace adaserve {
 
 namespace {
 
-constexpr int kThreads = 256;          // of passes 1 to 3
-constexpr int kDrawThreads = 1024;
+constexpr int kThreads = kServingThreads;          // of passes 1 to 3
+constexpr int kDrawThreads = kSampleDrawThreads;
 constexpr int kBins = kSampleBins;
 constexpr double kUnit = 4294967296.0;
 // Bins 0 .. 510 cover -z log2 e in [0, 33.01), where masses can be 1 or more;

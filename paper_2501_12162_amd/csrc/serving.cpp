@@ -53,6 +53,14 @@ int32_t validate_paged(int32_t num_requests, int32_t num_pages, int32_t bt_strid
   return ADASERVE_OK;
 }
 
+// HIP launches fewer than 2^32 threads.
+int32_t validate_launch(const char *what, int64_t blocks, int64_t threads) {
+  if (blocks * threads >> 32)
+    return fail(ADASERVE_ERR_UNSUPPORTED, "%s: %lld workgroups of %lld threads exceed a launch", what, (long long)blocks,
+                (long long)threads);
+  return ADASERVE_OK;
+}
+
 // `rows` rows `stride` elements apart stay within what a pointer reaches (and their byte count within 64 bits).
 int32_t validate_span(const char *name, int64_t rows, int64_t stride) {
   constexpr int64_t kMostElements = (int64_t)1 << 48;
@@ -207,7 +215,7 @@ int32_t validate_workspace(const void *workspace, size_t given, size_t need) {
   return ADASERVE_OK;
 }
 
-int32_t validate_decode(int32_t num_requests, int32_t hq, int32_t max_context, int32_t bt_stride_or_neg) {
+int32_t validate_decode(int32_t num_requests, int32_t hq, int32_t hkv, int32_t max_context, int32_t bt_stride_or_neg) {
   if (max_context < 0) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "max_context %d < 0", max_context);
   if (max_context > kMaxPrefixLen) return fail(ADASERVE_ERR_UNSUPPORTED, "max_context %d > %d", max_context, kMaxPrefixLen);
   if (bt_stride_or_neg >= 0 && ceil_div(max_context, kPageSize) > bt_stride_or_neg)
@@ -215,19 +223,20 @@ int32_t validate_decode(int32_t num_requests, int32_t hq, int32_t max_context, i
                 ceil_div(max_context, kPageSize), bt_stride_or_neg);
   if ((int64_t)num_requests * hq > INT32_MAX)
     return fail(ADASERVE_ERR_UNSUPPORTED, "%d requests of %d query heads exceed 2^31 - 1 rows", num_requests, hq);
-  return ADASERVE_OK;
+  // (one workgroup each at most, and per query head in the join, of at most kDecodeSplitRequests)
+  return validate_launch("decode attention", (int64_t)num_requests * hkv, kServingThreads);
 }
 
 int32_t validate_sample(int32_t num_rows, int32_t vocab, int32_t dtype) {
   if (num_rows < 0) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "num_rows %d < 0", num_rows);
-  if (num_rows > INT32_MAX / kSampleMaxParts)
-    return fail(ADASERVE_ERR_UNSUPPORTED, "num_rows %d > %d", num_rows, INT32_MAX / kSampleMaxParts);
   if (vocab < 1 || vocab > kSampleMaxVocab)
     return fail(vocab < 1 ? ADASERVE_ERR_INVALID_ARGUMENT : ADASERVE_ERR_UNSUPPORTED, "vocab %d outside [1, %d]",
                 vocab, kSampleMaxVocab);
   if (dtype != ADASERVE_F32 && dtype != ADASERVE_BF16)
     return fail(ADASERVE_ERR_INVALID_ARGUMENT, "dtype %d is neither F32 nor BF16", dtype);
-  return ADASERVE_OK;
+  const int64_t parts = sample_plan(num_rows, vocab, dtype == ADASERVE_BF16).parts;
+  const int32_t st = validate_launch("sampling", num_rows * parts, kServingThreads);
+  return st != ADASERVE_OK ? st : validate_launch("sampling", num_rows, kSampleDrawThreads);
 }
 
 }  // namespace
@@ -307,7 +316,11 @@ int32_t adaserve_rope_append_kv(int32_t num_requests, int32_t num_tokens, const 
         overlap(ko, qi) || overlap(ko, vi) || overlap(qo, ko))
       return fail(ADASERVE_ERR_INVALID_ARGUMENT, "q_out or k_out overlaps an input without being it (dense rows), or the other");
   }
-  const int32_t st = check_device();
+  const int64_t length_blocks = append ? rope_length_blocks(num_requests) : 0;
+  int32_t st = validate_launch("rotary append", new_prefix_len == prefix_len ? std::max<int64_t>(num_tokens, length_blocks)
+                                                                              : num_tokens + length_blocks, kServingThreads);
+  if (st != ADASERVE_OK) return st;
+  st = check_device();
   if (st != ADASERVE_OK) return st;
   RopeAppendArgs a{};
   a.num_requests = num_requests;
@@ -375,8 +388,6 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
                                       head_dim, dtype == ADASERVE_BF16);
   st = validate_workspace(workspace, workspace_bytes, plan.ws_bytes);
   if (st != ADASERVE_OK) return st;
-  st = check_device();
-  if (st != ADASERVE_OK) return st;
   PromptAttnArgs a{};
   a.num_requests = num_requests;
   a.token_indptr = token_indptr;
@@ -410,6 +421,11 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
     tiles.units = a.units;
     fill_prompt(a, tiles, token_indptr_host, context_len_host, a.f32_rows, nullptr);
   }
+  // (the join's rows: below 2^17, those of 512 tiles)
+  st = validate_launch("prompt attention", dtype == ADASERVE_BF16 ? a.grid : round_up(a.units, kPromptGrid), kServingThreads);
+  if (st != ADASERVE_OK) return st;
+  st = check_device();
+  if (st != ADASERVE_OK) return st;
   return launch_status(launch_prompt_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
                        "prompt attention launch");
 }
@@ -417,7 +433,7 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
 size_t adaserve_decode_attn_workspace_bytes(int32_t num_requests, int32_t max_context, int32_t num_q_heads,
                                             int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t dtype) {
   if (validate_paged(num_requests, 0, 0, num_q_heads, num_kv_heads, head_dim, page_size, 1.f, dtype) != ADASERVE_OK ||
-      validate_decode(num_requests, num_q_heads, max_context, -1) != ADASERVE_OK)
+      validate_decode(num_requests, num_q_heads, num_kv_heads, max_context, -1) != ADASERVE_OK)
     return SIZE_MAX;
   return decode_plan(num_requests, num_q_heads, num_kv_heads, head_dim, max_context).ws_bytes;
 }
@@ -431,7 +447,7 @@ int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_
   int32_t st = validate_paged(num_requests, num_pages, block_table_stride, num_q_heads, num_kv_heads, head_dim,
                               page_size, sm_scale, dtype);
   if (st != ADASERVE_OK) return st;
-  st = validate_decode(num_requests, num_q_heads, max_context, block_table_stride);
+  st = validate_decode(num_requests, num_q_heads, num_kv_heads, max_context, block_table_stride);
   if (st != ADASERVE_OK) return st;
   if (num_requests == 0) return ADASERVE_OK;
   if (!q || !out || !context_len) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "a required device pointer is NULL");

@@ -11,6 +11,8 @@
 namespace adaserve {
 
 constexpr int kMaxHeads = 4096;          // of one kind, in the serving operators
+constexpr int kServingThreads = 256;     // of a workgroup, but in sampling's last pass
+constexpr int kSampleDrawThreads = 1024;
 constexpr int kRopeMaxHeadDim = 512;
 
 struct RopeAppendArgs {
@@ -36,6 +38,9 @@ struct RopeAppendArgs {
   int32_t bt_stride;
   int32_t *new_prefix_len;       // [B], or null
 };
+
+// Workgroups that write the new lengths, a wave per request.
+inline int64_t rope_length_blocks(int32_t num_requests) { return ((int64_t)num_requests + 3) / 4; }
 
 hipError_t launch_rope_append(const RopeAppendArgs &a, bool bf16, hipStream_t stream);
 

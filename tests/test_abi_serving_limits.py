@@ -27,3 +27,20 @@ def test_rows_whose_span_leaves_the_address_space(lib):  # noqa: F811
     assert _prompt(lib, ip=[0, 2 ** 27, 2 ** 27], qs=far) == UNSUP
     assert _decode(lib, B=2 ** 24, qs=far) == UNSUP
     assert _sample(lib, rows=2 ** 20, stride=2 ** 62) == UNSUP
+
+
+def test_calls_of_more_threads_than_a_launch_takes(lib):  # noqa: F811
+    """HIP launches fewer than 2^32 threads: calls that would need more are refused before anything is enqueued."""
+    dense = dict(qs=64, ks=64, vs=64, hq=1, hkv=1, d=64, rot=64, qo=0x7000000000, kp=0x8000000000, vp=0x9000000000,
+                 q=0x1000000000, k=0x2000000000, v=0x3000000000)
+    assert _append(lib, T=2 ** 24, **dense) == UNSUP                       # a workgroup of 256 per token
+    assert _append(lib, B=2 ** 26, T=5, new=0x10000000000) == UNSUP        # and one per four requests' lengths
+    many = 2 ** 20                                                         # requests of a token: a workgroup each per kv-head
+    assert _prompt(lib, dtype=ada.ADASERVE_F32, ip=np.arange(many + 1), ctx=np.zeros(many), hq=16, hkv=16, d=64) == UNSUP
+    assert _prompt(lib, ip=np.arange(many + 1), ctx=np.zeros(many), hq=16, hkv=16, d=64) == UNSUP
+    assert _decode(lib, B=2 ** 24, hq=1, hkv=1, d=64, qs=64) == UNSUP      # a workgroup per request and kv-head
+    for rows in (2 ** 22, 2 ** 25):                                        # a workgroup of 1024 per row
+        assert _sample(lib, rows=rows, wsb=2 ** 60) == UNSUP
+        assert lib.adaserve_sample_workspace_bytes(rows, 100, ada.ADASERVE_F32) == SIZE_MAX
+    assert lib.adaserve_sample_workspace_bytes(2 ** 22 - 1, 100, ada.ADASERVE_F32) != SIZE_MAX
+    assert lib.adaserve_decode_attn_workspace_bytes(2 ** 24, 32, 1, 1, 64, 16, ada.ADASERVE_F32) == SIZE_MAX
