@@ -44,3 +44,31 @@ def test_calls_of_more_threads_than_a_launch_takes(lib):  # noqa: F811
         assert lib.adaserve_sample_workspace_bytes(rows, 100, ada.ADASERVE_F32) == SIZE_MAX
     assert lib.adaserve_sample_workspace_bytes(2 ** 22 - 1, 100, ada.ADASERVE_F32) != SIZE_MAX
     assert lib.adaserve_decode_attn_workspace_bytes(2 ** 24, 32, 1, 1, 64, 16, ada.ADASERVE_F32) == SIZE_MAX
+
+
+def _need_prompt(lib, ip, ctx):
+    ip, ctx = np.asarray(ip, np.int32), np.asarray(ctx, np.int32)
+    return lib.adaserve_prompt_attn_workspace_bytes(ctx.size, ip.ctypes.data, ctx.ctypes.data, 8, 2, 128, 16, ada.ADASERVE_BF16)
+
+
+def _workspace_cases(lib):
+    """Per entry point: its call with a workspace, the bytes it needs, and those of a smaller batch."""
+    prompt = dict(ip=[0, 64], ctx=[8064], bts=504)
+    yield (lambda **kw: _prompt(lib, **prompt, **kw), _need_prompt(lib, [0, 64], [8064]), _need_prompt(lib, [0, 64], [2000]))
+    decode = lambda B, most: lib.adaserve_decode_attn_workspace_bytes(B, most, 8, 2, 128, 16, ada.ADASERVE_BF16)
+    yield (lambda **kw: _decode(lib, B=3, most=4096, bts=256, **kw), decode(3, 4096), decode(3, 600))
+    sample = lambda rows, vocab: lib.adaserve_sample_workspace_bytes(rows, vocab, ada.ADASERVE_F32)
+    yield (lambda **kw: _sample(lib, rows=3, **kw), sample(3, 100), sample(2, 100))
+    yield (lambda **kw: _sample(lib, rows=3, vocab=20000, stride=20000, **kw), sample(3, 20000), sample(3, 4000))
+
+
+@pytest.mark.parametrize("which", range(4))
+def test_workspaces_that_are_missing_too_small_or_misaligned(lib, which):  # noqa: F811
+    call, need, smaller = list(_workspace_cases(lib))[which]
+    assert 0 < smaller < need < SIZE_MAX
+    at = FAKE * 256
+    assert call(ws=None, wsb=need) == WS and lib.adaserve_last_error()
+    assert call(ws=at, wsb=0) == WS
+    assert call(ws=at, wsb=need - 1) == WS
+    assert call(ws=at, wsb=smaller) == WS           # asked for a batch before this one
+    assert call(ws=at + 16, wsb=need) == BAD
