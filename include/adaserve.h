@@ -457,8 +457,9 @@ int32_t adaserve_tree_accept_sampled(int32_t num_requests, int32_t total_nodes,
  * positions[t] of its row t, or place where positions is NULL.  Pair j of a
  * head is columns (j, j + rotary_dim / 2), or (2j, 2j + 1) with interleaved = 1:
  *   y1 = x1 cos - x2 sin,  y2 = x1 sin + x2 cos;
- * columns from rotary_dim on are copied.  The angle is exact (fp64) at any
- * position, sine, cosine and rotation are fp32, rounded once to dtype.
+ * columns from rotary_dim on are copied.  The angle is taken in fp64 (within
+ * 2^-21 rad at any position for frequencies up to 1), sine, cosine and rotation
+ * are fp32, rounded once to dtype.
  *
  *   q [num_tokens, Hq, D], k, v [num_tokens, Hkv, D]: heads dense, rows
  *     *_row_stride elements apart (slices of one projection's rows can be given
@@ -512,10 +513,12 @@ int32_t adaserve_rope_append_kv(int32_t num_requests, int32_t num_tokens, const 
  * Scores are to be below 2^29 in magnitude, and the values that a row sees
  * finite (0 * Inf is NaN), with |value| * c below 2^118: sums over the keys are
  * taken in fp32, of weights up to 2^8.
- * token_indptr_host and context_len_host mirror the device arrays.  T * Hq <
- * 2^31.  workspace: at least adaserve_prompt_attn_workspace_bytes(...) bytes
- * (0 for most batches; 256-byte aligned, no initialisation needed); calls that
- * share one must not overlap in time.
+ * token_indptr_host and context_len_host mirror the device arrays; a captured
+ * call is replayed with the lengths of its capture (adaserve_decode_attn follows
+ * lengths on the device).  T * Hq < 2^31.  workspace: at least adaserve_prompt_attn_workspace_bytes(...) bytes
+ * (0 for most batches, and not bounded by another batch's: it depends on the
+ * lengths; 256-byte aligned, no initialisation needed); calls that share one must
+ * not overlap in time.
  */
 size_t adaserve_prompt_attn_workspace_bytes(int32_t num_requests, const int32_t *token_indptr_host,
                                             const int32_t *context_len_host, int32_t num_q_heads,

@@ -30,9 +30,10 @@
 //    only when it is exceeded by 2^8, which spares the rescaling of the output.
 //
 // Measured, bf16, D = 128 (a kernel that only reads gets 7.0 TB/s): 64 requests
-// of up to 4096 tokens, 64 on 8 heads, 668 MB: 110 us, 6.0 TB/s; 8 requests of
-// 32768 tokens, 32 on 8 heads, 1074 MB: 163 us, 6.6 TB/s; one of 1500 tokens: 7.5
-// us and 3.4 for the join.  With a unit per run of a request, two rounds of them,
+// of up to 4096 tokens, 64 on 8 heads, 668 MB: 111 us, 6.0 TB/s; 8 requests of
+// 32768 tokens, 32 on 8 heads, 1074 MB: 164 us, 6.5 TB/s; one of 1500 tokens: 6.4
+// us and 3.2 for the join.  fp32: 32 of the 64 requests 93 us, 5.8 TB/s, 4 of the 8
+// 165 us, 6.5 TB/s.  With a unit per run of a request, two rounds of them,
 // the first two took 124 and 169 us; with three workgroups per CU (168 registers,
 // 8 of them spilled) 130 and 185.  Loading a run's first block before the end of
 // the run before gains nothing: 111 and 166.

@@ -14,11 +14,13 @@
 // after one exchange of halves.  Weights are rounded to bf16 for that product (the
 // output is, too); their sum is of the unrounded ones.
 //
-// Measured, bf16, D = 128, 32 heads on 8: one prompt of 8191 tokens 454 - 473 us,
-// 1.16 - 1.21 PFLOP/s of the pairs seen (a library product of 8192 x 8192 x 8192
-// runs at 1.16); 16 ragged prompts of 512 - 2048 tokens 372 - 384 us, 0.81 PFLOP/s:
-// a tile's start, masked end and output take 19 thousand cycles, as long as 900
-// keys.  fp32, D = 64, 3 prompts of up to 700 tokens, 8 on 8 heads: 19.5 us.
+// Measured, bf16, D = 128, 32 heads on 8: one prompt of 8191 tokens 449 - 468 us
+// (over cards), 1.17 - 1.22 PFLOP/s of the pairs seen (a library product of 8192 x 8192
+// x 8192 runs at 1.16); 16 ragged prompts of 512 - 2048 tokens 354 - 369 us, 0.83 - 0.87
+// PFLOP/s: a tile's start, masked end and output take 8 us, as long as 300 keys of
+// the loop and a quarter of the whole (every tile but a workgroup's first waits for
+// all of its ring and for the stores of the one before).  fp32, D = 64, 3 prompts of
+// up to 700 tokens, 8 on 8 heads: 19.6 us.
 #include <float.h>
 
 #include <type_traits>
@@ -676,9 +678,13 @@ __global__ __launch_bounds__(kThreads) void prompt_join_kernel(PromptAttnArgs a)
 // so every lane loads 16 contiguous bytes of K and V straight into the operand
 // registers and P needs no exchange: slot q of QK step (c, e) is head-dim
 // element 16 c + 4 q + e, slot q of PV step e is key 4 q + e, and O^T tile (h, k)
-// holds the columns 64 h + 4 j + k.  Bound by the fp32 matrix rate (a sixteenth of
-// bf16's), so two row tiles share each operand only where there are enough tiles
-// to fill the device.
+// holds the columns 64 h + 4 j + k.  Every tile reads its keys for itself, one page
+// ahead, 8 flops a byte with 16 rows and 16 with 32, so two row tiles share each
+// operand where there are enough tiles to fill the device.  Bound by the fp32 matrix
+// rate (a sixteenth of bf16's) and the waits for those loads together: 2 prompts of
+// 1500 tokens (32 heads on 8, D = 128) 351 us, 105 TFLOP/s (a library product: 154),
+// matrix cores busy 0.70 of the time and 7.5 TB/s out of the L2s; the 3 prompts
+// above 0.41 and 8.6 TB/s.
 template <int D, int RB>
 __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArgs a) {
   constexpr int RT = 16 * RB;

@@ -21,7 +21,9 @@
 // Measured, bf16, D = 128, 32 + 8 + 8 heads: 9.6 thousand tokens of 8 prompts, 236 MB
 // read and written, 48 us, 4.9 TB/s, with inputs that no cache holds (a device
 // copy of 1 GiB runs at 5.0), 37 us when the caches hold some of them; 40 thousand
-// tokens 5.1 TB/s.  One token: 4.1 us in a graph.
+// tokens 5.1 TB/s.  fp32: 92 us, 5.1 TB/s.  One token: 4.1 us in a graph.  Few heads
+// leave most of a workgroup without a piece: 8 + 2 + 2 heads 18.5 us, 3.2 TB/s, 4 + 2 + 2 of
+// D = 64 16 us, 1.2 TB/s.
 #include "device_common.h"
 #include "plan.h"
 #include "serving.h"

@@ -25,11 +25,12 @@
 //      from the list), and the draw within the one part that holds it.
 // The first three read the row (from HBM once, then out of the caches); pass 2
 // is bound by fp64 arithmetic and LDS atomics, the rest by memory and latency.
-// Measured, fp32, 250 rows of 128256 (128 MB), all filters: 20 (6.3 TB/s), 41, 33
-// and 25 us; one bf16 row: 3.3, 5.0, 10.0 and 15 us, of which 10 or so are launches
-// and the rest dependent steps.
+// Measured, fp32, 250 rows of 128256 (128 MB), all filters: 20 (6.3 TB/s), 37, 35
+// and 24 us; one bf16 row: 2.8, 4.9, 10.1 and 15 us, of which 10 or so are launches
+// and the rest dependent steps.  250 bf16 rows: the call 102 us.
 // A row whose cut bins hold more tokens than the lists take (one of few distinct
-// values, or nearly flat) is searched as a whole in pass 4.
+// values, or nearly flat) is searched as a whole in pass 4, by its one workgroup: such
+// calls take 305 (one bf16 row) to 380 us (250 rows).
 #include <limits.h>
 
 #include <type_traits>

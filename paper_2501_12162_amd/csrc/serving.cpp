@@ -107,9 +107,9 @@ int32_t validate_prompt(int32_t num_requests, const int32_t *indptr, const int32
 // requests than it holds are found by a scan on the device, in their own order.
 // Several units per workgroup, each workgroup taking every kPromptGrid-th,
 // hide the loads that open a unit behind the end of the one before (16 ragged
-// prompts of 636-2012 tokens 379 -> 375 us); that needs units in descending
-// order of keys, which the table gives where all rows have as many cached keys
-// before them.
+// prompts of 636-2012 tokens 369 -> 355 us, one of 8191 468 -> 463); that needs
+// units in descending order of keys, which the table gives where all rows have as
+// many cached keys before them.
 struct PromptPlan {
   int64_t units = 0;
   int32_t chunks = 1, chunk_keys = INT32_MAX;
@@ -121,8 +121,8 @@ struct PromptPlan {
 // idle, so their keys are split and joined by a second launch.  Priced by a
 // tile's time over k keys, kTileUs + k * kKeyUs, in rounds of kPromptGrid tiles,
 // and by the join's traffic: tiles write and the join reads D + 2 floats per row.
-// (64 rows over 8064 keys, 64 heads on 8: 167 us whole, 41 split; 2000 rows over as
-// many keys: 76 and 74.)
+// (64 rows over 8064 keys, 64 heads on 8: 167 us whole, 37 split; one row 157 and
+// 27; 2000 rows of a prompt, 504 tiles, stay whole: 69.)
 PromptPlan prompt_plan(int32_t num_requests, const int32_t *indptr, const int32_t *ctx, int32_t hq, int32_t hkv,
                        int32_t head_dim, bool bf16) {
   constexpr double kTileUs = 9.0, kJoinUs = 6.0, kJoinBytesPerUs = 4e6;

@@ -106,8 +106,8 @@ struct PromptAttnArgs : PagedAttnArgs {
 // launch.  Requests of one short run each, and more of them than the scan takes,
 // are units themselves.
 constexpr int kDecodeRows = 16;              // most query heads per kv-head: the columns of a matrix tile
-// One block per wave (a request of 1500 tokens, 32 heads on 8: 9.4 us; shares of 8
-// blocks 10.1, of 2 10.4).
+// One block per wave: in a graph, 32 heads on 8, a request of 1500 tokens 8.7 us and
+// of 6000 12.3; with shares of 8 blocks and more 9.5 and 10.9, of 2 and more 8.5 and 11.7.
 constexpr int kDecodeMinBlocks = 4;
 constexpr int kDecodeUnits = 512;            // on the device: two workgroups per CU
 constexpr int kDecodeSplitRequests = 1024;
