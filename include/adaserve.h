@@ -28,7 +28,15 @@
  *                              values written into the paged cache;
  *   adaserve_prompt_attn       causal attention of packed prompts over it;
  *   adaserve_decode_attn       attention of one new token per request;
- *   adaserve_sample            a token per row by temperature, top-k, top-p, min-p.
+ *   adaserve_sample            a token per row by temperature, top-k, top-p, min-p;
+ *   adaserve_window_prompt_attn, adaserve_window_decode_attn, adaserve_window_tree_attn
+ *                              the three attentions of models that see a window of
+ *                              the newest keys and a few first ones (sinks);
+ * and the cache's pages, all on the device:
+ *   adaserve_update_pages      what left the window is freed, what comes next taken;
+ *   adaserve_fork_pages        rows of the cache go over to other rows (beams, samples);
+ *   adaserve_compact_pages     the pages in use move to the front of the pool;
+ *   adaserve_copy_pages        page contents, as the two before ask for.
  *
  * Conventions for every entry point:
  *  - Pointers without a _host suffix are DEVICE pointers owned by the caller;
@@ -595,6 +603,167 @@ int32_t adaserve_sample(const void *logits, int64_t row_stride, int32_t num_rows
                         int32_t dtype, const float *temperature, const int32_t *top_k,
                         const float *top_p, const float *min_p, const float *u, int32_t *out_token,
                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention over a window and sinks: a row at position p sees position j <= p
+ * where j > p - window (the newest `window` positions, its own among them) or
+ * j < sinks (the first ones, for good).  window >= 1, sinks >= 0; a window that
+ * reaches the first position gives the attention without one.  Three forms:
+ *
+ *   adaserve_window_prompt_attn  adaserve_prompt_attn's rows, at positions
+ *     c - n + i.
+ *   adaserve_window_decode_attn  adaserve_decode_attn's, at position c - 1.
+ *   adaserve_window_tree_attn    adaserve_tree_attn_verify's nodes, at positions
+ *     L + depth (the root's depth is 0): of the prefix and of the nodes on the
+ *     root-to-node path a node sees those that its position sees.
+ *
+ * Everything else -- layouts, types, head groups, roundings, limits, zero pages,
+ * lengths on the host and on the device, workspaces -- is as in those calls; rows of q
+ * may lie apart in the first two.  Pages that hold no position seen by any row of
+ * their request are not read, nor their block-table entries used: they may have
+ * been freed (adaserve_update_pages), given to other requests or hold anything.
+ * A position that a row does not see adds nothing to it, whatever key and value
+ * it holds; in BF16 trees that is so for prefix positions that no node of the
+ * request sees and for nodes past the request's, and the values of the others must
+ * be finite, as there.
+ */
+size_t adaserve_window_prompt_attn_workspace_bytes(int32_t num_requests, const int32_t *token_indptr_host,
+                                                   const int32_t *context_len_host, int32_t num_q_heads,
+                                                   int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                                                   int32_t window, int32_t sinks, int32_t dtype);
+
+int32_t adaserve_window_prompt_attn(int32_t num_requests, const int32_t *token_indptr,
+                                    const int32_t *token_indptr_host, const void *q, int64_t q_row_stride,
+                                    const void *k_pages, const void *v_pages, int32_t num_pages,
+                                    const int32_t *block_table, int32_t block_table_stride,
+                                    const int32_t *context_len, const int32_t *context_len_host,
+                                    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                    int32_t page_size, int32_t window, int32_t sinks, float sm_scale,
+                                    int32_t dtype, void *out, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
+size_t adaserve_window_decode_attn_workspace_bytes(int32_t num_requests, int32_t max_context,
+                                                   int32_t num_q_heads, int32_t num_kv_heads,
+                                                   int32_t head_dim, int32_t page_size, int32_t window,
+                                                   int32_t sinks, int32_t dtype);
+
+int32_t adaserve_window_decode_attn(int32_t num_requests, const void *q, int64_t q_row_stride,
+                                    const void *k_pages, const void *v_pages, int32_t num_pages,
+                                    const int32_t *block_table, int32_t block_table_stride,
+                                    const int32_t *context_len, int32_t max_context, int32_t num_q_heads,
+                                    int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                                    int32_t window, int32_t sinks, float sm_scale, int32_t dtype, void *out,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+
+size_t adaserve_window_tree_attn_workspace_bytes(int32_t num_requests, const int32_t *node_indptr_host,
+                                                 const int32_t *prefix_len_host, int32_t num_q_heads,
+                                                 int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                                                 int32_t window, int32_t sinks, int32_t dtype);
+
+int32_t adaserve_window_tree_attn(int32_t num_requests, const int32_t *node_indptr,
+                                  const int32_t *node_indptr_host, const int32_t *parent, const void *q,
+                                  const void *k_tree, const void *v_tree, const void *k_pages,
+                                  const void *v_pages, int32_t num_pages, const int32_t *block_table,
+                                  int32_t block_table_stride, const int32_t *prefix_len,
+                                  const int32_t *prefix_len_host, int32_t num_q_heads, int32_t num_kv_heads,
+                                  int32_t head_dim, int32_t page_size, int32_t window, int32_t sinks,
+                                  float sm_scale, int32_t dtype, void *out, void *workspace,
+                                  size_t workspace_bytes, void *stream);
+
+/*
+ * The cache's pages.  page_refs [num_pages] int32 counts the block-table
+ * entries, of all tables and whatever else keeps a page, that hold each page; a
+ * page is free where it is <= 0.  Taken pages are the free ones with the lowest
+ * numbers, so results depend on no order of execution.  A block-table entry
+ * outside [0, num_pages) holds no page.  Everything is read and written on the
+ * device, so that a captured call follows the tables; all arrays are int32.
+ *
+ * new_page_refs may be page_refs itself, and new_block_table block_table (not in
+ * adaserve_fork_pages); otherwise outputs overlap neither inputs nor each other
+ * and are written whole.  workspace: at least adaserve_pages_workspace_bytes(the
+ * larger of a call's row counts, num_pages) bytes, 256-byte aligned, no
+ * initialisation needed; calls that share one must not overlap in time, nor may
+ * calls on the same page_refs.  At most 65536 rows, 2^24 pages, page_size <= 2^16.
+ */
+size_t adaserve_pages_workspace_bytes(int32_t num_rows, int32_t num_pages);
+
+/*
+ * One step of a batch's pages.  Row r of block_table [num_requests,
+ * block_table_stride] has c = context_len[r] tokens.
+ *   c < 0: the request is over; all its entries become -1.
+ *   c >= 0, window > 0: entry e becomes -1 where none of its positions is a sink
+ *     or seen by a token at position c or later: e * page_size >= sinks and
+ *     (e + 1) * page_size <= c + 1 - window.  window = 0: no entry does.
+ * A page loses one reference per entry that held it and became -1.  Then, where
+ * need_len is given (NULL: pages are only freed, and capacity is NULL, too), the
+ * entries e with ceil(c / page_size) <= e < ceil(need_len[r] / page_size), inside
+ * the row, of requests with c >= 0 that hold no page get a free one each (those
+ * just freed among them), in order of rows and entries, as long as there are any,
+ * and one reference.  capacity[r]: the first position from c on and below need_len[r]
+ * whose entry holds no page (or lies past the row), or need_len[r] where there is
+ * none; 0 where c < 0.
+ */
+int32_t adaserve_update_pages(int32_t num_requests, const int32_t *context_len, const int32_t *need_len,
+                              int32_t window, int32_t sinks, int32_t page_size, const int32_t *block_table,
+                              int32_t block_table_stride, const int32_t *page_refs, int32_t num_pages,
+                              int32_t *new_block_table, int32_t *new_page_refs, int32_t *capacity,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Rows of a cache go over to the rows of a new batch: beams to their children
+ * (source = adaserve_beam_step's parents, as rows of the batch), a prompt to its
+ * samples, requests to other places.  New row r < num_requests has the cache of row
+ * source[r] of the num_sources old ones (outside [0, num_sources): an empty row).
+ * With c = context_len[source[r]], taken into [0, block_table_stride * page_size],
+ * the c / page_size whole pages are shared.  What is behind them -- the page that
+ * is filled in part, and pages taken for later tokens -- stays with the first of
+ * the new rows; every other one has -1 there, but for a page of its own in the place of the
+ * partly filled one, if c is not a multiple of page_size and that entry holds a page:
+ * the lowest free one, in order of rows, whose content adaserve_copy_pages then
+ * copies: copy_src[r] to copy_dst[r] (-1, -1 for rows that need none).  Rows for
+ * which no free page is left keep the whole pages alone.
+ *   new_context_len[r]: c; the whole pages' tokens where no page was left; 0 of an empty row.
+ *   new_page_refs: a page's references by old rows taken off, those by new rows
+ *   added; so pages of rows that nobody takes become free, and serve this call.
+ * Entries behind c / page_size are taken to belong to one row each.
+ */
+int32_t adaserve_fork_pages(int32_t num_sources, int32_t num_requests, const int32_t *source,
+                            const int32_t *context_len, int32_t page_size, const int32_t *block_table,
+                            int32_t block_table_stride, const int32_t *page_refs, int32_t num_pages,
+                            int32_t *new_block_table, int32_t *new_context_len, int32_t *new_page_refs,
+                            int32_t *copy_src, int32_t *copy_dst, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/*
+ * The pages in use move to the front of the pool: with U of them, the i-th one
+ * numbered U or higher goes to the i-th free place below U, and the pool ends at U
+ * (to be handed back, or to hold other caches).
+ *   new_place [num_pages]: a page's number afterwards, -1 of a free one (for page
+ *   numbers kept elsewhere);
+ *   new_block_table: every entry that held a page has its new number (a free
+ *   one: -1), others stay; new_page_refs: the references moved, 0 from U on;
+ *   counts [2]: U, and the number of moves;
+ *   move_src, move_dst [num_pages]: the moves, -1 behind them.
+ * The contents: adaserve_copy_pages(move_src, move_dst) with count = counts + 1.
+ */
+int32_t adaserve_compact_pages(int32_t num_requests, const int32_t *block_table, int32_t block_table_stride,
+                               const int32_t *page_refs, int32_t num_pages, int32_t *new_block_table,
+                               int32_t *new_page_refs, int32_t *new_place, int32_t *move_src,
+                               int32_t *move_dst, int32_t *counts, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/*
+ * Page src[i] of k_pages and v_pages goes to page dst[i], bit for bit, i <
+ * num_copies (count given: i < min(*count, num_copies), read on the device); a pair with
+ * a page outside [0, num_pages), or src = dst, is left out.  No page is the dst of two
+ * pairs, or the src of one and the dst of another.  num_layers pools [num_pages, Hkv,
+ * page_size, D], layer_stride elements apart (any for one layer), are copied in one
+ * launch.  Rows of a head are a multiple of 16 bytes; dtype F32 or BF16.
+ */
+int32_t adaserve_copy_pages(int32_t num_copies, const int32_t *src, const int32_t *dst, const int32_t *count,
+                            void *k_pages, void *v_pages, int32_t num_layers, int64_t layer_stride,
+                            int32_t num_pages, int32_t num_kv_heads, int32_t page_size, int32_t head_dim,
+                            int32_t dtype, void *stream);
 
 /* Message describing the last non-OK status returned on this thread. */
 const char *adaserve_last_error(void);

@@ -60,6 +60,20 @@ SIGNATURES = {
                                     _F32, _I32, _P, _P, _SZ, _P]),
     "adaserve_sample_workspace_bytes": (_SZ, [_I32, _I32, _I32]),
     "adaserve_sample": (_I32, [_P, _I64, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "adaserve_window_prompt_attn_workspace_bytes": (_SZ, [_I32, _P, _P, _I32, _I32, _I32, _I32, _I32, _I32, _I32]),
+    "adaserve_window_prompt_attn": (_I32, [_I32, _P, _P, _P, _I64, _P, _P, _I32, _P, _I32, _P, _P, _I32, _I32, _I32,
+                                           _I32, _I32, _I32, _F32, _I32, _P, _P, _SZ, _P]),
+    "adaserve_window_decode_attn_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _I32]),
+    "adaserve_window_decode_attn": (_I32, [_I32, _P, _I64, _P, _P, _I32, _P, _I32, _P, _I32, _I32, _I32, _I32, _I32,
+                                           _I32, _I32, _F32, _I32, _P, _P, _SZ, _P]),
+    "adaserve_window_tree_attn_workspace_bytes": (_SZ, [_I32, _P, _P, _I32, _I32, _I32, _I32, _I32, _I32, _I32]),
+    "adaserve_window_tree_attn": (_I32, [_I32, _P, _P, _P, _P, _P, _P, _P, _P, _I32, _P, _I32, _P, _P, _I32, _I32,
+                                         _I32, _I32, _I32, _I32, _F32, _I32, _P, _P, _SZ, _P]),
+    "adaserve_pages_workspace_bytes": (_SZ, [_I32, _I32]),
+    "adaserve_update_pages": (_I32, [_I32, _P, _P, _I32, _I32, _I32, _P, _I32, _P, _I32, _P, _P, _P, _P, _SZ, _P]),
+    "adaserve_fork_pages": (_I32, [_I32, _I32, _P, _P, _I32, _P, _I32, _P, _I32, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "adaserve_compact_pages": (_I32, [_I32, _P, _I32, _P, _I32, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "adaserve_copy_pages": (_I32, [_I32, _P, _P, _P, _P, _P, _I32, _I64, _I32, _I32, _I32, _I32, _I32, _P]),
     "adaserve_last_error": (ctypes.c_char_p, []),
 }
 
@@ -490,3 +504,171 @@ def adaserve_sample(*, logits, vocab: int, u, out_token, temperature=None, top_k
     device, (t, k, p, m, up, out, ws) = _pointers((temperature, top_k, top_p, min_p, u, out_token, workspace), (logits,))
     _device_call("adaserve_sample", device, stream, logits.data_ptr(), logits.stride(0) if rows > 1 else width, rows,
                  vocab, _dtype_code(logits), t, k, p, m, up, out, ws, _bytes(workspace))
+
+
+def adaserve_window_prompt_attn_workspace_bytes(token_indptr_host, context_len_host, num_q_heads: int, num_kv_heads: int,
+                                                head_dim: int, page_size: int, window: int, sinks: int, dtype: int) -> int:
+    ip, cl = _host_i32(token_indptr_host), _host_i32(context_len_host)
+    n = load_library().adaserve_window_prompt_attn_workspace_bytes(
+        cl.size, ip.ctypes.data, cl.ctypes.data, num_q_heads, num_kv_heads, head_dim, page_size, window, sinks, dtype)
+    if n == ctypes.c_size_t(-1).value:
+        _check(ADASERVE_ERR_INVALID_ARGUMENT)
+    return n
+
+
+def adaserve_window_prompt_attn(*, token_indptr, token_indptr_host, q, k_pages, v_pages, block_table, context_len,
+                                context_len_host, window: int, sinks: int, sm_scale: float, out, workspace=None,
+                                stream=None) -> None:
+    """``adaserve_prompt_attn`` of rows that see the newest ``window`` positions and the first ``sinks``."""
+    import torch
+    ip, cl = _host_i32(token_indptr_host), _host_i32(context_len_host)
+    B = cl.size
+    T, Hq, D = q.shape
+    if ip.size != B + 1 or token_indptr.shape[0] != B + 1 or (B and T < ip[B]):
+        raise ValueError("token_indptr must have %d entries, the last at most %d" % (B + 1, T))
+    _check_paged(q, k_pages, v_pages, block_table, context_len, out, B)
+    _typed(token_indptr, torch.int32, "token_indptr")
+    qp, qs = _rows(q, "q")
+    device, (tip, kp, vp, bt, clen, o, ws) = _pointers(
+        (token_indptr, k_pages, v_pages, block_table, context_len, out, workspace), (q,))
+    _device_call("adaserve_window_prompt_attn", device, stream, B, tip, ip.ctypes.data, qp, qs, kp, vp, k_pages.shape[0],
+                 bt, block_table.shape[1], clen, cl.ctypes.data, Hq, k_pages.shape[1], D, k_pages.shape[2], window, sinks,
+                 sm_scale, _dtype_code(q), o, ws, _bytes(workspace))
+
+
+def adaserve_window_decode_attn_workspace_bytes(num_requests: int, max_context: int, num_q_heads: int, num_kv_heads: int,
+                                                head_dim: int, page_size: int, window: int, sinks: int, dtype: int) -> int:
+    n = load_library().adaserve_window_decode_attn_workspace_bytes(
+        num_requests, max_context, num_q_heads, num_kv_heads, head_dim, page_size, window, sinks, dtype)
+    if n == ctypes.c_size_t(-1).value:
+        _check(ADASERVE_ERR_INVALID_ARGUMENT)
+    return n
+
+
+def adaserve_window_decode_attn(*, q, k_pages, v_pages, block_table, context_len, max_context: int, window: int,
+                                sinks: int, sm_scale: float, out, workspace=None, stream=None) -> None:
+    """``adaserve_decode_attn`` of tokens that see the newest ``window`` positions and the first ``sinks``."""
+    B, Hq, D = q.shape
+    _check_paged(q, k_pages, v_pages, block_table, context_len, out, B)
+    qp, qs = _rows(q, "q")
+    device, (kp, vp, bt, clen, o, ws) = _pointers((k_pages, v_pages, block_table, context_len, out, workspace), (q,))
+    _device_call("adaserve_window_decode_attn", device, stream, B, qp, qs, kp, vp, k_pages.shape[0], bt,
+                 block_table.shape[1], clen, max_context, Hq, k_pages.shape[1], D, k_pages.shape[2], window, sinks,
+                 sm_scale, _dtype_code(q), o, ws, _bytes(workspace))
+
+
+def adaserve_window_tree_attn_workspace_bytes(node_indptr_host, prefix_len_host, num_q_heads: int, num_kv_heads: int,
+                                              head_dim: int, page_size: int, window: int, sinks: int, dtype: int) -> int:
+    ip, pl = _host_i32(node_indptr_host), _host_i32(prefix_len_host)
+    n = load_library().adaserve_window_tree_attn_workspace_bytes(
+        pl.size, ip.ctypes.data, pl.ctypes.data, num_q_heads, num_kv_heads, head_dim, page_size, window, sinks, dtype)
+    if n == ctypes.c_size_t(-1).value:
+        _check(ADASERVE_ERR_INVALID_ARGUMENT)
+    return n
+
+
+def adaserve_window_tree_attn(*, node_indptr, node_indptr_host, parent, q, k_tree, v_tree, k_pages, v_pages, block_table,
+                              prefix_len, prefix_len_host, window: int, sinks: int, sm_scale: float, out, workspace=None,
+                              stream=None) -> None:
+    """``adaserve_tree_attn_verify`` of nodes that see the newest ``window`` positions and the first ``sinks``
+    (q, out [T, Hq, D], k_tree, v_tree [T, Hkv, D])."""
+    import torch
+    ip, pl = _host_i32(node_indptr_host), _host_i32(prefix_len_host)
+    B = pl.size
+    T, Hq, D = q.shape
+    if ip.size != B + 1 or node_indptr.shape[0] != B + 1 or parent.shape[0] < T or (B and T != ip[B]):
+        raise ValueError("node_indptr must have %d entries, the last of them %d, parent %d" % (B + 1, T, T))
+    _check_paged(q, k_pages, v_pages, block_table, prefix_len, out, B)
+    for t, name in ((k_tree, "k_tree"), (v_tree, "v_tree")):
+        if t.shape != (T, k_pages.shape[1], D):
+            raise ValueError("%s must be [%d, %d, %d]" % (name, T, k_pages.shape[1], D))
+        _typed(t, q.dtype, name)
+    _typed(node_indptr, torch.int32, "node_indptr")
+    _typed(parent, torch.int32, "parent")
+    device, (tip, par, qp, kt, vt, kp, vp, bt, plen, o, ws) = _pointers(
+        (node_indptr, parent, q, k_tree, v_tree, k_pages, v_pages, block_table, prefix_len, out, workspace))
+    _device_call("adaserve_window_tree_attn", device, stream, B, tip, ip.ctypes.data, par, qp, kt, vt, kp, vp,
+                 k_pages.shape[0], bt, block_table.shape[1], plen, pl.ctypes.data, Hq, k_pages.shape[1], D,
+                 k_pages.shape[2], window, sinks, sm_scale, _dtype_code(q), o, ws, _bytes(workspace))
+
+
+def adaserve_pages_workspace_bytes(num_rows: int, num_pages: int) -> int:
+    n = load_library().adaserve_pages_workspace_bytes(num_rows, num_pages)
+    if n == ctypes.c_size_t(-1).value:
+        _check(ADASERVE_ERR_INVALID_ARGUMENT)
+    return n
+
+
+def _int32s(shaped) -> None:
+    """Every tensor that is given is int32 and of its shape."""
+    import torch
+    for t, name, shape in shaped:
+        if t is not None:
+            _typed(t, torch.int32, name)
+            if t.shape != shape:
+                raise ValueError("%s must be %s, is %s" % (name, list(shape), list(t.shape)))
+
+
+def adaserve_update_pages(*, context_len, block_table, page_refs, page_size: int, need_len=None, capacity=None,
+                          window: int = 0, sinks: int = 0, new_block_table=None, new_page_refs=None, workspace,
+                          stream=None) -> None:
+    """Frees the pages of block_table [B, stride] that left the window (context_len[r] < 0: all of row r's) and takes
+    pages for the positions up to need_len; in place where no new_block_table, new_page_refs is given."""
+    B, stride = block_table.shape
+    new_bt = block_table if new_block_table is None else new_block_table
+    new_refs = page_refs if new_page_refs is None else new_page_refs
+    _int32s(((context_len, "context_len", (B,)), (need_len, "need_len", (B,)), (capacity, "capacity", (B,)),
+             (block_table, "block_table", (B, stride)), (new_bt, "new_block_table", (B, stride)),
+             (page_refs, "page_refs", (page_refs.shape[0],)), (new_refs, "new_page_refs", (page_refs.shape[0],))))
+    device, (clen, need, bt, refs, nbt, nrefs, cap, ws) = _pointers(
+        (context_len, need_len, block_table, page_refs, new_bt, new_refs, capacity, workspace))
+    _device_call("adaserve_update_pages", device, stream, B, clen, need, window, sinks, page_size, bt, stride, refs,
+                 page_refs.shape[0], nbt, nrefs, cap, ws, _bytes(workspace))
+
+
+def adaserve_fork_pages(*, source, context_len, block_table, page_refs, page_size: int, new_block_table, new_context_len,
+                        copy_src, copy_dst, new_page_refs=None, workspace, stream=None) -> None:
+    """New row r takes the cache of old row source[r]: block_table [S, stride] and context_len [S] give new_block_table
+    [B, stride] and new_context_len [B]; page copy_src[r] is to be copied to copy_dst[r] (-1: none)."""
+    (S, stride), B = block_table.shape, source.shape[0]
+    new_refs = page_refs if new_page_refs is None else new_page_refs
+    _int32s(((source, "source", (B,)), (context_len, "context_len", (S,)), (block_table, "block_table", (S, stride)),
+             (new_block_table, "new_block_table", (B, stride)), (new_context_len, "new_context_len", (B,)),
+             (copy_src, "copy_src", (B,)), (copy_dst, "copy_dst", (B,)), (page_refs, "page_refs", (page_refs.shape[0],)),
+             (new_refs, "new_page_refs", (page_refs.shape[0],))))
+    device, (src, clen, bt, refs, nbt, nlen, nrefs, cs, cd, ws) = _pointers(
+        (source, context_len, block_table, page_refs, new_block_table, new_context_len, new_refs, copy_src, copy_dst,
+         workspace))
+    _device_call("adaserve_fork_pages", device, stream, S, B, src, clen, page_size, bt, stride, refs, page_refs.shape[0],
+                 nbt, nlen, nrefs, cs, cd, ws, _bytes(workspace))
+
+
+def adaserve_compact_pages(*, block_table, page_refs, new_place, move_src, move_dst, counts, new_block_table=None,
+                           new_page_refs=None, workspace, stream=None) -> None:
+    """Numbers the pages in use from 0 on; the contents follow by ``adaserve_copy_pages`` of move_src to move_dst [P]
+    with count = counts[1:].  In place where no new_block_table, new_page_refs is given."""
+    B, stride = block_table.shape
+    P = page_refs.shape[0]
+    new_bt = block_table if new_block_table is None else new_block_table
+    new_refs = page_refs if new_page_refs is None else new_page_refs
+    _int32s(((block_table, "block_table", (B, stride)), (new_bt, "new_block_table", (B, stride)),
+             (page_refs, "page_refs", (P,)), (new_refs, "new_page_refs", (P,)), (new_place, "new_place", (P,)),
+             (move_src, "move_src", (P,)), (move_dst, "move_dst", (P,)), (counts, "counts", (2,))))
+    device, (bt, refs, nbt, nrefs, place, ms, md, cnt, ws) = _pointers(
+        (block_table, page_refs, new_bt, new_refs, new_place, move_src, move_dst, counts, workspace))
+    _device_call("adaserve_compact_pages", device, stream, B, bt, stride, refs, P, nbt, nrefs, place, ms, md, cnt, ws,
+                 _bytes(workspace))
+
+
+def adaserve_copy_pages(*, src, dst, k_pages, v_pages, count=None, stream=None) -> None:
+    """Pages src [n] of k_pages and v_pages ([P, Hkv, page_size, D], or [layers, P, Hkv, page_size, D]) to pages dst [n]
+    (-1: none); count [1]: how many of them, read on the device."""
+    n = src.shape[0]
+    _int32s(((src, "src", (n,)), (dst, "dst", (n,)), (count, "count", (1,))))
+    if k_pages.dim() not in (4, 5) or v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype:
+        raise ValueError("k_pages and v_pages must be [pages, kv-heads, page_size, dim], or that of every layer")
+    layers = k_pages.shape[0] if k_pages.dim() == 5 else 1
+    P, hkv, ps, D = k_pages.shape[-4:]
+    device, (s, d, c, kp, vp) = _pointers((src, dst, count, k_pages, v_pages))
+    _device_call("adaserve_copy_pages", device, stream, n, s, d, c, kp, vp, layers, P * hkv * ps * D, P, hkv, ps, D,
+                 _dtype_code(k_pages))

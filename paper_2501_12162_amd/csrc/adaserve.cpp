@@ -106,6 +106,14 @@ int32_t validate_step(const StepArgs &st, int32_t num_requests, int32_t total_no
   return ADASERVE_OK;
 }
 
+// Positions of the longest request: its prefix, and its nodes in a chain.
+int64_t most_positions(int32_t num_requests, const int32_t *node_indptr_host, const int32_t *prefix_len_host) {
+  int64_t most = 0;
+  for (int32_t r = 0; r < num_requests; ++r)
+    most = std::max<int64_t>(most, (int64_t)prefix_len_host[r] + node_indptr_host[r + 1] - node_indptr_host[r]);
+  return most;
+}
+
 // The tree-attention entry points and the verification step: the caller's
 // workspace, or (use_scratch) the library's static per-device scratch array;
 // with `step`, the argmax and acceptance of the same pass are enqueued too.
@@ -114,8 +122,9 @@ int32_t tree_attn_verify_impl(int32_t num_requests, const int32_t *node_indptr, 
                               const void *k_pages, const void *v_pages, int32_t num_pages,
                               const int32_t *block_table, int32_t block_table_stride, const int32_t *prefix_len,
                               const int32_t *prefix_len_host, int32_t num_q_heads, int32_t num_kv_heads,
-                              int32_t head_dim, int32_t page_size, float sm_scale, int32_t dtype, void *out,
-                              void *workspace, size_t workspace_bytes, bool use_scratch, const StepArgs *step,
+                              int32_t head_dim, int32_t page_size, int32_t window, int32_t sinks, float sm_scale,
+                              int32_t dtype, void *out, void *workspace, size_t workspace_bytes, bool use_scratch,
+                              const StepArgs *step,
                               void *stream) {
   if (block_table_stride < 0) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "block_table_stride < 0");
   if (num_pages < 0) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "num_pages < 0");
@@ -133,6 +142,7 @@ int32_t tree_attn_verify_impl(int32_t num_requests, const int32_t *node_indptr, 
     if (st != ADASERVE_OK) return st;
   }
   if (num_requests == 0) return ADASERVE_OK;
+  if (sees_all(window, sinks, most_positions(num_requests, node_indptr_host, prefix_len_host))) window = sinks = 0;
   if (!node_indptr || !parent || !q || !k_tree || !v_tree || !out || !prefix_len)
     return fail(ADASERVE_ERR_INVALID_ARGUMENT, "a required device pointer is NULL");
   bool any_prefix = false;
@@ -145,8 +155,9 @@ int32_t tree_attn_verify_impl(int32_t num_requests, const int32_t *node_indptr, 
   const void *tensors[] = {q, k_tree, v_tree, out, k_pages, v_pages};
   for (const void *t : tensors)
     if (t && !aligned(t, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "tensor pointers must be 16-byte aligned");
-  AttnPlan plan =
-      make_plan_cached(num_requests, node_indptr_host, prefix_len_host, num_kv_heads, shape.group, head_dim, dtype);
+  AttnPlan plan;
+  if (!window)
+    plan = make_plan_cached(num_requests, node_indptr_host, prefix_len_host, num_kv_heads, shape.group, head_dim, dtype);
   if (use_scratch && plan.ws_bytes > (size_t)ADASERVE_TREE_ATTN_SCRATCH_BYTES)
     plan = make_plan_cached(num_requests, node_indptr_host, prefix_len_host, num_kv_heads, shape.group, head_dim, dtype,
                             true);
@@ -198,7 +209,7 @@ int32_t tree_attn_verify_impl(int32_t num_requests, const int32_t *node_indptr, 
   a.merge_blocks = plan.row_groups * (kMaxRowsPerTile / 16);
   a.stream_kv = plan.single_tile ? 1 : 0;
   PlanTable t;
-  fill_plan_table(t, num_requests, node_indptr_host, prefix_len_host, num_kv_heads, shape.group, plan);
+  if (!window) fill_plan_table(t, num_requests, node_indptr_host, prefix_len_host, num_kv_heads, shape.group, plan);
   a.plan_count = t.count;
   if (t.count > 0) {
     std::copy(t.entry, t.entry + t.count, a.plan);
@@ -206,7 +217,11 @@ int32_t tree_attn_verify_impl(int32_t num_requests, const int32_t *node_indptr, 
   }
   a.sm_scale = sm_scale;
   a.scale_log2 = sm_scale * 1.4426950408889634f;
+  a.window = window;
+  a.sinks = sinks;
   hipStream_t s = (hipStream_t)stream;
+  if (window)
+    return launch_status(launch_window_tree_rows(a, head_dim, dtype == ADASERVE_BF16, s), "window attention launch");
   if (step) {
     a.logits = step->logits;
     a.logit_stride = step->row_stride;
@@ -241,7 +256,7 @@ int32_t adaserve_tree_attn_verify(int32_t num_requests, const int32_t *node_indp
                                   void *out, void *workspace, size_t workspace_bytes, void *stream) {
   return tree_attn_verify_impl(num_requests, node_indptr, node_indptr_host, parent, q, k_tree, v_tree, k_pages,
                                v_pages, num_pages, block_table, block_table_stride, prefix_len, prefix_len_host,
-                               num_q_heads, num_kv_heads, head_dim, page_size, sm_scale, dtype, out, workspace,
+                               num_q_heads, num_kv_heads, head_dim, page_size, 0, 0, sm_scale, dtype, out, workspace,
                                workspace_bytes, false, nullptr, stream);
 }
 
@@ -255,8 +270,37 @@ int32_t adaserve_tree_attn_verify_noalloc(int32_t num_requests, const int32_t *n
                                           float sm_scale, int32_t dtype, void *out, void *stream) {
   return tree_attn_verify_impl(num_requests, node_indptr, node_indptr_host, parent, q, k_tree, v_tree, k_pages,
                                v_pages, num_pages, block_table, block_table_stride, prefix_len, prefix_len_host,
-                               num_q_heads, num_kv_heads, head_dim, page_size, sm_scale, dtype, out, nullptr, 0,
+                               num_q_heads, num_kv_heads, head_dim, page_size, 0, 0, sm_scale, dtype, out, nullptr, 0,
                                true, nullptr, stream);
+}
+
+size_t adaserve_window_tree_attn_workspace_bytes(int32_t num_requests, const int32_t *node_indptr_host,
+                                                 const int32_t *prefix_len_host, int32_t num_q_heads,
+                                                 int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                                                 int32_t window, int32_t sinks, int32_t dtype) {
+  AttnShape shape;
+  if (validate_window(window, sinks) != ADASERVE_OK ||
+      validate_attn_shape(num_requests, node_indptr_host, prefix_len_host, num_q_heads, num_kv_heads, head_dim,
+                          page_size, dtype, -1, shape) != ADASERVE_OK)
+    return SIZE_MAX;
+  if (!sees_all(window, sinks, most_positions(num_requests, node_indptr_host, prefix_len_host))) return 0;
+  return adaserve_tree_attn_workspace_bytes(num_requests, node_indptr_host, prefix_len_host, num_q_heads, num_kv_heads,
+                                            head_dim, page_size, dtype);
+}
+
+int32_t adaserve_window_tree_attn(int32_t num_requests, const int32_t *node_indptr, const int32_t *node_indptr_host,
+                                  const int32_t *parent, const void *q, const void *k_tree, const void *v_tree,
+                                  const void *k_pages, const void *v_pages, int32_t num_pages,
+                                  const int32_t *block_table, int32_t block_table_stride, const int32_t *prefix_len,
+                                  const int32_t *prefix_len_host, int32_t num_q_heads, int32_t num_kv_heads,
+                                  int32_t head_dim, int32_t page_size, int32_t window, int32_t sinks, float sm_scale,
+                                  int32_t dtype, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  const int32_t st = validate_window(window, sinks);
+  if (st != ADASERVE_OK) return st;
+  return tree_attn_verify_impl(num_requests, node_indptr, node_indptr_host, parent, q, k_tree, v_tree, k_pages,
+                               v_pages, num_pages, block_table, block_table_stride, prefix_len, prefix_len_host,
+                               num_q_heads, num_kv_heads, head_dim, page_size, window, sinks, sm_scale, dtype, out,
+                               workspace, workspace_bytes, false, nullptr, stream);
 }
 
 int32_t adaserve_tree_verify_step(int32_t num_requests, const int32_t *node_indptr, const int32_t *node_indptr_host,
@@ -273,7 +317,7 @@ int32_t adaserve_tree_verify_step(int32_t num_requests, const int32_t *node_indp
                       accept_tokens, accept_nodes};
   return tree_attn_verify_impl(num_requests, node_indptr, node_indptr_host, parent, q, k_tree, v_tree, k_pages,
                                v_pages, num_pages, block_table, block_table_stride, prefix_len, prefix_len_host,
-                               num_q_heads, num_kv_heads, head_dim, page_size, sm_scale, dtype, out, workspace,
+                               num_q_heads, num_kv_heads, head_dim, page_size, 0, 0, sm_scale, dtype, out, workspace,
                                workspace_bytes, false, &step, stream);
 }
 

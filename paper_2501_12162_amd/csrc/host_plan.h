@@ -31,6 +31,11 @@ int32_t validate_attn_shape(int32_t num_requests, const int32_t *indptr_host, co
                             int32_t hq, int32_t hkv, int32_t head_dim, int32_t page_size, int32_t dtype,
                             int32_t bt_stride_or_neg, AttnShape &shape);
 
+// A window of at least one position and a number of sinks.
+int32_t validate_window(int32_t window, int32_t sinks);
+// Whether a row sees all of `positions` positions up to its own: no window at all.
+inline bool sees_all(int32_t window, int32_t sinks, int64_t positions) { return window >= positions || sinks >= positions; }
+
 struct AttnPlan {
   int32_t rows_per_tile = 0;
   int32_t chunk_target = 0;

@@ -52,10 +52,14 @@ struct TreeAttnArgs {
   int32_t *accept_len;         // [num_requests]
   int32_t *accept_tokens;      // [num_requests, max_accept]
   int32_t *accept_nodes;       // [num_requests, max_accept]
+  int32_t window, sinks;       // what a node sees of the positions up to its own (window 0: all of them)
   int32_t stream_kv;           // 1: every request is one row tile (K/V read once; non-temporal loads)
   int32_t plan_count;          // entries used in plan[] (0: scan the device arrays)
   PlanEntry plan[kPlanMax];
 };
+
+// Attention over a window and sinks, row by row (window_attn.hip).
+hipError_t launch_window_tree_rows(const TreeAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
 
 hipError_t launch_tree_attn_bf16(TreeAttnArgs &a, int head_dim, bool needs_combine, hipStream_t stream);
 // The verification step: attention + argmax workgroups (many short F32 rows

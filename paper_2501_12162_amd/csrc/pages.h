@@ -1,0 +1,69 @@
+// Internal interface between the host entry points of the cache's pages
+// (pages.cpp) and their kernels (pages.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace adaserve {
+
+constexpr int kPagesThreads = 256;
+constexpr int kPagesMaxRows = 1 << 16;
+constexpr int kPagesMaxPages = 1 << 24;
+constexpr int kPagesRun = 1024;          // pages that a wave counts at a time
+
+struct PagesArgs {
+  int32_t rows;                  // of the new table
+  int32_t sources;               // of the old one (fork)
+  const int32_t *source;         // [rows] (fork)
+  const int32_t *context_len;    // [rows], of a fork [sources]
+  const int32_t *need_len;       // [rows], or null
+  int32_t window, sinks;
+  int32_t page_size;
+  const int32_t *table;          // [sources or rows, stride]
+  int32_t stride;
+  const int32_t *refs;           // [pages]
+  int32_t pages;
+  int32_t *new_table;            // [rows, stride]
+  int32_t *new_refs;             // [pages]
+  int32_t *capacity;             // [rows]
+  int32_t *new_len;              // [rows]
+  int32_t *copy_src, *copy_dst;  // [rows], of a compaction [pages]
+  int32_t *new_place;            // [pages]
+  int32_t *counts;               // [2]
+  // workspace
+  int32_t *ws_want;              // [rows] pages wanted; then the sum of the rows before
+  int32_t *ws_total;             // [1] pages handed out
+  int32_t *ws_list;              // [pages] the pages handed out, or ranks of moves
+  int32_t *ws_runs;              // [runs] used pages per run
+};
+
+struct CopyPagesArgs {
+  int32_t copies;
+  const int32_t *src, *dst;
+  const int32_t *count;          // or null
+  char *pool[2];                 // keys, values
+  int32_t layers;
+  int64_t layer_bytes, page_bytes;
+  int32_t pages;
+};
+
+// Offsets of the workspace.
+struct PagesSpace {
+  size_t total, list, runs, bytes;
+};
+inline PagesSpace pages_space(int32_t rows, int32_t pages) {
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  PagesSpace s;
+  s.total = up((size_t)rows * 4);
+  s.list = s.total + 256;
+  s.runs = s.list + up((size_t)pages * 4);
+  s.bytes = s.runs + up((size_t)((pages + kPagesRun - 1) / kPagesRun) * 4);
+  return s;
+}
+
+hipError_t launch_update_pages(const PagesArgs &a, hipStream_t stream);
+hipError_t launch_fork_pages(const PagesArgs &a, hipStream_t stream);
+hipError_t launch_compact_pages(const PagesArgs &a, hipStream_t stream);
+hipError_t launch_copy_pages(const CopyPagesArgs &a, hipStream_t stream);
+
+}  // namespace adaserve

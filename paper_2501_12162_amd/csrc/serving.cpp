@@ -239,6 +239,149 @@ int32_t validate_sample(int32_t num_rows, int32_t vocab, int32_t dtype) {
   return st != ADASERVE_OK ? st : validate_launch("sampling", num_rows, kSampleDrawThreads);
 }
 
+int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Prompt attention; over a window where there is one.
+int32_t prompt_attn_impl(int32_t num_requests, const int32_t *token_indptr, const int32_t *token_indptr_host,
+                         const void *q, int64_t q_row_stride, const void *k_pages, const void *v_pages,
+                         int32_t num_pages, const int32_t *block_table, int32_t block_table_stride,
+                         const int32_t *context_len, const int32_t *context_len_host, int32_t num_q_heads,
+                         int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t window, int32_t sinks,
+                         float sm_scale, int32_t dtype, void *out, void *workspace, size_t workspace_bytes,
+                         void *stream) {
+  int32_t st = validate_paged(num_requests, num_pages, block_table_stride, num_q_heads, num_kv_heads, head_dim,
+                              page_size, sm_scale, dtype);
+  if (st != ADASERVE_OK) return st;
+  int64_t total, most;
+  st = validate_prompt(num_requests, token_indptr_host, context_len_host, block_table_stride, num_q_heads, total, most);
+  if (st != ADASERVE_OK) return st;
+  if (total == 0) return ADASERVE_OK;
+  if (sees_all(window, sinks, most)) window = sinks = 0;
+  if (!token_indptr || !q || !out || !context_len)
+    return fail(ADASERVE_ERR_INVALID_ARGUMENT, "a required device pointer is NULL");
+  st = validate_rows("q", q, total, q_row_stride, (int64_t)num_q_heads * head_dim, elem_size(dtype));
+  if (st != ADASERVE_OK) return st;
+  if (!aligned(out, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "out must be 16-byte aligned");
+  st = validate_pages(most > 0, k_pages, v_pages, num_pages, block_table);
+  if (st != ADASERVE_OK) return st;
+  PromptPlan plan;
+  if (!window)
+    plan = prompt_plan(num_requests, token_indptr_host, context_len_host, num_q_heads, num_kv_heads, head_dim,
+                       dtype == ADASERVE_BF16);
+  st = validate_workspace(workspace, workspace_bytes, plan.ws_bytes);
+  if (st != ADASERVE_OK) return st;
+  PromptAttnArgs a{};
+  a.num_requests = num_requests;
+  a.token_indptr = token_indptr;
+  a.context_len = context_len;
+  a.block_table = block_table;
+  a.bt_stride = block_table_stride;
+  a.num_pages = num_pages;
+  a.q = q;
+  a.q_stride = q_row_stride;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.out = out;
+  a.total_tokens = (int32_t)total;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = num_kv_heads;
+  a.group = num_q_heads / num_kv_heads;
+  a.sm_scale = sm_scale;
+  a.scale_log2 = sm_scale * 1.4426950408889634f;
+  a.window = window;
+  a.sinks = sinks;
+  if (window) {
+    st = validate_launch("window attention", ceil_div64(total * num_q_heads, 4), kServingThreads);
+    if (st != ADASERVE_OK) return st;
+    st = check_device();
+    if (st != ADASERVE_OK) return st;
+    return launch_status(launch_window_rows(a, head_dim, dtype == ADASERVE_BF16, false, (hipStream_t)stream),
+                         "window attention launch");
+  }
+  if (dtype == ADASERVE_BF16) {
+    fill_prompt(a, plan, token_indptr_host, context_len_host, kPromptTileRows, workspace);
+  } else {
+    // 32-row tiles read each key half as often, 16-row tiles put more units to work: 2250 tiles of 32
+    // (2 prompts of up to 1500 tokens, D = 128) 301 against 341 us, 1800 (8 of up to 300) 88 against 83
+    for (a.f32_rows = 32;; a.f32_rows = 16) {
+      a.units = 0;
+      for (int32_t r = 0; r < num_requests; ++r)
+        a.units += (int64_t)prompt_tiles(token_indptr_host[r + 1] - token_indptr_host[r], a.group, a.f32_rows) * num_kv_heads;
+      if (a.units >= 2048 || a.f32_rows == 16) break;
+    }
+    PromptPlan tiles;
+    tiles.units = a.units;
+    fill_prompt(a, tiles, token_indptr_host, context_len_host, a.f32_rows, nullptr);
+  }
+  // (the join's rows: below 2^17, those of 512 tiles)
+  st = validate_launch("prompt attention", dtype == ADASERVE_BF16 ? a.grid : round_up(a.units, kPromptGrid), kServingThreads);
+  if (st != ADASERVE_OK) return st;
+  st = check_device();
+  if (st != ADASERVE_OK) return st;
+  return launch_status(launch_prompt_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
+                       "prompt attention launch");
+}
+
+// Single-token attention; over a window where there is one.
+int32_t decode_attn_impl(int32_t num_requests, const void *q, int64_t q_row_stride, const void *k_pages,
+                         const void *v_pages, int32_t num_pages, const int32_t *block_table,
+                         int32_t block_table_stride, const int32_t *context_len, int32_t max_context,
+                         int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                         int32_t window, int32_t sinks, float sm_scale, int32_t dtype, void *out, void *workspace,
+                         size_t workspace_bytes, void *stream) {
+  int32_t st = validate_paged(num_requests, num_pages, block_table_stride, num_q_heads, num_kv_heads, head_dim,
+                              page_size, sm_scale, dtype);
+  if (st != ADASERVE_OK) return st;
+  st = validate_decode(num_requests, num_q_heads, num_kv_heads, max_context, block_table_stride);
+  if (st != ADASERVE_OK) return st;
+  if (num_requests == 0) return ADASERVE_OK;
+  if (sees_all(window, sinks, max_context)) window = sinks = 0;
+  if (!q || !out || !context_len) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "a required device pointer is NULL");
+  st = validate_rows("q", q, num_requests, q_row_stride, (int64_t)num_q_heads * head_dim, elem_size(dtype));
+  if (st != ADASERVE_OK) return st;
+  if (!aligned(out, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "out must be 16-byte aligned");
+  st = validate_pages(max_context > 0, k_pages, v_pages, num_pages, block_table);
+  if (st != ADASERVE_OK) return st;
+  DecodePlan plan{};
+  if (!window) plan = decode_plan(num_requests, num_q_heads, num_kv_heads, head_dim, max_context);
+  st = validate_workspace(workspace, workspace_bytes, plan.ws_bytes);
+  if (st != ADASERVE_OK) return st;
+  st = check_device();
+  if (st != ADASERVE_OK) return st;
+  PagedAttnArgs a{};
+  a.num_requests = num_requests;
+  a.context_len = context_len;
+  a.block_table = block_table;
+  a.bt_stride = block_table_stride;
+  a.num_pages = num_pages;
+  a.q = q;
+  a.q_stride = q_row_stride;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.out = out;
+  a.total_tokens = num_requests;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = num_kv_heads;
+  a.group = num_q_heads / num_kv_heads;
+  a.max_context = max_context;
+  a.units_per_head = plan.units_per_head;
+  a.min_blocks = kDecodeMinBlocks;
+  if (plan.split) {
+    a.ws_request = (int32_t *)workspace;
+    a.ws_ml = (float *)((char *)workspace + plan.ml_offset);
+    a.ws_o = (float *)((char *)workspace + plan.o_offset);
+  }
+  a.sm_scale = sm_scale;
+  a.scale_log2 = sm_scale * 1.4426950408889634f;
+  a.window = window;
+  a.sinks = sinks;
+  if (window)
+    return launch_status(launch_window_rows(a, head_dim, dtype == ADASERVE_BF16, true, (hipStream_t)stream),
+                         "window attention launch");
+  return launch_status(launch_decode_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
+                       "decode attention launch");
+}
+
 }  // namespace
 
 extern "C" {
@@ -370,64 +513,38 @@ int32_t adaserve_prompt_attn(int32_t num_requests, const int32_t *token_indptr, 
                              const int32_t *context_len, const int32_t *context_len_host, int32_t num_q_heads,
                              int32_t num_kv_heads, int32_t head_dim, int32_t page_size, float sm_scale, int32_t dtype,
                              void *out, void *workspace, size_t workspace_bytes, void *stream) {
-  int32_t st = validate_paged(num_requests, num_pages, block_table_stride, num_q_heads, num_kv_heads, head_dim,
-                              page_size, sm_scale, dtype);
-  if (st != ADASERVE_OK) return st;
+  return prompt_attn_impl(num_requests, token_indptr, token_indptr_host, q, q_row_stride, k_pages, v_pages, num_pages,
+                          block_table, block_table_stride, context_len, context_len_host, num_q_heads, num_kv_heads,
+                          head_dim, page_size, 0, 0, sm_scale, dtype, out, workspace, workspace_bytes, stream);
+}
+
+size_t adaserve_window_prompt_attn_workspace_bytes(int32_t num_requests, const int32_t *token_indptr_host,
+                                                   const int32_t *context_len_host, int32_t num_q_heads,
+                                                   int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                                                   int32_t window, int32_t sinks, int32_t dtype) {
   int64_t total, most;
-  st = validate_prompt(num_requests, token_indptr_host, context_len_host, block_table_stride, num_q_heads, total, most);
+  if (validate_window(window, sinks) != ADASERVE_OK ||
+      validate_paged(num_requests, 0, 0, num_q_heads, num_kv_heads, head_dim, page_size, 1.f, dtype) != ADASERVE_OK ||
+      validate_prompt(num_requests, token_indptr_host, context_len_host, -1, num_q_heads, total, most) != ADASERVE_OK)
+    return SIZE_MAX;
+  if (!sees_all(window, sinks, most)) return 0;
+  return adaserve_prompt_attn_workspace_bytes(num_requests, token_indptr_host, context_len_host, num_q_heads,
+                                              num_kv_heads, head_dim, page_size, dtype);
+}
+
+int32_t adaserve_window_prompt_attn(int32_t num_requests, const int32_t *token_indptr,
+                                    const int32_t *token_indptr_host, const void *q, int64_t q_row_stride,
+                                    const void *k_pages, const void *v_pages, int32_t num_pages,
+                                    const int32_t *block_table, int32_t block_table_stride,
+                                    const int32_t *context_len, const int32_t *context_len_host, int32_t num_q_heads,
+                                    int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t window,
+                                    int32_t sinks, float sm_scale, int32_t dtype, void *out, void *workspace,
+                                    size_t workspace_bytes, void *stream) {
+  const int32_t st = validate_window(window, sinks);
   if (st != ADASERVE_OK) return st;
-  if (total == 0) return ADASERVE_OK;
-  if (!token_indptr || !q || !out || !context_len)
-    return fail(ADASERVE_ERR_INVALID_ARGUMENT, "a required device pointer is NULL");
-  st = validate_rows("q", q, total, q_row_stride, (int64_t)num_q_heads * head_dim, elem_size(dtype));
-  if (st != ADASERVE_OK) return st;
-  if (!aligned(out, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "out must be 16-byte aligned");
-  st = validate_pages(most > 0, k_pages, v_pages, num_pages, block_table);
-  if (st != ADASERVE_OK) return st;
-  const PromptPlan plan = prompt_plan(num_requests, token_indptr_host, context_len_host, num_q_heads, num_kv_heads,
-                                      head_dim, dtype == ADASERVE_BF16);
-  st = validate_workspace(workspace, workspace_bytes, plan.ws_bytes);
-  if (st != ADASERVE_OK) return st;
-  PromptAttnArgs a{};
-  a.num_requests = num_requests;
-  a.token_indptr = token_indptr;
-  a.context_len = context_len;
-  a.block_table = block_table;
-  a.bt_stride = block_table_stride;
-  a.num_pages = num_pages;
-  a.q = q;
-  a.q_stride = q_row_stride;
-  a.k_pages = k_pages;
-  a.v_pages = v_pages;
-  a.out = out;
-  a.total_tokens = (int32_t)total;
-  a.num_q_heads = num_q_heads;
-  a.num_kv_heads = num_kv_heads;
-  a.group = num_q_heads / num_kv_heads;
-  a.sm_scale = sm_scale;
-  a.scale_log2 = sm_scale * 1.4426950408889634f;
-  if (dtype == ADASERVE_BF16) {
-    fill_prompt(a, plan, token_indptr_host, context_len_host, kPromptTileRows, workspace);
-  } else {
-    // 32-row tiles read each key half as often, 16-row tiles put more units to work: 2250 tiles of 32
-    // (2 prompts of up to 1500 tokens, D = 128) 301 against 341 us, 1800 (8 of up to 300) 88 against 83
-    for (a.f32_rows = 32;; a.f32_rows = 16) {
-      a.units = 0;
-      for (int32_t r = 0; r < num_requests; ++r)
-        a.units += (int64_t)prompt_tiles(token_indptr_host[r + 1] - token_indptr_host[r], a.group, a.f32_rows) * num_kv_heads;
-      if (a.units >= 2048 || a.f32_rows == 16) break;
-    }
-    PromptPlan tiles;
-    tiles.units = a.units;
-    fill_prompt(a, tiles, token_indptr_host, context_len_host, a.f32_rows, nullptr);
-  }
-  // (the join's rows: below 2^17, those of 512 tiles)
-  st = validate_launch("prompt attention", dtype == ADASERVE_BF16 ? a.grid : round_up(a.units, kPromptGrid), kServingThreads);
-  if (st != ADASERVE_OK) return st;
-  st = check_device();
-  if (st != ADASERVE_OK) return st;
-  return launch_status(launch_prompt_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
-                       "prompt attention launch");
+  return prompt_attn_impl(num_requests, token_indptr, token_indptr_host, q, q_row_stride, k_pages, v_pages, num_pages,
+                          block_table, block_table_stride, context_len, context_len_host, num_q_heads, num_kv_heads,
+                          head_dim, page_size, window, sinks, sm_scale, dtype, out, workspace, workspace_bytes, stream);
 }
 
 size_t adaserve_decode_attn_workspace_bytes(int32_t num_requests, int32_t max_context, int32_t num_q_heads,
@@ -444,50 +561,34 @@ int32_t adaserve_decode_attn(int32_t num_requests, const void *q, int64_t q_row_
                              int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
                              float sm_scale, int32_t dtype, void *out, void *workspace, size_t workspace_bytes,
                              void *stream) {
-  int32_t st = validate_paged(num_requests, num_pages, block_table_stride, num_q_heads, num_kv_heads, head_dim,
-                              page_size, sm_scale, dtype);
+  return decode_attn_impl(num_requests, q, q_row_stride, k_pages, v_pages, num_pages, block_table, block_table_stride,
+                          context_len, max_context, num_q_heads, num_kv_heads, head_dim, page_size, 0, 0, sm_scale,
+                          dtype, out, workspace, workspace_bytes, stream);
+}
+
+size_t adaserve_window_decode_attn_workspace_bytes(int32_t num_requests, int32_t max_context, int32_t num_q_heads,
+                                                   int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                                                   int32_t window, int32_t sinks, int32_t dtype) {
+  if (validate_window(window, sinks) != ADASERVE_OK ||
+      validate_paged(num_requests, 0, 0, num_q_heads, num_kv_heads, head_dim, page_size, 1.f, dtype) != ADASERVE_OK ||
+      validate_decode(num_requests, num_q_heads, num_kv_heads, max_context, -1) != ADASERVE_OK)
+    return SIZE_MAX;
+  if (!sees_all(window, sinks, max_context)) return 0;
+  return adaserve_decode_attn_workspace_bytes(num_requests, max_context, num_q_heads, num_kv_heads, head_dim, page_size,
+                                              dtype);
+}
+
+int32_t adaserve_window_decode_attn(int32_t num_requests, const void *q, int64_t q_row_stride, const void *k_pages,
+                                    const void *v_pages, int32_t num_pages, const int32_t *block_table,
+                                    int32_t block_table_stride, const int32_t *context_len, int32_t max_context,
+                                    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                                    int32_t window, int32_t sinks, float sm_scale, int32_t dtype, void *out,
+                                    void *workspace, size_t workspace_bytes, void *stream) {
+  const int32_t st = validate_window(window, sinks);
   if (st != ADASERVE_OK) return st;
-  st = validate_decode(num_requests, num_q_heads, num_kv_heads, max_context, block_table_stride);
-  if (st != ADASERVE_OK) return st;
-  if (num_requests == 0) return ADASERVE_OK;
-  if (!q || !out || !context_len) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "a required device pointer is NULL");
-  st = validate_rows("q", q, num_requests, q_row_stride, (int64_t)num_q_heads * head_dim, elem_size(dtype));
-  if (st != ADASERVE_OK) return st;
-  if (!aligned(out, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "out must be 16-byte aligned");
-  st = validate_pages(max_context > 0, k_pages, v_pages, num_pages, block_table);
-  if (st != ADASERVE_OK) return st;
-  const DecodePlan plan = decode_plan(num_requests, num_q_heads, num_kv_heads, head_dim, max_context);
-  st = validate_workspace(workspace, workspace_bytes, plan.ws_bytes);
-  if (st != ADASERVE_OK) return st;
-  st = check_device();
-  if (st != ADASERVE_OK) return st;
-  PagedAttnArgs a{};
-  a.num_requests = num_requests;
-  a.context_len = context_len;
-  a.block_table = block_table;
-  a.bt_stride = block_table_stride;
-  a.num_pages = num_pages;
-  a.q = q;
-  a.q_stride = q_row_stride;
-  a.k_pages = k_pages;
-  a.v_pages = v_pages;
-  a.out = out;
-  a.total_tokens = num_requests;
-  a.num_q_heads = num_q_heads;
-  a.num_kv_heads = num_kv_heads;
-  a.group = num_q_heads / num_kv_heads;
-  a.max_context = max_context;
-  a.units_per_head = plan.units_per_head;
-  a.min_blocks = kDecodeMinBlocks;
-  if (plan.split) {
-    a.ws_request = (int32_t *)workspace;
-    a.ws_ml = (float *)((char *)workspace + plan.ml_offset);
-    a.ws_o = (float *)((char *)workspace + plan.o_offset);
-  }
-  a.sm_scale = sm_scale;
-  a.scale_log2 = sm_scale * 1.4426950408889634f;
-  return launch_status(launch_decode_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
-                       "decode attention launch");
+  return decode_attn_impl(num_requests, q, q_row_stride, k_pages, v_pages, num_pages, block_table, block_table_stride,
+                          context_len, max_context, num_q_heads, num_kv_heads, head_dim, page_size, window, sinks,
+                          sm_scale, dtype, out, workspace, workspace_bytes, stream);
 }
 
 size_t adaserve_sample_workspace_bytes(int32_t num_rows, int32_t vocab, int32_t dtype) {

@@ -77,6 +77,7 @@ struct PagedAttnArgs {
   int32_t group;                 // Hq / Hkv
   float sm_scale;
   float scale_log2;              // sm_scale * log2(e)
+  int32_t window, sinks;         // a row sees the newest `window` positions and the first `sinks` (window 0: all)
   // prompt attention
   int64_t units;                 // tiles of all heads, times chunks
   int32_t chunks;                // most chunks of keys per tile: 1 unless there are few tiles
@@ -140,6 +141,9 @@ inline DecodePlan decode_plan(int32_t B, int32_t hq, int32_t hkv, int32_t head_d
 
 hipError_t launch_prompt_attn(const PromptAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
 hipError_t launch_decode_attn(const PagedAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
+// Attention over a window and sinks, row by row (window_attn.hip): of prompts,
+// or of one token per request.
+hipError_t launch_window_rows(const PagedAttnArgs &a, int head_dim, bool bf16, bool decode, hipStream_t stream);
 
 constexpr int kSampleMaxVocab = 1 << 20;   // sums of 2^32 per token stay below 2^53
 
