@@ -53,6 +53,7 @@ constexpr int kThreads = kServingThreads;
 constexpr int kWaves = kThreads / 64;
 constexpr float kLowest = -FLT_MAX;     // running maximum before any key
 constexpr float kRescaleLog2 = 8.f;
+constexpr int kPagesPerBlock = kKeysPerBlock / kPageSize;
 
 // The batch's 32-key blocks in one line, request after request; unit u takes
 // blocks [lo, hi) of it.
@@ -65,10 +66,19 @@ struct DecodeUnit {
 
 __device__ __forceinline__ int32_t decode_blocks(int32_t len) { return len > 0 ? (len + kKeysPerBlock - 1) / kKeysPerBlock : 0; }
 
+// Over a window: the keys of a request of `len` that are read, numbered through
+// (WindowSpan).
+template <bool WINDOW>
+__device__ __forceinline__ int32_t decode_len(const PagedAttnArgs &a, int32_t len) {
+  if (!WINDOW || len <= 0) return len;
+  return len - window_span(len - a.window, a.sinks, kKeysPerBlock).shift * kKeysPerBlock;
+}
+
 // Unit u, from all lengths: every unit has `per` blocks but for the last one.
 // Each thread takes 1 to 4 neighbouring requests (at most kDecodeSplitRequests
 // in all); start[] gets each request's first block, len[] its length (-1: out of
 // range).  False: no such unit.
+template <bool WINDOW>
 __device__ __forceinline__ bool schedule(const PagedAttnArgs &a, int32_t u, int32_t *start, int32_t *len, DecodeUnit &un) {
   __shared__ int32_t part[2][kWaves];
   __shared__ int32_t first;
@@ -82,7 +92,7 @@ __device__ __forceinline__ bool schedule(const PagedAttnArgs &a, int32_t u, int3
     if (i < per_thread && r < a.num_requests) {
       const int32_t x = a.context_len[r], ok = x >= 0 && x <= a.max_context ? x : -1;
       len[r] = ok;
-      nb[i] = decode_blocks(ok);
+      nb[i] = decode_blocks(decode_len<WINDOW>(a, ok));
     }
     mine += nb[i];
   }
@@ -141,7 +151,7 @@ __device__ __forceinline__ bool schedule(const PagedAttnArgs &a, int32_t u, int3
         bool before = false;
         if (i > 0) before = is_in(at - space(nb[i - 1]), nb[i - 1]);
         else if (r > 0) {
-          const int32_t x = a.context_len[r - 1], n = decode_blocks(x <= a.max_context ? x : -1);
+          const int32_t x = a.context_len[r - 1], n = decode_blocks(decode_len<WINDOW>(a, x <= a.max_context ? x : -1));
           before = is_in(at - space(n), n);
         }
         if (!before) first = r;
@@ -160,9 +170,11 @@ struct Run {
   int32_t k0, k1;     // its keys
   int32_t nb, mine;   // blocks of the wave's size; this wave's: wave, wave + 4, ...
   int32_t slot;       // of the workspace: 2 u + 1 where it begins a request, 2 u where it goes on with one; -1: all of it
+  WindowSpan span;    // over a window: where the keys stand in the cache,
+  int32_t lo;         // and the window's first one: those from the sinks to it are not seen
 };
 
-template <bool BF16, int D>
+template <bool BF16, int D, bool WINDOW>
 __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs a) {
   constexpr int T = BF16 ? 2 : 1;          // 16-key tiles (pages) per block of a wave
   constexpr int KB = T * 16;
@@ -181,7 +193,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
   const int rows = a.group;
   const bool split = a.ws_request != nullptr;
   DecodeUnit un{0, INT32_MAX, u, 0, false};
-  if (split && !schedule(a, u, start, lens, un)) return;
+  if (split && !schedule<WINDOW>(a, u, start, lens, un)) return;
 
   // The unit's run of request r or of the first one after it that has keys
   // there; the rows of the empty requests on the way become zeros, of lengths
@@ -205,6 +217,12 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
           else ((float *)a.out)[at + i] = x;
         }
         continue;
+      }
+      if (WINDOW) {
+        const int32_t first = len - a.window;
+        run.span = window_span(first, a.sinks, kKeysPerBlock);
+        run.lo = first - run.span.shift * kKeysPerBlock;
+        len -= run.span.shift * kKeysPerBlock;
       }
       const int32_t end = from + decode_blocks(len);
       const int32_t b0 = max(from, un.lo), b1 = min(end, un.hi);
@@ -231,9 +249,11 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
   auto page_ids = [&](const Run &w, int base) -> int32_t {
     const int i = base + lane;                       // tile of the wave
     const int32_t b = wave + (i / T) * kWaves;
-    const int32_t e = (w.k0 + b * KB) / kPageSize + i % T;
+    int32_t e = (w.k0 + b * KB) / kPageSize + i % T;
     int32_t p = -1;
-    if (b < w.nb && e < a.bt_stride && e * kPageSize < w.k1) {
+    const bool inside = b < w.nb && e * kPageSize < w.k1;
+    if (WINDOW) e = w.span.real(e / kPagesPerBlock) * kPagesPerBlock + e % kPagesPerBlock;
+    if (inside && e < a.bt_stride) {
       p = a.block_table[(int64_t)w.r * a.bt_stride + e];
       if (p < 0 || p >= a.num_pages) p = -1;
     }
@@ -332,13 +352,16 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
     const int32_t left = run.k1 - (run.k0 + (wave + i * kWaves) * KB);   // keys of the block and after
     float p[T][4];
     float bm = kLowest;
-    const bool edge = left < KB;
+    // over a window: the block's keys [cut0, cut1) are not seen
+    const int32_t cut0 = WINDOW ? left - run.k1 + a.sinks : 0, cut1 = WINDOW ? left - run.k1 + run.lo : 0;
+    const bool edge = left < KB || (WINDOW && cut0 < KB && cut1 > 0);
+    auto unseen = [&](int key) { return key >= left || (WINDOW && key >= cut0 && key < cut1); };
 #pragma unroll
     for (int t = 0; t < T; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float x = hk[t] ? s[t][e] * a.scale_log2 : 0.f;
-        p[t][e] = !edge || t * 16 + quad * 4 + e < left ? x : -INFINITY;
+        p[t][e] = !edge || !unseen(t * 16 + quad * 4 + e) ? x : -INFINITY;
         bm = fmaxf(bm, p[t][e]);
       }
     bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
@@ -365,7 +388,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(PagedAttnArgs 
       if (edge || !have_v[t]) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (!have_v[t] || t * 16 + quad * 4 + e >= left)
+          if (!have_v[t] || unseen(t * 16 + quad * 4 + e))
 #pragma unroll
             for (int w = 0; w < NV; ++w) vr[t][e][w] = 0;
       }
@@ -542,7 +565,8 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(PagedAttnArgs a) 
 template <bool BF16, int D>
 hipError_t launch(const PagedAttnArgs &a, hipStream_t stream) {
   const int64_t blocks = (int64_t)a.units_per_head * a.num_kv_heads;
-  hipLaunchKernelGGL((decode_attn_kernel<BF16, D>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+  if (a.window) hipLaunchKernelGGL((decode_attn_kernel<BF16, D, true>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((decode_attn_kernel<BF16, D, false>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.ws_request) return e;
   hipLaunchKernelGGL((decode_join_kernel<BF16, D>), dim3((unsigned)((int64_t)a.num_requests * a.num_q_heads)),

@@ -74,6 +74,29 @@ ADASERVE_HD int64_t request_units(int32_t n_nodes, int32_t prefix_len, int32_t n
          prefix_chunks(prefix_len, chunk_keys(n_nodes, group, rows_per_tile, chunk_target, floor_mult));
 }
 
+// What attention over a window and sinks reads of a request's keys, in blocks:
+// those of the sinks, then those from the first one that any row's window
+// reaches on.  Kernels number these blocks (and their keys) through; block b is
+// block real(b) of the cache.  Without a gap there is no shift.
+struct WindowSpan {
+  int32_t sink_blocks, shift;
+  ADASERVE_HD int32_t real(int32_t b) const { return b < sink_blocks ? b : b + shift; }
+};
+
+// `first`: the first key of the first row's window (below 0: all keys are in it).
+ADASERVE_HD WindowSpan window_span(int32_t first, int32_t sinks, int32_t block) {
+  const int32_t lo = first > 0 ? first / block : 0;
+  const int32_t s = sinks > 0 ? (sinks - 1) / block + 1 : 0;
+  return {s < lo ? s : lo, s < lo ? lo - s : 0};
+}
+
+// Most keys of a row tile of `tokens` neighbouring positions, numbered through,
+// that a call with keys of its own of at most `context` reads.
+ADASERVE_HD int32_t window_keys(int32_t context, int32_t window, int32_t sinks, int32_t tokens) {
+  const int64_t most = (int64_t)window + tokens + 2 * kKeysPerBlock + sinks;
+  return most < context ? (int32_t)most : context;
+}
+
 // Requests in descending order of per-unit cost, carried in the kernel
 // arguments so a workgroup finds its unit without touching memory.  Batches
 // with more requests fall back to a scan of node_indptr / prefix_len.

@@ -30,6 +30,7 @@
 #include "paged_rows.h"
 #include "plan.h"
 #include "serving.h"
+#include "window_rows.h"
 
 namespace adaserve {
 
@@ -132,6 +133,13 @@ __device__ __forceinline__ int64_t prompt_round_unit(int64_t b, int64_t k, int64
   return k * grid + in;
 }
 
+// Over a window a tile's keys are numbered through (WindowSpan of its first row).
+template <bool WINDOW>
+__device__ __forceinline__ WindowSpan prompt_span(const PromptAttnArgs &a, const PromptUnit &un, int32_t tile_rows, int32_t block) {
+  if (!WINDOW) return {0, 0};
+  return window_span(un.ctx - un.n + 1 + un.tile * tile_rows / a.group - a.window, a.sinks, block);
+}
+
 // 64 rows per wave, one wave per SIMD.  The two 32-row halves of a wave run
 // half a sub-block apart, so that the matrix products of one half always meet
 // the softmax of the other in the instruction stream:
@@ -139,7 +147,12 @@ __device__ __forceinline__ int64_t prompt_round_unit(int64_t b, int64_t k, int64
 //   phase B:                S1(i+1) = K Q1, O1 += V P1(i)  beside  P0(i+1) from S0(i+1)
 // Both halves take the same K and V fragments from registers; the next ones
 // are read in phase B as the current ones are used up.
-template <int D>
+//
+// Over a window the tile's keys begin with the sinks' blocks and the one that the
+// first row's window begins in; from them to the first block that all rows of the
+// wave see, and once beyond (a row's reference comes from the first keys that it
+// sees), blocks are masked and maxima taken.
+template <int D, bool WINDOW>
 __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAttnArgs a) {
   constexpr int KS = D / 16, DT = D / 32, KB = 32, ROWB = D * 2, NCH = D / 8;
   constexpr int BLK = KB * ROWB;
@@ -162,6 +175,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   // of their joined chunks, within fp32.
   constexpr float kMost = 0x1p64f, kMostOut = 0x1p120f;
   __shared__ int redo;
+  __shared__ RowScratch<D> scratch[WINDOW ? kWaves : 1];
   __shared__ __align__(1024) char ring[NST * STAGE];   // (K of sub-block 0: in the last stage at first)
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -175,17 +189,28 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   // what follows from the unit
   int32_t row_end, wrow0, first, k_end, nb, wave_nb, n_full;
   int64_t head_bytes;
+  // over a window: the first key that any row sees there, the sinks (of the unit's
+  // keys, numbered through), the blocks before the one from which on all are
+  // loaded whole, and those before the common path
+  int32_t lo = 0, sinks = 0, n_cut = 0, n_edge = 0;
   auto derive = [&]() __attribute__((always_inline)) {
     const int32_t row0 = un.tile * kTileRows;
     row_end = min(un.n * G, row0 + kTileRows);
     wrow0 = row0 + wave * 64;
-    first = un.ctx - un.n + 1 - un.k0;            // keys (of the unit's) that token 0 sees
+    first = un.ctx - un.n + 1 - un.k0 - prompt_span<WINDOW>(a, un, kTileRows, KB).shift * KB;   // keys (of the unit's) that token 0 sees
     // keys that the tile's (the wave's) last row sees; sub-blocks whose keys the wave's rows all see
     k_end = min(max(0, first + (row_end - 1) / G), a.chunk_keys);
     const int32_t wave_end = wrow0 < row_end ? min(max(0, first + (min(row_end, wrow0 + 64) - 1) / G), a.chunk_keys) : 0;
     nb = (k_end + KB - 1) / KB;
     wave_nb = (wave_end + KB - 1) / KB;
     n_full = min(wave_nb, max(0, first + wrow0 / G) / KB);
+    if constexpr (WINDOW) {
+      lo = first + row0 / G - a.window;
+      sinks = a.sinks - un.k0;
+      const int32_t last_lo = first + (min(row_end, wrow0 + 64) - 1) / G - a.window;
+      n_cut = (max(lo, 0) + KB - 1) / KB;
+      n_edge = last_lo > 0 ? (last_lo + KB - 1) / KB + 1 : 0;
+    }
     head_bytes = (int64_t)un.g * kPageSize * D * 2;
   };
   derive();
@@ -200,12 +225,14 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   // 16 ragged prompts, half of them such, 386 -> 364 us)
   bool all_pages;
   auto load_pages = [&](const PromptUnit &of, int base) __attribute__((always_inline)) -> int32_t {
-    const int32_t e = of.k0 / kPageSize + (base + lane) * (KB / kPageSize) + wave_page;
+    int32_t e = of.k0 / kPageSize + (base + lane) * (KB / kPageSize) + wave_page;
+    if constexpr (WINDOW)
+      e = prompt_span<WINDOW>(a, of, kTileRows, KB).real(of.k0 / KB + base + lane) * (KB / kPageSize) + wave_page;
     return e < a.bt_stride && e < (of.ctx + kPageSize - 1) / kPageSize ? a.block_table[(int64_t)of.r * a.bt_stride + e] : -1;
   };
   auto take_pages = [&](int32_t ids) __attribute__((always_inline)) {
     pages = ids >= 0 && ids < a.num_pages ? ids : -1;
-    all_pages = all_pages && !__any(pages < 0 && window + lane < k_end / KB);
+    all_pages = all_pages && !__any(pages < 0 && window + lane < k_end / KB && window + lane >= n_cut);
     pages_after = load_pages(un, window + 64);
   };
   auto next_window = [&]() __attribute__((always_inline)) {
@@ -216,13 +243,15 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   // Query fragments (B operand of S^T = K Q^T): lane holds row (lane & 31) of
   // each half, head-dim elements ks*16 + (lane >> 5)*8 .. +7.
   bf16x8 qf[2][KS];
-  int32_t vis[2];   // keys that the row sees
+  int32_t vis[2];     // keys that the row sees,
+  int32_t vis_lo[2];  // over a window those from here on, and the sinks
   auto load_q = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
       const int32_t row = min(wrow0 + rt * 32 + (lane & 31), row_end - 1);   // (a row past the end repeats the last)
       const int32_t tok = row / G, head = un.g * G + row - tok * G;
       vis[rt] = min(first + tok, a.chunk_keys);
+      vis_lo[rt] = first + tok - a.window;
       const __bf16 *qp = (const __bf16 *)a.q + (int64_t)(un.token0 + tok) * a.q_stride + (int64_t)head * D + half * 8;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) qf[rt][ks] = *(const bf16x8 *)(qp + ks * 16);
@@ -246,15 +275,18 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   const uint32_t wave_lds = lds_addr(ring) + wave * WI * 1024;
   const void *zeros = zero_line;
   asm volatile("" : "+s"(zeros));   // (its address is looked up once)
-  // Sub-block blk of K or V into LDS at `dst`; rows past the tile's keys and
-  // pages that do not exist come from the zero line, so that every stage is the
+  // Sub-block blk of K or V into LDS at `dst`; rows past the tile's keys, those that no
+  // row's window holds, and pages that do not exist come from the zero line, so that every stage is the
   // same number of loads.
   auto issue = [&](const void *pool, uint32_t dst, int blk, int32_t page) __attribute__((always_inline)) {
     const int32_t left = page >= 0 ? k_end - blk * KB : 0;
     const char *base = (const char *)pool + (int64_t)max(page, 0) * page_bytes + head_bytes;
 #pragma unroll
-    for (int i = 0; i < WI; ++i)
-      dma16<false>(dma_row[i] < left ? (const void *)(base + page_off[i]) : zeros, dst + i * 1024);
+    for (int i = 0; i < WI; ++i) {
+      bool seen = dma_row[i] < left;
+      if constexpr (WINDOW) seen = seen && (blk * KB + dma_row[i] >= lo || blk * KB + dma_row[i] < sinks);
+      dma16<false>(seen ? (const void *)(base + page_off[i]) : zeros, dst + i * 1024);
+    }
   };
   // Stage i's loads: K first, then V.
   int32_t page = -1;   // of sub-block i (before stage i's loads)
@@ -301,8 +333,12 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   };
   auto mask = [&](f32x16 &x, int rt, int blk) {
     const int32_t left = vis[rt] - blk * KB - half * 4;
+    const int32_t from = vis_lo[rt] - blk * KB - half * 4, sunk = sinks - blk * KB - half * 4;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = (i >> 2) * 8 + (i & 3) < left ? x[i] : -INFINITY;
+    for (int i = 0; i < 16; ++i) {
+      const int key = (i >> 2) * 8 + (i & 3);
+      x[i] = key < left && (!WINDOW || key >= from || key < sunk) ? x[i] : -INFINITY;
+    }
   };
   auto rowmax = [&](const f32x16 &x) {
     float m0 = x[0], m1 = x[1];
@@ -315,10 +351,14 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
     return max_over_halves(__builtin_elementwise_maximum(__builtin_elementwise_maximum(m0, m1), x[15]));
   };
   // Takes row half rt's reference up to the maximum bm of sub-block scores where
-  // that is more than 2^8 above it.
+  // that is more than 2^8 above it.  Over a window that is done behind blocks without
+  // maxima, too: `beyond` keeps that their sums were further than with maxima, which
+  // the checks at the end no longer see (and a factor below 2^-126 loses them).
+  bool beyond = false;
   auto rescale = [&](int rt, float bm) __attribute__((always_inline)) {
     const bool up = bm > m_ref[rt] + up_raw;
     if (__any(up)) {
+      if (WINDOW) beyond = beyond || (up && !(lsum[rt] <= 0x1p8f * (float)k_end));
       const float mn = up ? bm : m_ref[rt];
       const float al = __builtin_amdgcn_exp2f((m_ref[rt] - mn) * c);
       m_ref[rt] = mn;
@@ -358,7 +398,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
     constexpr bool kDma = decltype(dma)::value;
     constexpr int SLOTS = KS + 2 * DT;   // matrix instructions
     if constexpr (kMasked) mask(sy, ry, yblk);
-    if (kMasked && careful) rescale(ry, rowmax(sy));
+    if (kMasked && (WINDOW || careful)) rescale(ry, rowmax(sy));
     // A slot is one matrix instruction and the vector work that issues while it
     // runs: one step each of a few weights (scale; exponential; sum and
     // rounding), none of which waits for another, and two LDS reads.  The empty
@@ -480,6 +520,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   start(load_pages(un, 0));
 #pragma unroll 1
   for (;;) {
+    beyond = false;
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
       lsum[rt] = 0.f;
@@ -523,7 +564,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
     while (i < nb) {
       if (!careful && (i & 3) == 0) {
 #pragma unroll 1
-        for (; i + 4 < n_full && (k_end % KB == 0 || i + 8 < k_end / KB); i += 4) {
+        for (; i + 4 < n_full && i >= n_edge && (k_end % KB == 0 || i + 8 < k_end / KB); i += 4) {
           if (i + 8 >= window + 64) break;   // (the other path moves the window)
           if (!all_pages) break;
           full_sub(i, std::integral_constant<int, 0>{});
@@ -532,14 +573,14 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
           full_sub(i + 3, std::integral_constant<int, 3>{});
         }
       }
-      if (i == n_full) {   // hidden keys from here on
+      if (!WINDOW && i == n_full) {   // hidden keys from here on
         had_nan[0] = is_nan(0);
         had_nan[1] = is_nan(1);
       }
       any_sub(i++);
     }
     if (!careful) {
-      bool beyond = !(lsum[0] < kMost) || !(lsum[1] < kMost);
+      beyond = beyond || !(lsum[0] < kMost) || !(lsum[1] < kMost);
       // (rarely: 2 x 16 DT comparisons)
       const float fair = 0x1p8f * (float)k_end;
       if (__any(fmaxf(lsum[0], lsum[1]) > fair)) {
@@ -615,7 +656,9 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
       while (todo) {
         const int l = __ffsll(todo) - 1;
         todo &= todo - 1;
-        attend_row<true, D>(a, done.r, done.token0 + __shfl(tok, l, 64), __shfl(head, l, 64), __shfl(done_vis[rt], l, 64));
+        const int32_t t = done.token0 + __shfl(tok, l, 64), h = __shfl(head, l, 64);
+        if constexpr (WINDOW) attend_seen<true, D>(a, done.r, t, h, done.ctx - done.n + (t - done.token0), scratch[wave]);
+        else attend_row<true, D>(a, done.r, t, h, __shfl(done_vis[rt], l, 64));
       }
     }
     if (!more) return;
@@ -624,7 +667,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
 
 // Joins the chunks of split keys: with m the largest reference of the row's
 // chunks, out = sum 2^(m_c - m) o_c / sum 2^(m_c - m) l_c.  One wave per row.
-template <int D>
+template <int D, bool WINDOW>
 __global__ __launch_bounds__(kThreads) void prompt_join_kernel(PromptAttnArgs a) {
   constexpr int EPL = D / 64;
   const int lane = threadIdx.x & 63;
@@ -647,7 +690,9 @@ __global__ __launch_bounds__(kThreads) void prompt_join_kernel(PromptAttnArgs a)
   const int32_t tile = row / kTileRows;
   const int32_t level = a.table[e].unit_end / a.num_kv_heads - 1 - tile;
   const int32_t seen = max(0, a.table[e].ctx - a.table[e].n + 1 + (t - a.table[e].token0));
-  const int32_t chunks = min(a.chunks, (seen + a.chunk_keys - 1) / a.chunk_keys);
+  const PromptUnit un{a.table[e].request, a.table[e].token0, a.table[e].n, a.table[e].ctx, tile, g, 0};
+  const int32_t keys = max(0, seen - prompt_span<WINDOW>(a, un, kTileRows, kKeysPerBlock).shift * kKeysPerBlock);
+  const int32_t chunks = min(a.chunks, (keys + a.chunk_keys - 1) / a.chunk_keys);
   float m = -1e30f, l = 0.f, o[EPL] = {};
   for (int c = 0; c < chunks; ++c) {
     const int64_t slot = (((int64_t)level * a.chunks + c) * a.num_kv_heads + g) * kTileRows + (row - tile * kTileRows);
@@ -663,7 +708,12 @@ __global__ __launch_bounds__(kThreads) void prompt_join_kernel(PromptAttnArgs a)
     for (int i = 0; i < EPL; ++i) o[i] = o[i] * f + w * x[i];
   }
   if (m == INFINITY) {
-    attend_row<true, D>(a, a.table[e].request, t, h, seen);
+    if constexpr (WINDOW) {
+      __shared__ RowScratch<D> scratch[kWaves];
+      attend_seen<true, D>(a, un.r, t, h, seen - 1, scratch[threadIdx.x >> 6]);
+    } else {
+      attend_row<true, D>(a, un.r, t, h, seen);
+    }
     return;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;   // (a NaN stays one)
@@ -685,7 +735,7 @@ __global__ __launch_bounds__(kThreads) void prompt_join_kernel(PromptAttnArgs a)
 // 1500 tokens (32 heads on 8, D = 128) 351 us, 105 TFLOP/s (a library product: 154),
 // matrix cores busy 0.70 of the time and 7.5 TB/s out of the L2s; the 3 prompts
 // above 0.41 and 8.6 TB/s.
-template <int D, int RB>
+template <int D, int RB, bool WINDOW>
 __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArgs a) {
   constexpr int RT = 16 * RB;
   constexpr int NC = D / 16;      // 16-byte K loads per lane and page
@@ -694,6 +744,7 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArg
   __shared__ __align__(16) float mo[kWaves * RT * LDO];
   __shared__ float mw[kWaves][RT], lw[kWaves][RT];
   __shared__ int taken[RT];
+  __shared__ RowScratch<D> scratch[WINDOW ? kWaves : 1];
   const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, j = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = a.group;
@@ -707,8 +758,12 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArg
   const int r = __builtin_amdgcn_readfirstlane(un.r);
   const int32_t token0 = un.token0, n = un.n, ctx = un.ctx, tile = un.tile, g = un.g;
   const int32_t row0 = tile * RT, row_end = min(n * G, row0 + RT);
-  const int32_t first = ctx - n + 1;
+  const WindowSpan span = prompt_span<WINDOW>(a, un, RT, kPageSize);
+  const int32_t first = ctx - n + 1 - span.shift * kPageSize;
   const int32_t k_end = max(0, first + (row_end - 1) / G);
+  // over a window: the first key that any row sees there, and pages before those that all rows see
+  const int32_t lo = WINDOW ? first + row0 / G - a.window : 0;
+  const int32_t n_edge = WINDOW ? (max(0, first + (row_end - 1) / G - a.window) + 15) / 16 : 0;
   const int32_t n_full = max(0, first + row0 / G) / 16;   // pages that all rows see
   const int32_t nb = (k_end + 15) / 16;
   const int32_t b0 = (int32_t)((int64_t)nb * wave / kWaves), b1 = (int32_t)((int64_t)nb * (wave + 1) / kWaves);
@@ -728,8 +783,9 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArg
   auto load_pages = [&]() {
     const int b = page_base + lane;
     pages = -1;
-    if (b < nb && b < a.bt_stride) {
-      const int32_t p = a.block_table[(int64_t)r * a.bt_stride + b];
+    const int e = WINDOW ? span.real(b) : b;
+    if (b < nb && e < a.bt_stride) {
+      const int32_t p = a.block_table[(int64_t)r * a.bt_stride + e];
       if (p >= 0 && p < a.num_pages) pages = p;
     }
   };
@@ -785,7 +841,7 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArg
     load_v(page);
   }
   for (int b = b0; b < b1; ++b) {
-    if (b == n_full || (b == b0 && b > n_full))
+    if (!WINDOW && (b == n_full || (b == b0 && b > n_full)))
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) had_nan[rb] = is_nan(rb);
     const int32_t next = page_of(min(b + 1, b1 - 1));
@@ -801,13 +857,15 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArg
           s[rb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[c][e], qf[rb][c][e], s[rb], 0, 0, 0);
     load_k(next);
     // s[rb][e]: key 4 q + e of the page, row j; in log2 units from here on
-    const bool masked = b >= n_full, none = page < 0;
+    const bool masked = b >= n_full || (WINDOW && b < n_edge), none = page < 0;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float x = none ? 0.f : s[rb][e] * a.scale_log2;
-        s[rb][e] = !masked || b * 16 + q * 4 + e < vis[rb] ? x : -INFINITY;
+        const int32_t key = b * 16 + q * 4 + e;
+        const bool seen = key < vis[rb] && (!WINDOW || key >= vis[rb] - a.window || key < a.sinks);
+        s[rb][e] = !masked || seen ? x : -INFINITY;
       }
       const float bm = max_over_lane_rows(fmax3(s[rb][0], s[rb][1], __builtin_elementwise_maximum(s[rb][2], s[rb][3])));
       if (__any(bm > m[rb])) {
@@ -826,12 +884,15 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArg
       }
     }
     // a slot past the tile's keys may hold anything
-    if (none || b * 16 + 16 > k_end) {
+    const bool cut = WINDOW && b * 16 < lo;
+    if (none || b * 16 + 16 > k_end || cut) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int e = 0; e < 4; ++e) {
+        const int32_t key = b * 16 + q * 4 + e;
 #pragma unroll
         for (int h = 0; h < NH; ++h)
-          if (none || b * 16 + q * 4 + e >= k_end) vr[e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (none || key >= k_end || (cut && key < lo && key >= a.sinks)) vr[e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -853,7 +914,7 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArg
     const float ls = sum_over_lane_rows(l[rb]);
     // a key that the row does not see has weight 0, and 0 times an infinite value
     // is NaN: such rows are taken again, key by key
-    if (b1 > n_full && is_nan(rb) && !had_nan[rb]) taken[rl] = 1;
+    if ((WINDOW || b1 > n_full) && is_nan(rb) && !had_nan[rb]) taken[rl] = 1;
     if (q == 0) {
       mw[wave][rl] = m[rb];
       lw[wave][rl] = ls;
@@ -889,41 +950,40 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArg
   for (int rl = wave; rl < RT && row0 + rl < row_end; rl += kWaves)
     if (taken[rl]) {
       const int tok = (row0 + rl) / G, head = g * G + row0 + rl - tok * G;
-      attend_row<false, D>(a, r, token0 + tok, head, first + tok);
+      if constexpr (WINDOW) attend_seen<false, D>(a, r, token0 + tok, head, ctx - n + tok, scratch[wave]);
+      else attend_row<false, D>(a, r, token0 + tok, head, first + tok);
     }
 }
 
-template <int D, int RB>
-void launch_prompt_f32(const PromptAttnArgs &a, int64_t units, hipStream_t stream) {
-  const int64_t blocks = (units + kPromptGrid - 1) / kPromptGrid * kPromptGrid;   // whole rounds
-  hipLaunchKernelGGL((prompt_attn_f32_kernel<D, RB>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+template <int D, bool WINDOW>
+hipError_t launch_bf16(const PromptAttnArgs &a, hipStream_t stream) {
+  const dim3 block(kThreads);
+  hipLaunchKernelGGL((prompt_attn_bf16_kernel<D, WINDOW>), dim3((unsigned)a.grid), block, 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.chunks <= 1) return e;
+  const dim3 rows((unsigned)(((int64_t)a.total_tokens * a.num_q_heads + kWaves - 1) / kWaves));
+  hipLaunchKernelGGL((prompt_join_kernel<D, WINDOW>), rows, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int D, bool WINDOW>
+hipError_t launch_f32(const PromptAttnArgs &a, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.units + kPromptGrid - 1) / kPromptGrid * kPromptGrid)), block(kThreads);   // whole rounds
+  if (a.f32_rows == 32) hipLaunchKernelGGL((prompt_attn_f32_kernel<D, 2, WINDOW>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((prompt_attn_f32_kernel<D, 1, WINDOW>), grid, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int D, bool WINDOW>
+hipError_t launch(const PromptAttnArgs &a, bool bf16, hipStream_t stream) {
+  return bf16 ? launch_bf16<D, WINDOW>(a, stream) : launch_f32<D, WINDOW>(a, stream);
 }
 
 }  // namespace
 
 hipError_t launch_prompt_attn(const PromptAttnArgs &a, int head_dim, bool bf16, hipStream_t stream) {
-  const dim3 block(kThreads);
-  if (bf16) {
-    const dim3 grid((unsigned)a.grid);
-    if (head_dim == 128) hipLaunchKernelGGL((prompt_attn_bf16_kernel<128>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((prompt_attn_bf16_kernel<64>), grid, block, 0, stream, a);
-    if (a.chunks > 1) {
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      const dim3 rows((unsigned)(((int64_t)a.total_tokens * a.num_q_heads + kWaves - 1) / kWaves));
-      if (head_dim == 128) hipLaunchKernelGGL((prompt_join_kernel<128>), rows, block, 0, stream, a);
-      else hipLaunchKernelGGL((prompt_join_kernel<64>), rows, block, 0, stream, a);
-    }
-    return hipGetLastError();
-  }
-  if (head_dim == 128) {
-    if (a.f32_rows == 32) launch_prompt_f32<128, 2>(a, a.units, stream);
-    else launch_prompt_f32<128, 1>(a, a.units, stream);
-  } else {
-    if (a.f32_rows == 32) launch_prompt_f32<64, 2>(a, a.units, stream);
-    else launch_prompt_f32<64, 1>(a, a.units, stream);
-  }
-  return hipGetLastError();
+  if (a.window) return head_dim == 128 ? launch<128, true>(a, bf16, stream) : launch<64, true>(a, bf16, stream);
+  return head_dim == 128 ? launch<128, false>(a, bf16, stream) : launch<64, false>(a, bf16, stream);
 }
 
 }  // namespace adaserve

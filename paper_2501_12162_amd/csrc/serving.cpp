@@ -123,8 +123,9 @@ struct PromptPlan {
 // and by the join's traffic: tiles write and the join reads D + 2 floats per row.
 // (64 rows over 8064 keys, 64 heads on 8: 167 us whole, 37 split; one row 157 and
 // 27; 2000 rows of a prompt, 504 tiles, stay whole: 69.)
+// Over a window a tile's keys are those of its rows' windows.
 PromptPlan prompt_plan(int32_t num_requests, const int32_t *indptr, const int32_t *ctx, int32_t hq, int32_t hkv,
-                       int32_t head_dim, bool bf16) {
+                       int32_t head_dim, int32_t window, int32_t sinks, bool bf16) {
   constexpr double kTileUs = 9.0, kJoinUs = 6.0, kJoinBytesPerUs = 4e6;
   constexpr int32_t kLeastKeys = 256, kMostChunks = 64;
   const double key_us = 0.022 * head_dim / 128;
@@ -139,7 +140,8 @@ PromptPlan prompt_plan(int32_t num_requests, const int32_t *indptr, const int32_
     most = std::max<int64_t>(most, ctx[r] - n);
     keys = std::max(keys, ctx[r]);
   }
-  p.in_order = most - least <= 128;
+  if (window) keys = window_keys(keys, window, sinks, kPromptTileRows / (hq / hkv) + 1);
+  p.in_order = most - least <= 128 || (window && least >= window);
   if (!bf16 || num_requests > kPromptTable || p.units == 0 || p.units >= 2 * kPromptGrid) return p;
   const double row_bytes = 2.0 * (head_dim * 4 + 8) * indptr[num_requests] * hq;
   double best = 0.95 * std::ceil((double)p.units / kPromptGrid) * (kTileUs + keys * key_us);
@@ -239,8 +241,6 @@ int32_t validate_sample(int32_t num_rows, int32_t vocab, int32_t dtype) {
   return st != ADASERVE_OK ? st : validate_launch("sampling", num_rows, kSampleDrawThreads);
 }
 
-int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 // Prompt attention; over a window where there is one.
 int32_t prompt_attn_impl(int32_t num_requests, const int32_t *token_indptr, const int32_t *token_indptr_host,
                          const void *q, int64_t q_row_stride, const void *k_pages, const void *v_pages,
@@ -264,10 +264,8 @@ int32_t prompt_attn_impl(int32_t num_requests, const int32_t *token_indptr, cons
   if (!aligned(out, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "out must be 16-byte aligned");
   st = validate_pages(most > 0, k_pages, v_pages, num_pages, block_table);
   if (st != ADASERVE_OK) return st;
-  PromptPlan plan;
-  if (!window)
-    plan = prompt_plan(num_requests, token_indptr_host, context_len_host, num_q_heads, num_kv_heads, head_dim,
-                       dtype == ADASERVE_BF16);
+  const PromptPlan plan = prompt_plan(num_requests, token_indptr_host, context_len_host, num_q_heads, num_kv_heads,
+                                      head_dim, window, sinks, dtype == ADASERVE_BF16);
   st = validate_workspace(workspace, workspace_bytes, plan.ws_bytes);
   if (st != ADASERVE_OK) return st;
   PromptAttnArgs a{};
@@ -290,14 +288,6 @@ int32_t prompt_attn_impl(int32_t num_requests, const int32_t *token_indptr, cons
   a.scale_log2 = sm_scale * 1.4426950408889634f;
   a.window = window;
   a.sinks = sinks;
-  if (window) {
-    st = validate_launch("window attention", ceil_div64(total * num_q_heads, 4), kServingThreads);
-    if (st != ADASERVE_OK) return st;
-    st = check_device();
-    if (st != ADASERVE_OK) return st;
-    return launch_status(launch_window_rows(a, head_dim, dtype == ADASERVE_BF16, false, (hipStream_t)stream),
-                         "window attention launch");
-  }
   if (dtype == ADASERVE_BF16) {
     fill_prompt(a, plan, token_indptr_host, context_len_host, kPromptTileRows, workspace);
   } else {
@@ -342,8 +332,8 @@ int32_t decode_attn_impl(int32_t num_requests, const void *q, int64_t q_row_stri
   if (!aligned(out, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "out must be 16-byte aligned");
   st = validate_pages(max_context > 0, k_pages, v_pages, num_pages, block_table);
   if (st != ADASERVE_OK) return st;
-  DecodePlan plan{};
-  if (!window) plan = decode_plan(num_requests, num_q_heads, num_kv_heads, head_dim, max_context);
+  const DecodePlan plan = decode_plan(num_requests, num_q_heads, num_kv_heads, head_dim,
+                                      window ? window_keys(max_context, window, sinks, 1) : max_context);
   st = validate_workspace(workspace, workspace_bytes, plan.ws_bytes);
   if (st != ADASERVE_OK) return st;
   st = check_device();
@@ -375,9 +365,6 @@ int32_t decode_attn_impl(int32_t num_requests, const void *q, int64_t q_row_stri
   a.scale_log2 = sm_scale * 1.4426950408889634f;
   a.window = window;
   a.sinks = sinks;
-  if (window)
-    return launch_status(launch_window_rows(a, head_dim, dtype == ADASERVE_BF16, true, (hipStream_t)stream),
-                         "window attention launch");
   return launch_status(launch_decode_attn(a, head_dim, dtype == ADASERVE_BF16, (hipStream_t)stream),
                        "decode attention launch");
 }
@@ -502,7 +489,7 @@ size_t adaserve_prompt_attn_workspace_bytes(int32_t num_requests, const int32_t 
   if (validate_paged(num_requests, 0, 0, num_q_heads, num_kv_heads, head_dim, page_size, 1.f, dtype) != ADASERVE_OK ||
       validate_prompt(num_requests, token_indptr_host, context_len_host, -1, num_q_heads, total, most) != ADASERVE_OK)
     return SIZE_MAX;
-  return prompt_plan(num_requests, token_indptr_host, context_len_host, num_q_heads, num_kv_heads, head_dim,
+  return prompt_plan(num_requests, token_indptr_host, context_len_host, num_q_heads, num_kv_heads, head_dim, 0, 0,
                      dtype == ADASERVE_BF16)
       .ws_bytes;
 }
@@ -527,9 +514,10 @@ size_t adaserve_window_prompt_attn_workspace_bytes(int32_t num_requests, const i
       validate_paged(num_requests, 0, 0, num_q_heads, num_kv_heads, head_dim, page_size, 1.f, dtype) != ADASERVE_OK ||
       validate_prompt(num_requests, token_indptr_host, context_len_host, -1, num_q_heads, total, most) != ADASERVE_OK)
     return SIZE_MAX;
-  if (!sees_all(window, sinks, most)) return 0;
-  return adaserve_prompt_attn_workspace_bytes(num_requests, token_indptr_host, context_len_host, num_q_heads,
-                                              num_kv_heads, head_dim, page_size, dtype);
+  if (sees_all(window, sinks, most)) window = sinks = 0;
+  return prompt_plan(num_requests, token_indptr_host, context_len_host, num_q_heads, num_kv_heads, head_dim, window, sinks,
+                     dtype == ADASERVE_BF16)
+      .ws_bytes;
 }
 
 int32_t adaserve_window_prompt_attn(int32_t num_requests, const int32_t *token_indptr,
@@ -573,9 +561,8 @@ size_t adaserve_window_decode_attn_workspace_bytes(int32_t num_requests, int32_t
       validate_paged(num_requests, 0, 0, num_q_heads, num_kv_heads, head_dim, page_size, 1.f, dtype) != ADASERVE_OK ||
       validate_decode(num_requests, num_q_heads, num_kv_heads, max_context, -1) != ADASERVE_OK)
     return SIZE_MAX;
-  if (!sees_all(window, sinks, max_context)) return 0;
-  return adaserve_decode_attn_workspace_bytes(num_requests, max_context, num_q_heads, num_kv_heads, head_dim, page_size,
-                                              dtype);
+  const int32_t keys = sees_all(window, sinks, max_context) ? max_context : window_keys(max_context, window, sinks, 1);
+  return decode_plan(num_requests, num_q_heads, num_kv_heads, head_dim, keys).ws_bytes;
 }
 
 int32_t adaserve_window_decode_attn(int32_t num_requests, const void *q, int64_t q_row_stride, const void *k_pages,

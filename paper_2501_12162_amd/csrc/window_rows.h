@@ -110,4 +110,15 @@ __device__ __forceinline__ void attend_keys(const void *q, int64_t count, At at,
   }
 }
 
+// out[t, h] = attention of q[t, h], at position `pos` of request r, over a window and sinks.
+template <bool BF16, int D>
+__device__ __forceinline__ void attend_seen(const PagedAttnArgs &a, int32_t r, int64_t t, int32_t h, int64_t pos,
+                                            RowScratch<D> &scratch) {
+  constexpr int ESZ = BF16 ? 2 : 4;
+  const SeenKeys seen = seen_keys(pos, a.window, a.sinks);
+  attend_keys<BF16, D>((const char *)a.q + (t * a.q_stride + (int64_t)h * D) * ESZ, seen.count,
+                       [&](int64_t i) { return paged_key(a, r, h / a.group, seen.place(i), D * ESZ); }, a.sm_scale,
+                       (char *)a.out + (t * a.num_q_heads + h) * D * ESZ, scratch);
+}
+
 }  // namespace adaserve
