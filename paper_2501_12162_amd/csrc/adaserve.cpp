@@ -106,6 +106,18 @@ int32_t validate_step(const StepArgs &st, int32_t num_requests, int32_t total_no
   return ADASERVE_OK;
 }
 
+std::vector<int32_t> window_prefixes(int32_t num_requests, const int32_t *prefix_len_host, int32_t window, int32_t sinks) {
+  std::vector<int32_t> keys(num_requests);
+  for (int32_t r = 0; r < num_requests; ++r) keys[r] = window_prefix(prefix_len_host[r], window, sinks);
+  return keys;
+}
+
+// Partial outputs in fp32 instead of bf16.
+void grow_partials(AttnPlan &plan) {
+  plan.ws_bytes += plan.ws_o_bytes;
+  plan.ws_o_bytes *= 2;
+}
+
 // Positions of the longest request: its prefix, and its nodes in a chain.
 int64_t most_positions(int32_t num_requests, const int32_t *node_indptr_host, const int32_t *prefix_len_host) {
   int64_t most = 0;
@@ -155,12 +167,17 @@ int32_t tree_attn_verify_impl(int32_t num_requests, const int32_t *node_indptr, 
   const void *tensors[] = {q, k_tree, v_tree, out, k_pages, v_pages};
   for (const void *t : tensors)
     if (t && !aligned(t, 16)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "tensor pointers must be 16-byte aligned");
-  AttnPlan plan;
-  if (!window)
-    plan = make_plan_cached(num_requests, node_indptr_host, prefix_len_host, num_kv_heads, shape.group, head_dim, dtype);
+  std::vector<int32_t> keys;   // over a window: of each prefix, what is read
+  if (window) {
+    keys = window_prefixes(num_requests, prefix_len_host, window, sinks);
+    prefix_len_host = keys.data();
+  }
+  AttnPlan plan =
+      make_plan_cached(num_requests, node_indptr_host, prefix_len_host, num_kv_heads, shape.group, head_dim, dtype);
   if (use_scratch && plan.ws_bytes > (size_t)ADASERVE_TREE_ATTN_SCRATCH_BYTES)
     plan = make_plan_cached(num_requests, node_indptr_host, prefix_len_host, num_kv_heads, shape.group, head_dim, dtype,
                             true);
+  if (window) grow_partials(plan);
   if (use_scratch) {
     if (plan.ws_bytes > (size_t)ADASERVE_TREE_ATTN_SCRATCH_BYTES)
       return fail(ADASERVE_ERR_WORKSPACE,
@@ -209,7 +226,7 @@ int32_t tree_attn_verify_impl(int32_t num_requests, const int32_t *node_indptr, 
   a.merge_blocks = plan.row_groups * (kMaxRowsPerTile / 16);
   a.stream_kv = plan.single_tile ? 1 : 0;
   PlanTable t;
-  if (!window) fill_plan_table(t, num_requests, node_indptr_host, prefix_len_host, num_kv_heads, shape.group, plan);
+  fill_plan_table(t, num_requests, node_indptr_host, prefix_len_host, num_kv_heads, shape.group, plan);
   a.plan_count = t.count;
   if (t.count > 0) {
     std::copy(t.entry, t.entry + t.count, a.plan);
@@ -220,8 +237,6 @@ int32_t tree_attn_verify_impl(int32_t num_requests, const int32_t *node_indptr, 
   a.window = window;
   a.sinks = sinks;
   hipStream_t s = (hipStream_t)stream;
-  if (window)
-    return launch_status(launch_window_tree_rows(a, head_dim, dtype == ADASERVE_BF16, s), "window attention launch");
   if (step) {
     a.logits = step->logits;
     a.logit_stride = step->row_stride;
@@ -283,9 +298,13 @@ size_t adaserve_window_tree_attn_workspace_bytes(int32_t num_requests, const int
       validate_attn_shape(num_requests, node_indptr_host, prefix_len_host, num_q_heads, num_kv_heads, head_dim,
                           page_size, dtype, -1, shape) != ADASERVE_OK)
     return SIZE_MAX;
-  if (!sees_all(window, sinks, most_positions(num_requests, node_indptr_host, prefix_len_host))) return 0;
-  return adaserve_tree_attn_workspace_bytes(num_requests, node_indptr_host, prefix_len_host, num_q_heads, num_kv_heads,
-                                            head_dim, page_size, dtype);
+  if (num_requests > 0 && sees_all(window, sinks, most_positions(num_requests, node_indptr_host, prefix_len_host)))
+    window = sinks = 0;
+  const std::vector<int32_t> keys = window_prefixes(num_requests, prefix_len_host, window, sinks);
+  AttnPlan plan =
+      make_plan_cached(num_requests, node_indptr_host, keys.data(), num_kv_heads, shape.group, head_dim, dtype);
+  if (window) grow_partials(plan);
+  return plan.ws_bytes;
 }
 
 int32_t adaserve_window_tree_attn(int32_t num_requests, const int32_t *node_indptr, const int32_t *node_indptr_host,

@@ -22,7 +22,7 @@ struct TreeAttnArgs {
   const void *v_pages;
   const void *zero16;          // 16 zero bytes in device memory (source of masked DMA lanes)
   void *out;                   // [T, Hq, D]
-  __bf16 *ws_o;                // [units, kMaxRowsPerTile, D] partial outputs (each chunk normalised)
+  __bf16 *ws_o;                // [units, kMaxRowsPerTile, D] partial outputs (each chunk normalised; over a window fp32)
   float *ws_ml;                // [units, kMaxRowsPerTile, 2]  (reference max in raw units, denominator)
   int32_t num_requests;
   int32_t total_nodes;
@@ -57,9 +57,6 @@ struct TreeAttnArgs {
   int32_t plan_count;          // entries used in plan[] (0: scan the device arrays)
   PlanEntry plan[kPlanMax];
 };
-
-// Attention over a window and sinks, row by row (window_attn.hip).
-hipError_t launch_window_tree_rows(const TreeAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
 
 hipError_t launch_tree_attn_bf16(TreeAttnArgs &a, int head_dim, bool needs_combine, hipStream_t stream);
 // The verification step: attention + argmax workgroups (many short F32 rows

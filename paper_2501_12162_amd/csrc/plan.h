@@ -90,6 +90,11 @@ ADASERVE_HD WindowSpan window_span(int32_t first, int32_t sinks, int32_t block) 
   return {s < lo ? s : lo, s < lo ? lo - s : 0};
 }
 
+// Keys of a prefix of L that the nodes of a tree behind it read, numbered through.
+ADASERVE_HD int32_t window_prefix(int32_t L, int32_t window, int32_t sinks) {
+  return window > 0 ? L - window_span(L - window + 1, sinks, kKeysPerBlock).shift * kKeysPerBlock : L;
+}
+
 // Most keys of a row tile of `tokens` neighbouring positions, numbered through,
 // that a call with keys of its own of at most `context` reads.
 ADASERVE_HD int32_t window_keys(int32_t context, int32_t window, int32_t sinks, int32_t tokens) {

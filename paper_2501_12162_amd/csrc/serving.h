@@ -141,9 +141,6 @@ inline DecodePlan decode_plan(int32_t B, int32_t hq, int32_t hkv, int32_t head_d
 
 hipError_t launch_prompt_attn(const PromptAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
 hipError_t launch_decode_attn(const PagedAttnArgs &a, int head_dim, bool bf16, hipStream_t stream);
-// Attention over a window and sinks, row by row (window_attn.hip): of prompts,
-// or of one token per request.
-hipError_t launch_window_rows(const PagedAttnArgs &a, int head_dim, bool bf16, bool decode, hipStream_t stream);
 
 constexpr int kSampleMaxVocab = 1 << 20;   // sums of 2^32 per token stay below 2^53
 

@@ -96,7 +96,7 @@ __device__ bool locate_request(int64_t idx, bool count_groups, const TreeAttnArg
     if (r < a.num_requests) {
       int32_t n = a.node_indptr[r + 1] - a.node_indptr[r];
       n = min(max(n, 0), kMaxTreeNodes);
-      const int32_t L = max(a.prefix_len[r], 0);
+      const int32_t L = window_prefix(max(a.prefix_len[r], 0), a.window, a.sinks);
       ng = (int64_t)a.num_kv_heads * row_tiles(n, a.group, a.rows_per_tile);
       nu = ng * prefix_chunks(L, chunk_keys(n, a.group, a.rows_per_tile, a.chunk_target, a.chunk_floor));
     }
@@ -119,8 +119,8 @@ __device__ bool locate_request(int64_t idx, bool count_groups, const TreeAttnArg
   return false;
 }
 
-// The work unit with logical id `uid`: its request, that request's sizes, the
-// prefix keys per unit (F32: of no meaning, always the whole prefix) and the
+// The work unit with logical id `uid`: its request, that request's sizes (over a
+// window L counts the prefix keys that are read, window_prefix()), the prefix keys per unit (F32: of no meaning, always the whole prefix) and the
 // request's first unit id.  From the plan table in the kernel arguments, or,
 // without one, by the scan.  Every field is uniform; false when there is no
 // such unit or its request does not fit the batch.
@@ -146,7 +146,7 @@ __device__ __forceinline__ bool find_unit(const TreeAttnArgs &a, int64_t uid, Un
     if (!locate_request(uid, false, a, r, ubase, gbase)) return false;
     node_base = a.node_indptr[r];
     n = min(max(a.node_indptr[r + 1] - node_base, 0), kMaxTreeNodes);
-    L = max(a.prefix_len[r], 0);
+    L = window_prefix(max(a.prefix_len[r], 0), a.window, a.sinks);
     chunk_len = chunk_keys(n, a.group, a.rows_per_tile, a.chunk_target, a.chunk_floor);
   }
   // Request values are uniform; make that visible so branches on them stay scalar.
@@ -164,21 +164,40 @@ __device__ __forceinline__ uint32_t set_bit_in(uint32_t w, int word, int v) {
   return ((v >> 5) == word) ? (w | (1u << (v & 31))) : w;
 }
 
+// Steps from node i to where its path ends.
+__device__ __forceinline__ int node_depth(const int32_t *par, int i) {
+  int d = 0;
+  for (int v = i; d < kMaxTreeNodes - 1 && v != 0; ++d) {
+    const int p = par[v];
+    if (p < 0 || p >= v) break;
+    v = p;
+  }
+  return d;
+}
+
 // Ancestor sets of a request's n nodes from its parents in LDS: bit j of
 // node i's 128-bit set is 1 when j is on i's root-to-node path, i included.
 // The walk stops at anything that is not a parent strictly before its child,
 // so malformed trees stay in bounds.  Called by all of the workgroup's
 // `threads` threads.
-__device__ __forceinline__ void build_ancestors(const int32_t *par, uint32_t *anc, int n, int threads) {
+// Over a window, behind a prefix of L: of the path, the nodes that node i's
+// position sees; and depth[i].
+template <bool WINDOW>
+__device__ __forceinline__ void build_ancestors(const int32_t *par, uint32_t *anc, int n, int threads, const TreeAttnArgs &a,
+                                                int32_t L, int32_t *depth) {
   for (int i = threadIdx.x; i < kMaxTreeNodes; i += threads) {
     uint32_t w0 = 0, w1 = 0, w2 = 0, w3 = 0;
     if (i < n) {
+      int d = 0;
+      if constexpr (WINDOW) depth[i] = d = node_depth(par, i);
       int v = i;
       for (int step = 0; step < kMaxTreeNodes; ++step) {
-        w0 = set_bit_in(w0, 0, v);
-        w1 = set_bit_in(w1, 1, v);
-        w2 = set_bit_in(w2, 2, v);
-        w3 = set_bit_in(w3, 3, v);
+        if (!WINDOW || step < a.window || L + d - step < a.sinks) {
+          w0 = set_bit_in(w0, 0, v);
+          w1 = set_bit_in(w1, 1, v);
+          w2 = set_bit_in(w2, 2, v);
+          w3 = set_bit_in(w3, 3, v);
+        }
         if (v == 0) break;
         const int p = par[v];
         if (p < 0 || p >= v) break;
@@ -192,7 +211,7 @@ __device__ __forceinline__ void build_ancestors(const int32_t *par, uint32_t *an
   }
 }
 
-template <int D, bool NT>
+template <int D, bool NT, bool WINDOW>
 __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArgs a) {
   constexpr int KS = D / 16;                 // MFMA k-steps over the head dim
   constexpr int DT = D / 32;                 // 32-wide output tiles over the head dim
@@ -217,7 +236,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
   __shared__ __align__(1024) char ring[NST * 2 * BLK];
   int32_t *const par = (int32_t *)(ring + (NST - 1) * 2 * BLK + BLK);
   uint32_t *const anc = (uint32_t *)(ring + (NST - 1) * 2 * BLK + BLK + kMaxTreeNodes * 4);
-  static_assert(kMaxTreeNodes * 4 * 5 <= BLK, "parents and ancestor sets fit in a V half-stage");
+  int32_t *const depth = (int32_t *)(anc + kMaxTreeNodes * 4);
+  static_assert(kMaxTreeNodes * 4 * 6 <= BLK, "parents, ancestor sets and depths fit in a V half-stage");
 
   if ((int64_t)blockIdx.x >= a.padded_grid) {
     // fused verification step: argmax workgroups follow the attention units,
@@ -258,6 +278,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
   const int32_t nb = n_prefix_blocks + n_tree_blocks;
   const int32_t page0 = k0 / kPageSize;
   const int32_t npages = k1 > k0 ? ceil_div(k1, kPageSize) - page0 : 0;
+  // Over a window: where the prefix's keys stand in the cache; the first one that the
+  // root's window holds (a node's begins as much later as it is deep); the chunk's
+  // blocks before those that all nodes see.
+  const int32_t prefix = WINDOW ? __builtin_amdgcn_readfirstlane(max(a.prefix_len[r], 0)) : L;
+  const WindowSpan span = WINDOW ? window_span(prefix - a.window + 1, a.sinks, KB) : WindowSpan{0, 0};
+  const int32_t lo = WINDOW ? prefix - a.window + 1 - span.shift * KB : 0;
+  const int32_t n_edge = WINDOW ? min(max(0, ceil_div(max(0, lo + n - 1 - k0), KB)), n_prefix_blocks) : 0;
+  const bool need_tree = WINDOW || last_chunk;
 
   // ---- start-up: page ids, parents and queries, all loads in flight together.
   // The DMA rows of a wave lie in one 16-key page of each 32-key block (page
@@ -269,7 +297,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int32_t blk = i * 64 + lane;
-    const int32_t e = page0 + blk * (KB / kPageSize) + wave_page;
+    int32_t e = page0 + blk * (KB / kPageSize) + wave_page;
+    if constexpr (WINDOW) e = span.real(k0 / KB + blk) * (KB / kPageSize) + wave_page;
     int32_t p = -1;
     if (blk < n_prefix_blocks && e < a.bt_stride) {
       p = a.block_table[(int64_t)r * a.bt_stride + e];
@@ -278,7 +307,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
     pgv[i] = p;
   }
   (void)npages;
-  if (last_chunk)
+  if (need_tree)
     for (int i = tid; i < n; i += kThreads) par[i] = a.parent[node_base + i];
 
   // Query fragments (B operand of S^T = K Q^T): lane holds row (lane & 31) of
@@ -343,6 +372,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
     const char *base;
     int rows_left;
     const bool pre = blk < n_prefix_blocks;
+    const int key0 = k0 + blk * KB;
+    const bool cut = WINDOW && pre && key0 < lo;   // keys that no node sees
     if (blk >= nb) {
       rows_left = 0;
       base = (const char *)tree;
@@ -356,13 +387,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
       base = (const char *)tree + tree_off_b + (int64_t)tb * KB * tree_stride * 2;
     }
     const uint32_t lds = lds_addr(dst) + wave * WI * 1024;
-    if (rows_left >= KB) {
+    if (rows_left >= KB && !cut) {
 #pragma unroll
       for (int i = 0; i < WI; ++i) dma16_off<NT>(base, pre ? page_off[i] : tree_off[i], lds + i * 1024);
     } else {
 #pragma unroll
       for (int i = 0; i < WI; ++i) {
-        const bool ok = dma_row[i] < rows_left;
+        bool ok = dma_row[i] < rows_left;
+        if constexpr (WINDOW) ok = ok && (!cut || key0 + dma_row[i] >= lo || key0 + dma_row[i] < a.sinks);
         dma16<NT>(ok ? (const void *)(base + (pre ? page_off[i] : tree_off[i])) : a.zero16, lds + i * 1024);
       }
     }
@@ -392,15 +424,17 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
   }
 
   // Ancestor sets, while the first blocks are in flight.
-  if (last_chunk) build_ancestors(par, anc, n, kThreads);
+  if (need_tree) build_ancestors<WINDOW>(par, anc, n, kThreads, a, prefix, depth);
 
   // Per-lane LDS offsets of the MFMA operand fragments inside a stage.
   const int half = lane >> 5;
 
   // The ancestor set of this lane's row's node, in registers.
   uint32_t an0 = 0, an1 = 0, an2 = 0, an3 = 0;
-  if (last_chunk) {
+  int32_t row_lo = 0;   // over a window: the row's first key there
+  if (need_tree) {
     __syncthreads();  // anc[] complete
+    if constexpr (WINDOW) row_lo = lo + depth[row_node];
     an0 = anc[row_node * 4 + 0], an1 = anc[row_node * 4 + 1], an2 = anc[row_node * 4 + 2], an3 = anc[row_node * 4 + 3];
   }
   int koff[KS];  // K fragment: key row lane & 31, chunk ks*2 + half
@@ -451,6 +485,11 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
       aw = (tb & 2) ? ((tb & 1) ? w3 : w2) : ((tb & 1) ? w1 : w0);
     }
     if (valid < KB) aw &= (1u << valid) - 1u;
+    if constexpr (WINDOW) {
+      const int32_t from = a.sinks - k0 - blk * KB, to = row_lo - k0 - blk * KB;   // not seen
+      const auto below = [](int32_t x) -> uint32_t { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1u; };
+      if (!tree_blk) aw &= ~below(to) | below(from);
+    }
     aw >>= half * 4;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = ((aw >> ((i >> 2) * 8 + (i & 3))) & 1u) ? s[i] : -INFINITY;
@@ -519,7 +558,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
     wait_loads_barrier<8 * WI>();
     if (wave_live) {
       scores(ring + 4 * 2 * BLK, s);
-      if (n_full == 0) mask(s, 0);
+      if (n_full == 0 || n_edge > 0) mask(s, 0);
       bm = rowmax(s);
     }
   }
@@ -587,7 +626,11 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
   // Blocks j+4 and j+5 whole prefix blocks: five steps per iteration (one
   // per ring stage, starting at stage 0), so every LDS address of a step is
   // a constant and folds into the instruction's offset.
-  for (; j + 9 < n_full; j += 5) {
+  if constexpr (WINDOW) {
+    for (; j + 1 < n_edge; ++j, cs = next_stage(cs)) step(j, cs, Yes{}, Yes{}, No{});
+    for (; cs != 0 && j + 5 < n_full; ++j, cs = next_stage(cs)) step(j, cs, No{}, Yes{}, Yes{});
+  }
+  for (; (!WINDOW || cs == 0) && j + 9 < n_full; j += 5) {
     step(j, 0, No{}, Yes{}, Yes{});
     step(j + 1, 1, No{}, Yes{}, Yes{});
     step(j + 2, 2, No{}, Yes{}, Yes{});
@@ -606,7 +649,22 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
   // split, as this chunk's partial (a weighted mean of V rows, so bf16 keeps
   // 2^-9 relative precision) with its reference max and denominator in fp32;
   // tree_attn_combine_kernel merges the chunks after this kernel.
+  // Over a window, whose calls are short and their partials few, they are fp32:
+  // no rounding but those of P and the output (16 trees over windows of 2048, error
+  // against fp64 0.0029 -> 0.0021).
   const int64_t pslot = uid * kMaxRowsPerTile + (row - row0);
+  if (WINDOW && chunks > 1) {
+    if (row_valid) {
+      float *part = (float *)a.ws_o + pslot * D + half * 4;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *(f32x4 *)(part + dt * 32 + i * 2) = f32x4{o[dt][i] * inv, o[dt][i + 1] * inv, o[dt][i + 2] * inv, o[dt][i + 3] * inv};
+      if (half == 0) *(f32x2 *)(a.ws_ml + pslot * 2) = f32x2{m_ref, l_tot};
+    }
+    return;
+  }
   __bf16 *dst = chunks == 1 ? (__bf16 *)a.out + ((int64_t)(node_base + row_node) * a.num_q_heads + row_head) * D
                             : a.ws_o + pslot * D;
 #pragma unroll
@@ -634,7 +692,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
 // blocks); without one, workgroup b takes rows (b % 8) * 16 .. +15 of
 // (kv-head, row tile) group b / 8 in the scan order, and the workgroups of
 // unsplit requests or past a tile's rows return at once.
-template <int D>
+template <int D, bool WINDOW>
 __global__ __launch_bounds__(kThreads) void tree_attn_combine_kernel(TreeAttnArgs a) {
   constexpr int kRowsPerWg = 16;
   constexpr int TPR = kThreads / kRowsPerWg;  // threads per row
@@ -679,7 +737,7 @@ __global__ __launch_bounds__(kThreads) void tree_attn_combine_kernel(TreeAttnArg
     if (!locate_request(gid, true, a, r, ubase, gbase)) return;
     node_base = a.node_indptr[r];
     n = min(max(a.node_indptr[r + 1] - node_base, 0), kMaxTreeNodes);
-    L = max(a.prefix_len[r], 0);
+    L = window_prefix(max(a.prefix_len[r], 0), a.window, a.sinks);
     chunk_len = chunk_keys(n, G, RT, a.chunk_target, a.chunk_floor);
     if (n == 0) return;
     const int32_t tiles_r = row_tiles(n, G, RT);
@@ -704,20 +762,26 @@ __global__ __launch_bounds__(kThreads) void tree_attn_combine_kernel(TreeAttnArg
   for (int cc = 0; cc < chunks; ++cc) {
     const int64_t slot = (ubase + ((int64_t)cc * a.num_kv_heads + g) * tiles + tile) * kMaxRowsPerTile + rl;
     const f32x2 ml = *(const f32x2 *)(a.ws_ml + slot * 2);
-    u32x4 raw = {0u, 0u, 0u, 0u};  // CPT bf16 values
-    if (CPT == 8) raw = *(const u32x4 *)(a.ws_o + slot * D + col);
-    else { const u32x2 h = *(const u32x2 *)(a.ws_o + slot * D + col); raw[0] = h[0]; raw[1] = h[1]; }
+    f32x4 part[CPT / 4];
+    if constexpr (WINDOW) {
+#pragma unroll
+      for (int k = 0; k < CPT / 4; ++k) part[k] = *(const f32x4 *)((const float *)a.ws_o + slot * D + col + 4 * k);
+    } else {
+      u32x4 raw = {0u, 0u, 0u, 0u};  // CPT bf16 values
+      if (CPT == 8) raw = *(const u32x4 *)(a.ws_o + slot * D + col);
+      else { const u32x2 h = *(const u32x2 *)(a.ws_o + slot * D + col); raw[0] = h[0]; raw[1] = h[1]; }
+#pragma unroll
+      for (int k = 0; k < CPT / 4; ++k)
+        part[k] = f32x4{bf16_bits_to_float(raw[2 * k] & 0xffffu), bf16_bits_to_float(raw[2 * k] >> 16),
+                        bf16_bits_to_float(raw[2 * k + 1] & 0xffffu), bf16_bits_to_float(raw[2 * k + 1] >> 16)};
+    }
     const float m_new = fmaxf(mm, ml[0]);
     const float sa = __builtin_amdgcn_exp2f((mm - m_new) * c);
     const float wb = ml[1] * __builtin_amdgcn_exp2f((ml[0] - m_new) * c);
     mm = m_new;
     ll = ll * sa + wb;
 #pragma unroll
-    for (int k = 0; k < CPT / 4; ++k) {
-      const f32x4 v = {bf16_bits_to_float(raw[2 * k] & 0xffffu), bf16_bits_to_float(raw[2 * k] >> 16),
-                       bf16_bits_to_float(raw[2 * k + 1] & 0xffffu), bf16_bits_to_float(raw[2 * k + 1] >> 16)};
-      acc[k] = acc[k] * sa + v * wb;
-    }
+    for (int k = 0; k < CPT / 4; ++k) acc[k] = acc[k] * sa + part[k] * wb;
   }
   const float inv = ll > 0.f ? 1.f / ll : 0.f;
   const int row = tile * RT + rl;
@@ -754,7 +818,7 @@ __global__ __launch_bounds__(kThreads) void tree_attn_combine_kernel(TreeAttnArg
 // whole prefix once for each and took 266.  One request of 16 nodes over 256
 // keys (8 / 8 heads, D = 64): 14.8 -> 10 us.  A second set of K and V registers
 // (loads two blocks ahead) and 12 or 16 waves with one set measured no faster.
-template <int D, int RB>
+template <int D, int RB, bool WINDOW>
 __global__ __launch_bounds__(kWavesF32 * 64) void tree_attn_f32_kernel(TreeAttnArgs a) {
   constexpr int NW = kWavesF32, kT = NW * 64;
   constexpr int RT = 16 * RB;
@@ -795,7 +859,11 @@ __global__ __launch_bounds__(kWavesF32 * 64) void tree_attn_f32_kernel(TreeAttnA
 
   // The waves that have tree blocks fetch the parents (each into its part of
   // mo, which holds nothing else before the merge).
-  const bool has_tree = b1 > n_prefix_blocks && b1 > b0;
+  // (over a window every wave does, for the nodes' depths)
+  const bool has_tree = (WINDOW || b1 > n_prefix_blocks) && b1 > b0;
+  const int32_t prefix = WINDOW ? __builtin_amdgcn_readfirstlane(max(a.prefix_len[r], 0)) : L;
+  const WindowSpan span = WINDOW ? window_span(prefix - a.window + 1, a.sinks, kKeysPerBlock) : WindowSpan{0, 0};
+  const int32_t lo = WINDOW ? prefix - a.window + 1 - span.shift * kKeysPerBlock : 0;   // the root's first key there
   int32_t *const par = (int32_t *)(mo + wave * RT * LDO);
   if (has_tree)
     for (int i = lane; i < n; i += 64) par[i] = a.parent[node_base + i];
@@ -818,9 +886,14 @@ __global__ __launch_bounds__(kWavesF32 * 64) void tree_attn_f32_kernel(TreeAttnA
   int32_t page_base = b0, pages = -1;
   auto load_pages = [&]() {
     const int b = page_base + lane;
+    int e = b;
+    if constexpr (WINDOW) {
+      constexpr int kPages = kKeysPerBlock / kPageSize;
+      e = span.real(b / kPages) * kPages + b % kPages;
+    }
     pages = -1;
-    if (b < n_prefix_blocks && b < a.bt_stride) {
-      const int32_t p = a.block_table[(int64_t)r * a.bt_stride + b];
+    if (b < n_prefix_blocks && e < a.bt_stride) {
+      const int32_t p = a.block_table[(int64_t)r * a.bt_stride + e];
       if (p >= 0 && p < a.num_pages) pages = p;
     }
   };
@@ -890,17 +963,25 @@ __global__ __launch_bounds__(kWavesF32 * 64) void tree_attn_f32_kernel(TreeAttnA
   // The ancestor sets of the lane's rows' nodes, while the first block's loads
   // are in flight: bit i is 1 when node i is on the root-to-node path.  The
   // walk stops at anything that is not a parent strictly before its child.
+  // (over a window: and its position is seen from the node's)
   uint32_t an[RB][4];
+  int32_t row_lo[RB];   // over a window: the row's first key there
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) an[rb][0] = an[rb][1] = an[rb][2] = an[rb][3] = 0;
+  for (int rb = 0; rb < RB; ++rb) an[rb][0] = an[rb][1] = an[rb][2] = an[rb][3] = row_lo[rb] = 0;
   if (has_tree) {
     wave_lds_sync();
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      int v = min((row0 + rb * 16 + j) / G, n - 1);
+      int v = min((row0 + rb * 16 + j) / G, n - 1), d = 0;
+      if constexpr (WINDOW) {
+        d = node_depth(par, v);
+        row_lo[rb] = lo + d;
+      }
       for (int step = 0; step < kMaxTreeNodes; ++step) {
+        if (!WINDOW || step < a.window || prefix + d - step < a.sinks) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) an[rb][w] = set_bit_in(an[rb][w], w, v);
+          for (int w = 0; w < 4; ++w) an[rb][w] = set_bit_in(an[rb][w], w, v);
+        }
         if (v == 0) break;
         const int p = par[v];
         if (p < 0 || p >= v) break;
@@ -981,15 +1062,16 @@ __global__ __launch_bounds__(kWavesF32 * 64) void tree_attn_f32_kernel(TreeAttnA
       for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[rb][e] *= a.sm_scale;
-      const bool prefix = b < n_prefix_blocks;
+      const bool in_prefix = b < n_prefix_blocks;
       const int tb = b - n_prefix_blocks;
-      const int valid = prefix ? min(kPageSize, L - b * kPageSize) : min(16, n - tb * 16);
-      const bool zero_page = prefix && page < 0;
-      if (!prefix || valid < 16 || zero_page) {
+      const int valid = in_prefix ? min(kPageSize, L - b * kPageSize) : min(16, n - tb * 16);
+      const bool zero_page = in_prefix && page < 0;
+      const bool cut = WINDOW && in_prefix && b * 16 < lo + n - 1;   // keys that some node does not see
+      if (!in_prefix || valid < 16 || zero_page || cut) {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
           uint32_t seen = 0xffffu;
-          if (!prefix) {
+          if (!in_prefix) {
             const uint32_t w0 = an[rb][0], w1 = an[rb][1], w2 = an[rb][2], w3 = an[rb][3];
             const uint32_t w = (tb & 4) ? ((tb & 2) ? w3 : w2) : ((tb & 2) ? w1 : w0);
             seen = (tb & 1) ? w >> 16 : w;
@@ -998,14 +1080,16 @@ __global__ __launch_bounds__(kWavesF32 * 64) void tree_attn_f32_kernel(TreeAttnA
           for (int e = 0; e < 4; ++e) {
             const int key = q * 4 + e;
             const float x = zero_page ? 0.f : s[rb][e];
-            s[rb][e] = key < valid && ((seen >> key) & 1u) ? x : -INFINITY;
+            const bool far = cut && b * 16 + key < row_lo[rb] && b * 16 + key >= a.sinks;
+            s[rb][e] = key < valid && ((seen >> key) & 1u) && !far ? x : -INFINITY;
           }
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
           for (int h = 0; h < NH; ++h)
-            if (zero_page || q * 4 + e >= valid) vr[e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (zero_page || q * 4 + e >= valid || (cut && b * 16 + q * 4 + e < lo && b * 16 + q * 4 + e >= a.sinks))
+              vr[e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
       float mn[RB];
       bool up = false;
@@ -1164,40 +1248,45 @@ static hipError_t zero16_address(const void **out) {
 
 // The attention grid (and, in the one-call step, the argmax workgroups after
 // it) with the K/V load hint the plan chose.
-static void launch_attention(const TreeAttnArgs &a, int head_dim, int64_t blocks, hipStream_t stream) {
+template <int D, bool WINDOW>
+static void launch_bf16_tile(const TreeAttnArgs &a, int64_t blocks, hipStream_t stream) {
   const dim3 grid((unsigned)blocks), block(kThreads);
-  if (head_dim == 128) {
-    if (a.stream_kv)
-      hipLaunchKernelGGL((tree_attn_bf16_kernel<128, true>), grid, block, 0, stream, a);
-    else
-      hipLaunchKernelGGL((tree_attn_bf16_kernel<128, false>), grid, block, 0, stream, a);
-  } else {
-    if (a.stream_kv)
-      hipLaunchKernelGGL((tree_attn_bf16_kernel<64, true>), grid, block, 0, stream, a);
-    else
-      hipLaunchKernelGGL((tree_attn_bf16_kernel<64, false>), grid, block, 0, stream, a);
-  }
+  if (a.stream_kv) hipLaunchKernelGGL((tree_attn_bf16_kernel<D, true, WINDOW>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((tree_attn_bf16_kernel<D, false, WINDOW>), grid, block, 0, stream, a);
+}
+
+static void launch_attention(const TreeAttnArgs &a, int head_dim, int64_t blocks, hipStream_t stream) {
+  if (a.window) head_dim == 128 ? launch_bf16_tile<128, true>(a, blocks, stream) : launch_bf16_tile<64, true>(a, blocks, stream);
+  else head_dim == 128 ? launch_bf16_tile<128, false>(a, blocks, stream) : launch_bf16_tile<64, false>(a, blocks, stream);
+}
+
+template <int D>
+static void launch_combine_tile(const TreeAttnArgs &a, int64_t blocks, hipStream_t stream) {
+  const dim3 grid((unsigned)blocks), block(kThreads);
+  if (a.window) hipLaunchKernelGGL((tree_attn_combine_kernel<D, true>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((tree_attn_combine_kernel<D, false>), grid, block, 0, stream, a);
+}
+
+static void launch_combine(const TreeAttnArgs &a, int head_dim, int64_t blocks, hipStream_t stream) {
+  head_dim == 128 ? launch_combine_tile<128>(a, blocks, stream) : launch_combine_tile<64>(a, blocks, stream);
 }
 
 hipError_t launch_tree_attn_bf16(TreeAttnArgs &a, int head_dim, bool needs_combine, hipStream_t stream) {
   if (a.units == 0) return hipSuccess;
   hipError_t e = zero16_address(&a.zero16);
   if (e != hipSuccess) return e;
-  const dim3 block(kThreads);
   launch_attention(a, head_dim, a.padded_grid, stream);
   e = hipGetLastError();
   if (e != hipSuccess || !needs_combine) return e;
-  const dim3 cgrid((unsigned)a.merge_blocks);
-  if (head_dim == 128)
-    hipLaunchKernelGGL(tree_attn_combine_kernel<128>, cgrid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL(tree_attn_combine_kernel<64>, cgrid, block, 0, stream, a);
+  launch_combine(a, head_dim, a.merge_blocks, stream);
   return hipGetLastError();
 }
 
 template <int D, int RB>
 static void launch_f32_tile(const TreeAttnArgs &a, int64_t blocks, hipStream_t stream) {
-  hipLaunchKernelGGL((tree_attn_f32_kernel<D, RB>), dim3((unsigned)blocks), dim3(kWavesF32 * 64), 0, stream, a);
+  const dim3 grid((unsigned)blocks), block(kWavesF32 * 64);
+  if (a.window) hipLaunchKernelGGL((tree_attn_f32_kernel<D, RB, true>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((tree_attn_f32_kernel<D, RB, false>), grid, block, 0, stream, a);
 }
 
 hipError_t launch_tree_attn_f32(const TreeAttnArgs &a, int head_dim, int64_t blocks, hipStream_t stream) {
@@ -1223,7 +1312,6 @@ constexpr int kF32RowsBeside = 768, kF32LongRow = 32768;
 hipError_t launch_verify_step(TreeAttnArgs &a, int head_dim, bool bf16, bool needs_combine, hipStream_t stream) {
   hipError_t e = zero16_address(&a.zero16);
   if (e != hipSuccess) return e;
-  const dim3 block(kThreads);
   const bool apart = !bf16 && a.argmax_rows > kF32RowsBeside && a.vocab <= kF32LongRow;
   const int64_t g1 = (a.units > 0 ? a.padded_grid : 0) + (apart ? 0 : a.argmax_rows);
   if (a.units == 0) a.padded_grid = 0;
@@ -1243,10 +1331,7 @@ hipError_t launch_verify_step(TreeAttnArgs &a, int head_dim, bool bf16, bool nee
   if (!needs_combine) a.merge_blocks = 0;
   const int64_t g2 = a.merge_blocks + (a.accept_requests + kThreads / 64 - 1) / (kThreads / 64);
   if (g2 == 0) return hipSuccess;
-  if (head_dim == 128)
-    hipLaunchKernelGGL(tree_attn_combine_kernel<128>, dim3((unsigned)g2), block, 0, stream, a);
-  else
-    hipLaunchKernelGGL(tree_attn_combine_kernel<64>, dim3((unsigned)g2), block, 0, stream, a);
+  launch_combine(a, head_dim, g2, stream);
   return hipGetLastError();
 }
 
