@@ -683,7 +683,7 @@ int32_t adaserve_window_tree_attn(int32_t num_requests, const int32_t *node_indp
  * and are written whole.  workspace: at least adaserve_pages_workspace_bytes(the
  * larger of a call's row counts, num_pages) bytes, 256-byte aligned, no
  * initialisation needed; calls that share one must not overlap in time, nor may
- * calls on the same page_refs.  At most 65536 rows, 2^24 pages, page_size <= 2^16.
+ * calls on the same page_refs.  At most 65536 rows, 2^23 pages, page_size <= 2^16.
  */
 size_t adaserve_pages_workspace_bytes(int32_t num_rows, int32_t num_pages);
 

@@ -61,8 +61,8 @@ int32_t set_space(PagesArgs &a, int32_t rows, int32_t num_pages, void *workspace
   if (!aligned(workspace, 256)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "workspace must be 256-byte aligned");
   char *ws = (char *)workspace;
   a.ws_want = (int32_t *)ws;
-  a.ws_total = (int32_t *)(ws + s.total);
   a.ws_list = (int32_t *)(ws + s.list);
+  a.ws_bits = (unsigned long long *)(ws + s.list);
   a.ws_runs = (int32_t *)(ws + s.runs);
   return ADASERVE_OK;
 }

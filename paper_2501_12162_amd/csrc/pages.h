@@ -8,7 +8,7 @@ namespace adaserve {
 
 constexpr int kPagesThreads = 256;
 constexpr int kPagesMaxRows = 1 << 16;
-constexpr int kPagesMaxPages = 1 << 24;
+constexpr int kPagesMaxPages = 1 << 23;
 constexpr int kPagesRun = 1024;          // pages that a wave counts at a time
 
 struct PagesArgs {
@@ -31,10 +31,10 @@ struct PagesArgs {
   int32_t *new_place;            // [pages]
   int32_t *counts;               // [2]
   // workspace
-  int32_t *ws_want;              // [rows] pages wanted; then the sum of the rows before
-  int32_t *ws_total;             // [1] pages handed out
-  int32_t *ws_list;              // [pages] the pages handed out, or ranks of moves
-  int32_t *ws_runs;              // [runs] used pages per run
+  int32_t *ws_want;              // [rows] pages wanted
+  int32_t *ws_list;              // [pages] ranks of moves (compaction)
+  unsigned long long *ws_bits;   // [runs, kPagesRun / 64] free pages (in the same place)
+  int32_t *ws_runs;              // [runs] free pages, or pages in use, per run
 };
 
 struct CopyPagesArgs {
@@ -49,15 +49,15 @@ struct CopyPagesArgs {
 
 // Offsets of the workspace.
 struct PagesSpace {
-  size_t total, list, runs, bytes;
+  size_t list, runs, bytes;
 };
 inline PagesSpace pages_space(int32_t rows, int32_t pages) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   PagesSpace s;
-  s.total = up((size_t)rows * 4);
-  s.list = s.total + 256;
-  s.runs = s.list + up((size_t)pages * 4);
-  s.bytes = s.runs + up((size_t)((pages + kPagesRun - 1) / kPagesRun) * 4);
+  const size_t runs = ((size_t)pages + kPagesRun - 1) / kPagesRun;
+  s.list = up((size_t)rows * 4);
+  s.runs = s.list + up(runs * kPagesRun * 4);
+  s.bytes = s.runs + up(runs * 4);
   return s;
 }
 

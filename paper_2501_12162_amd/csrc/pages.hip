@@ -11,8 +11,7 @@ namespace adaserve {
 namespace {
 
 constexpr int kThreads = kPagesThreads;
-constexpr int kTakeThreads = 1024;
-constexpr int kTakeWaves = kTakeThreads / 64;
+constexpr int kRunWords = kPagesRun / 64;
 
 __device__ __forceinline__ bool in_pool(const PagesArgs &a, int32_t p) { return p >= 0 && p < a.pages; }
 
@@ -23,6 +22,17 @@ __device__ __forceinline__ int32_t group_sum(int32_t x, int32_t *parts) {
   if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = x;
   __syncthreads();
   return parts[0] + parts[1] + parts[2] + parts[3];
+}
+
+// Lane i's pages p0 + i, p0 + 64 + i, ... of a run; `none` past the last one.
+__device__ __forceinline__ void load_run(const int32_t *refs, int32_t pages, int64_t p0, int32_t none, int32_t (&x)[kRunWords]) {
+#pragma unroll
+  for (int i = 0; i < kRunWords; ++i) x[i] = refs[min(p0 + i * 64 + (threadIdx.x & 63), (int64_t)pages - 1)];
+#pragma unroll
+  for (int i = 0; i < kRunWords; ++i) {
+    asm volatile("" : "+v"(x[i]));   // (loaded by now: no load goes behind a ballot)
+    if (p0 + i * 64 + (threadIdx.x & 63) >= pages) x[i] = none;
+  }
 }
 
 __global__ __launch_bounds__(kThreads) void copy_refs_kernel(PagesArgs a) {
@@ -73,80 +83,106 @@ __global__ __launch_bounds__(kThreads) void update_drop_kernel(PagesArgs a) {
   if (threadIdx.x == 0) a.ws_want[r] = want;
 }
 
-// One workgroup: the sums of the rows' wants before each row, and the list of
-// as many free pages as all want, or as there are; then `after`.
-template <class After>
-__device__ __forceinline__ void take_pages(const PagesArgs &a, After after) {
-  __shared__ int64_t parts[2][kTakeWaves];
+// Which pages are free, a bit each, and how many per run of kPagesRun; a wave per
+// run.  (All of a lane's loads before the first ballot: a ballot per load takes one
+// round trip each, 8.7 us for 8000 pages.)
+__global__ __launch_bounds__(kThreads) void free_pages_kernel(PagesArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t run = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t p0 = run * kPagesRun;
+  if (p0 >= a.pages) return;
+  int32_t x[kRunWords];
+  load_run(a.new_refs, a.pages, p0, 1, x);
+  unsigned long long mine = 0;
+  int32_t n = 0;
+#pragma unroll
+  for (int i = 0; i < kRunWords; ++i) {
+    const unsigned long long word = __ballot(x[i] <= 0);
+    n += __popcll(word);
+    if (lane == i) mine = word;
+  }
+  if (lane < kRunWords) a.ws_bits[run * kRunWords + lane] = mine;
+  if (lane == 0) a.ws_runs[run] = n;
+}
+
+// The sums of the runs' free pages before each, in LDS; all of them.  For a
+// workgroup of 4 waves.
+__device__ __forceinline__ int32_t sum_runs(const PagesArgs &a, int32_t *before) {
+  __shared__ int64_t parts[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const unsigned long long below = (1ull << lane) - 1;
-  // exclusive sum over the workgroup, and the total (of 2^10 wants of up to 2^24)
-  auto scan = [&](int64_t x, int64_t *p, int64_t &total) {
-    int64_t upto = wave_inclusive_scan(x);
-    if (lane == 63) p[wave] = upto;
-    __syncthreads();
-    total = 0;
-    for (int w = 0; w < kTakeWaves; ++w) {
-      if (w < wave) upto += p[w];
-      total += p[w];
-    }
-    return upto - x;
-  };
-  int32_t want = 0;   // (wants beyond the pages that there are need not be told apart)
+  const int32_t runs = (a.pages + kPagesRun - 1) / kPagesRun;
+  int64_t sum = 0;
   int flip = 0;
-  for (int32_t r0 = 0; r0 < a.rows; r0 += kTakeThreads, flip ^= 1) {
-    const int32_t r = r0 + tid;
-    int64_t total;
-    const int64_t x = r < a.rows ? min(a.ws_want[r], a.pages) : 0;
-    const int64_t at = scan(x, parts[flip], total);
-    if (r < a.rows) a.ws_want[r] = (int32_t)min(want + at, (int64_t)a.pages);
-    want = (int32_t)min(want + total, (int64_t)a.pages);
-  }
-  int32_t got = 0;
-  constexpr int kPer = kPagesRun / 64;
-  for (int64_t base = 0; base < a.pages && got < want; base += kTakeWaves * kPagesRun, flip ^= 1) {
-    const int64_t p0 = base + (int64_t)wave * kPagesRun + lane;
-    unsigned long long free[kPer];
-    int32_t n = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int64_t p = p0 + i * 64;
-      free[i] = __ballot(p < a.pages && a.new_refs[min(p, (int64_t)a.pages - 1)] <= 0);
-    }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) n += __popcll(free[i]);
-    if (lane == 0) parts[flip][wave] = n;
+  for (int32_t i0 = 0; i0 < runs; i0 += kThreads, flip ^= 1) {
+    const int32_t i = i0 + tid, x = i < runs ? a.ws_runs[i] : 0;
+    int64_t at = wave_inclusive_scan(x);
+    if (lane == 63) parts[flip][wave] = at;
     __syncthreads();
-    int32_t at = got, all = 0;
-    for (int w = 0; w < kTakeWaves; ++w) {
-      const int32_t x = (int32_t)parts[flip][w];
-      if (w < wave) at += x;
-      all += x;
+    at += sum;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) at += parts[flip][w];
+      sum += parts[flip][w];
     }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int32_t rank = at + __popcll(free[i] & below);
-      if (((free[i] >> lane) & 1) && rank < want) {
-        a.ws_list[rank] = (int32_t)(p0 + i * 64);
-        a.new_refs[p0 + i * 64] = 1;
-      }
-      at += __popcll(free[i]);
-    }
-    got = min(want, got + all);
+    if (i < runs) before[i] = (int32_t)(at - x);
   }
-  if (tid == 0) a.ws_total[0] = got;
-  __syncthreads();   // the list and the sums, for this workgroup's own reads
-  after(got);
+  __syncthreads();
+  return (int32_t)sum;
 }
 
-__global__ __launch_bounds__(kTakeThreads) void update_take_kernel(PagesArgs a) {
-  take_pages(a, [](int32_t) {});
+// The rank-th free page.
+__device__ __forceinline__ int32_t free_page(const PagesArgs &a, const int32_t *before, int32_t rank) {
+  int32_t lo = 0, hi = (a.pages + kPagesRun - 1) / kPagesRun;   // the last run with before[run] <= rank that has any
+  while (hi - lo > 1) {
+    const int32_t mid = (lo + hi) / 2;
+    if (before[mid] <= rank) lo = mid;
+    else hi = mid;
+  }
+  rank -= before[lo];
+  unsigned long long words[kRunWords];
+#pragma unroll
+  for (int i = 0; i < kRunWords; ++i) words[i] = a.ws_bits[(int64_t)lo * kRunWords + i];
+  unsigned long long word = 0;
+  int32_t page = lo * kPagesRun;
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < kRunWords; ++i) {
+    const int32_t n = __popcll(words[i]);
+    if (!found && rank < n) {
+      found = true;
+      word = words[i];
+      page += i * 64;
+    }
+    if (!found) rank -= n;
+  }
+#pragma unroll
+  for (int half = 32; half >= 1; half /= 2) {
+    const int32_t n = __popcll(word & ((1ull << half) - 1));
+    if (rank >= n) {
+      rank -= n;
+      word >>= half;
+      page += half;
+    }
+  }
+  return page;
 }
 
-// A workgroup per row: its entries without a page get the row's share of the
-// list, in order; and how far the row reaches.
+// What rows [0, n) want, for a workgroup of 4 waves.
+__device__ __forceinline__ int64_t wanted_before(const PagesArgs &a, int32_t n, int64_t *parts) {
+  int64_t sum = 0;
+  for (int32_t i = threadIdx.x; i < n; i += kThreads) sum += a.ws_want[i];
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+  if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  return parts[0] + parts[1] + parts[2] + parts[3];
+}
+
+// A workgroup per row: its entries without a page get the row's share of the free
+// ones, in order; and how far the row reaches.
 __global__ __launch_bounds__(kThreads) void update_assign_kernel(PagesArgs a) {
+  extern __shared__ int32_t before[];
   __shared__ int32_t parts[2][4];
+  __shared__ int64_t sums[4];
   __shared__ int32_t missing;
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t c = a.context_len[r], need = a.need_len[r], ps = a.page_size;
@@ -154,12 +190,15 @@ __global__ __launch_bounds__(kThreads) void update_assign_kernel(PagesArgs a) {
     if (tid == 0) a.capacity[r] = 0;
     return;
   }
-  int32_t first, last;
+  int32_t first, last, got = 0;
   wanted_range(a, c, need, first, last);
   if (tid == 0) missing = a.stride;
   int32_t *row = a.new_table + (int64_t)r * a.stride;
-  int32_t rank0 = a.ws_want[r];
-  const int32_t got = a.ws_total[0];
+  int64_t rank0 = 0;
+  if (a.ws_want[r] > 0) {
+    rank0 = wanted_before(a, r, sums);
+    got = sum_runs(a, before);
+  }
   __syncthreads();
   // (an entry that holds some of the c tokens is looked at, and left as it is)
   const int32_t begin = (int32_t)min(c / ps, (int64_t)a.stride);
@@ -170,14 +209,19 @@ __global__ __launch_bounds__(kThreads) void update_assign_kernel(PagesArgs a) {
     const unsigned long long wants = __ballot(without && e >= first);
     if (lane == 0) parts[flip][wave] = __popcll(wants);
     __syncthreads();
-    int32_t rank = rank0 + __popcll(wants & ((1ull << lane) - 1));
+    int64_t rank = rank0 + __popcll(wants & ((1ull << lane) - 1));
     for (int w = 0; w < 4; ++w) {
       if (w < wave) rank += parts[flip][w];
       rank0 += parts[flip][w];
     }
     if (without) {
-      if (e >= first && rank < got) row[e] = a.ws_list[rank];
-      else atomicMin(&missing, e);
+      if (e >= first && rank < got) {
+        const int32_t p = free_page(a, before, (int32_t)rank);
+        row[e] = p;
+        a.new_refs[p] = 1;
+      } else {
+        atomicMin(&missing, e);
+      }
     }
   }
   __syncthreads();
@@ -223,27 +267,30 @@ __global__ __launch_bounds__(kThreads) void fork_rows_kernel(PagesArgs a) {
   }
 }
 
-// The copies' pages.  (After the launch before, ws_want tells who wants one; the
-// sums that take_pages leaves there tell it by their steps.)
-__global__ __launch_bounds__(kTakeThreads) void fork_take_kernel(PagesArgs a) {
-  take_pages(a, [&](int32_t got) {
-    for (int32_t r = threadIdx.x; r < a.rows; r += kTakeThreads) {
-      const int32_t s = a.source[r];
-      if (s < 0 || s >= a.sources) continue;
-      const int64_t c = a.new_len[r];
-      const int32_t whole = (int32_t)(c / a.page_size);
-      if (c % a.page_size == 0) continue;
-      int32_t *entry = a.new_table + (int64_t)r * a.stride + whole;
-      const int32_t from = a.table[(int64_t)s * a.stride + whole], rank = a.ws_want[r];
-      if (*entry == from || !in_pool(a, from)) continue;   // (its own, as the first that takes it)
-      if (rank < got) {
-        a.copy_src[r] = from;
-        a.copy_dst[r] = *entry = a.ws_list[rank];
-      } else {
-        a.new_len[r] = whole * a.page_size;
-      }
-    }
-  });
+// The copies' pages, a thread per row.
+__global__ __launch_bounds__(kThreads) void fork_assign_kernel(PagesArgs a) {
+  extern __shared__ int32_t before[];
+  __shared__ int32_t parts[4];
+  __shared__ int64_t sums[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t r0 = blockIdx.x * kThreads, r = r0 + tid;
+  const bool want = r < a.rows && a.ws_want[r] != 0;
+  const unsigned long long wants = __ballot(want);
+  if (lane == 0) parts[wave] = __popcll(wants);
+  int64_t rank = wanted_before(a, r0, sums) + __popcll(wants & ((1ull << lane) - 1));
+  for (int w = 0; w < wave; ++w) rank += parts[w];
+  const int32_t got = sum_runs(a, before);
+  if (!want) return;
+  const int32_t whole = a.new_len[r] / a.page_size;
+  if (rank < got) {
+    const int32_t p = free_page(a, before, (int32_t)rank);
+    a.copy_src[r] = a.table[(int64_t)a.source[r] * a.stride + whole];
+    a.copy_dst[r] = p;
+    a.new_table[(int64_t)r * a.stride + whole] = p;
+    a.new_refs[p] = 1;
+  } else {
+    a.new_len[r] = whole * a.page_size;
+  }
 }
 
 // Pages in use per run of kPagesRun, a wave each.
@@ -252,12 +299,10 @@ __global__ __launch_bounds__(kThreads) void compact_count_kernel(PagesArgs a) {
   const int64_t run = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int64_t p0 = run * kPagesRun;
   if (p0 >= a.pages) return;
-  int32_t n = 0;
+  int32_t x[kRunWords], n = 0;
+  load_run(a.refs, a.pages, p0, 0, x);
 #pragma unroll
-  for (int i = 0; i < kPagesRun / 64; ++i) {
-    const int64_t p = p0 + i * 64 + lane;
-    n += __popcll(__ballot(p < a.pages && a.refs[min(p, (int64_t)a.pages - 1)] > 0));
-  }
+  for (int i = 0; i < kRunWords; ++i) n += __popcll(__ballot(x[i] > 0));
   if (lane == 0) a.ws_runs[run] = n;
 }
 
@@ -267,12 +312,14 @@ __global__ __launch_bounds__(kThreads) void compact_rank_kernel(PagesArgs a) {
   __shared__ int32_t parts[3][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t runs = (a.pages + kPagesRun - 1) / kPagesRun;
-  const int32_t run0 = blockIdx.x * 4;
+  const int32_t run0 = blockIdx.x * 4, run = run0 + wave;
+  int32_t x[kRunWords];
+  if (run < runs) load_run(a.refs, a.pages, (int64_t)run * kPagesRun, 0, x);
   int32_t all = 0, before = 0;
   for (int32_t i = tid; i < runs; i += kThreads) {
-    const int32_t x = a.ws_runs[i];
-    all += x;
-    if (i < run0) before += x;
+    const int32_t n = a.ws_runs[i];
+    all += n;
+    if (i < run0) before += n;
   }
   const int32_t used = group_sum(all, parts[0]);
   before = group_sum(before, parts[1]);
@@ -286,14 +333,13 @@ __global__ __launch_bounds__(kThreads) void compact_rank_kernel(PagesArgs a) {
     a.counts[0] = used;
     a.counts[1] = moves;
   }
-  const int32_t run = run0 + wave;
   if (run >= runs) return;
   for (int32_t i = run0; i < run; ++i) before += a.ws_runs[i];
   const unsigned long long below = (1ull << lane) - 1;
-#pragma unroll 4
-  for (int i = 0; i < kPagesRun / 64; ++i) {
+#pragma unroll
+  for (int i = 0; i < kRunWords; ++i) {
     const int32_t p = run * kPagesRun + i * 64 + lane;
-    const bool is_used = p < a.pages && a.refs[min(p, a.pages - 1)] > 0;
+    const bool is_used = x[i] > 0;
     const unsigned long long mask = __ballot(is_used);
     const int32_t rank = before + __popcll(mask & below);   // pages in use before p
     before += __popcll(mask);
@@ -374,6 +420,15 @@ hipError_t copy_refs(const PagesArgs &a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+hipError_t find_free(const PagesArgs &a, hipStream_t stream) {
+  if (a.pages == 0) return hipSuccess;
+  hipLaunchKernelGGL(free_pages_kernel, dim3(blocks_of(a.pages, 4 * kPagesRun)), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+// LDS of the kernels that hand out free pages: at most 32 KB, of 2^23 pages.
+unsigned run_bytes(const PagesArgs &a) { return blocks_of(a.pages, kPagesRun) * 4; }
+
 }  // namespace
 
 hipError_t launch_update_pages(const PagesArgs &a, hipStream_t stream) {
@@ -382,10 +437,9 @@ hipError_t launch_update_pages(const PagesArgs &a, hipStream_t stream) {
   hipLaunchKernelGGL(update_drop_kernel, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
   e = hipGetLastError();
   if (e != hipSuccess || !a.need_len) return e;
-  hipLaunchKernelGGL(update_take_kernel, dim3(1), dim3(kTakeThreads), 0, stream, a);
-  e = hipGetLastError();
+  e = find_free(a, stream);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(update_assign_kernel, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(update_assign_kernel, dim3((unsigned)a.rows), dim3(kThreads), run_bytes(a), stream, a);
   return hipGetLastError();
 }
 
@@ -395,7 +449,9 @@ hipError_t launch_fork_pages(const PagesArgs &a, hipStream_t stream) {
   hipLaunchKernelGGL(fork_rows_kernel, dim3((unsigned)(a.sources + a.rows)), dim3(kThreads), 0, stream, a);
   e = hipGetLastError();
   if (e != hipSuccess || a.rows == 0) return e;
-  hipLaunchKernelGGL(fork_take_kernel, dim3(1), dim3(kTakeThreads), 0, stream, a);
+  e = find_free(a, stream);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(fork_assign_kernel, dim3(blocks_of(a.rows, kThreads)), dim3(kThreads), run_bytes(a), stream, a);
   return hipGetLastError();
 }
 

@@ -112,8 +112,8 @@ def test_workspace_queries(lib):
     for bad in ((4, 1000, 8, 2, 128, 16, 0, 4, 1), (4, 1000, 8, 2, 128, 16, 100, -4, 1), (4, -1, 8, 2, 128, 16, 100, 4, 1)):
         assert query(*bad) == SIZE_MAX
     query = lib.adaserve_pages_workspace_bytes
-    assert query(0, 0) != SIZE_MAX and query(65536, 2 ** 24) != SIZE_MAX
-    for bad in ((-1, 5), (5, -1), (65537, 5), (5, 2 ** 24 + 1)):
+    assert query(0, 0) != SIZE_MAX and query(65536, 2 ** 23) != SIZE_MAX
+    for bad in ((-1, 5), (5, -1), (65537, 5), (5, 2 ** 23 + 1)):
         assert query(*bad) == SIZE_MAX
 
 
@@ -130,7 +130,7 @@ def _update(lib, **kw):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(B=-1), BAD), (dict(B=65537), UNSUP), (dict(pages=-1), BAD), (dict(pages=2 ** 24 + 1), UNSUP), (dict(bts=-1), BAD),
+    (dict(B=-1), BAD), (dict(B=65537), UNSUP), (dict(pages=-1), BAD), (dict(pages=2 ** 23 + 1), UNSUP), (dict(bts=-1), BAD),
     (dict(bts=2 ** 24 + 1), UNSUP), (dict(ps=0), BAD), (dict(ps=65537), UNSUP), (dict(w=-1), BAD), (dict(s=-1), BAD),
     (dict(need=None), BAD), (dict(cap=None), BAD), (dict(clen=None), BAD), (dict(bt=None), BAD), (dict(refs=None), BAD),
     (dict(nbt=None), BAD), (dict(nrefs=None), BAD), (dict(ws=None), WS), (dict(wsb=100), WS), (dict(ws=at(8) + 4), BAD),
@@ -187,10 +187,10 @@ def _copy(lib, **kw):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(n=-1), BAD), (dict(n=2 ** 24 + 1), UNSUP), (dict(layers=-1), BAD), (dict(layers=65537), UNSUP), (dict(pages=-1), BAD),
-    (dict(pages=2 ** 24 + 1), UNSUP), (dict(hkv=0), BAD), (dict(hkv=4097), UNSUP), (dict(d=0), BAD), (dict(d=12), UNSUP),
+    (dict(n=-1), BAD), (dict(n=2 ** 23 + 1), UNSUP), (dict(layers=-1), BAD), (dict(layers=65537), UNSUP), (dict(pages=-1), BAD),
+    (dict(pages=2 ** 23 + 1), UNSUP), (dict(hkv=0), BAD), (dict(hkv=4097), UNSUP), (dict(d=0), BAD), (dict(d=12), UNSUP),
     (dict(d=4104), UNSUP), (dict(ps=0), BAD), (dict(ps=65537), UNSUP), (dict(dtype=3), BAD), (dict(stride=2 * 16 * 64 * 10 - 8), BAD),
-    (dict(stride=2 ** 20 + 4), BAD), (dict(stride=2 ** 48), UNSUP), (dict(pages=2 ** 24, hkv=4096, ps=65536, d=4096), UNSUP),
+    (dict(stride=2 ** 20 + 4), BAD), (dict(stride=2 ** 48), UNSUP), (dict(pages=2 ** 23, hkv=4096, ps=65536, d=4096), UNSUP),
     (dict(src=None), BAD), (dict(dst=None), BAD), (dict(kp=None), BAD), (dict(vp=None), BAD), (dict(src=at(1) + 2), BAD),
     (dict(count=at(5) + 1), BAD), (dict(kp=at(3) + 8), BAD), (dict(vp=at(4) + 4), BAD),
 ])
