@@ -37,6 +37,15 @@ struct PagesArgs {
   int32_t *ws_runs;              // [runs] free pages, or pages in use, per run
 };
 
+// Caches whose pages and tables one workgroup goes over sooner than several
+// launches do.
+constexpr int kSmallPages = 4096;
+constexpr int kSmallSteps = 32;          // 64 entries of a row per step of its 16 waves
+constexpr int kSmallRows = 1024;         // of either table
+inline bool small_cache(int64_t rows, int64_t stride, int32_t pages) {
+  return pages <= kSmallPages && rows <= kSmallRows && ((rows + 15) / 16) * ((stride + 63) / 64) <= kSmallSteps;
+}
+
 struct CopyPagesArgs {
   int32_t copies;
   const int32_t *src, *dst;
@@ -64,6 +73,9 @@ inline PagesSpace pages_space(int32_t rows, int32_t pages) {
 hipError_t launch_update_pages(const PagesArgs &a, hipStream_t stream);
 hipError_t launch_fork_pages(const PagesArgs &a, hipStream_t stream);
 hipError_t launch_compact_pages(const PagesArgs &a, hipStream_t stream);
+hipError_t launch_update_small(const PagesArgs &a, hipStream_t stream);
+hipError_t launch_fork_small(const PagesArgs &a, hipStream_t stream);
+hipError_t launch_compact_small(const PagesArgs &a, hipStream_t stream);
 hipError_t launch_copy_pages(const CopyPagesArgs &a, hipStream_t stream);
 
 }  // namespace adaserve
