@@ -599,14 +599,36 @@ def adaserve_pages_workspace_bytes(num_rows: int, num_pages: int) -> int:
     return n
 
 
-def _int32s(shaped) -> None:
-    """Every tensor that is given is int32 and of its shape."""
+def _int32s(shaped):
+    """The device and the pointers of int32 tensors (None -> NULL), each of its shape."""
     import torch
+    int32, device, pointers = torch.int32, -1, []
     for t, name, shape in shaped:
-        if t is not None:
-            _typed(t, torch.int32, name)
-            if t.shape != shape:
-                raise ValueError("%s must be %s, is %s" % (name, list(shape), list(t.shape)))
+        if t is None:
+            pointers.append(None)
+            continue
+        if t.dtype is not int32 or t.shape != shape:
+            raise ValueError("%s must be int32 %s, is %s %s" % (name, list(shape), t.dtype, list(t.shape)))
+        at = t.get_device()
+        if at != device:
+            if at < 0 or device >= 0:
+                raise ValueError("expected a device tensor" if at < 0 else "tensors are on different devices")
+            device = at
+        if not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+        pointers.append(t.data_ptr())
+    return device, pointers
+
+
+def _on_device(t, device, name: str):
+    """Pointer of a tensor on the device of the others."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError("expected a device tensor" if t.get_device() < 0 else "tensors are on different devices")
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
 
 
 def adaserve_update_pages(*, context_len, block_table, page_refs, page_size: int, need_len=None, capacity=None,
@@ -617,13 +639,13 @@ def adaserve_update_pages(*, context_len, block_table, page_refs, page_size: int
     B, stride = block_table.shape
     new_bt = block_table if new_block_table is None else new_block_table
     new_refs = page_refs if new_page_refs is None else new_page_refs
-    _int32s(((context_len, "context_len", (B,)), (need_len, "need_len", (B,)), (capacity, "capacity", (B,)),
-             (block_table, "block_table", (B, stride)), (new_bt, "new_block_table", (B, stride)),
-             (page_refs, "page_refs", (page_refs.shape[0],)), (new_refs, "new_page_refs", (page_refs.shape[0],))))
-    device, (clen, need, bt, refs, nbt, nrefs, cap, ws) = _pointers(
-        (context_len, need_len, block_table, page_refs, new_bt, new_refs, capacity, workspace))
-    _device_call("adaserve_update_pages", device, stream, B, clen, need, window, sinks, page_size, bt, stride, refs,
-                 page_refs.shape[0], nbt, nrefs, cap, ws, _bytes(workspace))
+    P, rows, table = page_refs.shape[0], (B,), (B, stride)
+    device, (clen, need, bt, refs, nbt, nrefs, cap) = _int32s((
+        (context_len, "context_len", rows), (need_len, "need_len", rows), (block_table, "block_table", table),
+        (page_refs, "page_refs", (P,)), (new_bt, "new_block_table", table), (new_refs, "new_page_refs", (P,)),
+        (capacity, "capacity", rows)))
+    _device_call("adaserve_update_pages", device, stream, B, clen, need, window, sinks, page_size, bt, stride, refs, P, nbt,
+                 nrefs, cap, _on_device(workspace, device, "workspace"), _bytes(workspace))
 
 
 def adaserve_fork_pages(*, source, context_len, block_table, page_refs, page_size: int, new_block_table, new_context_len,
@@ -632,15 +654,14 @@ def adaserve_fork_pages(*, source, context_len, block_table, page_refs, page_siz
     [B, stride] and new_context_len [B]; page copy_src[r] is to be copied to copy_dst[r] (-1: none)."""
     (S, stride), B = block_table.shape, source.shape[0]
     new_refs = page_refs if new_page_refs is None else new_page_refs
-    _int32s(((source, "source", (B,)), (context_len, "context_len", (S,)), (block_table, "block_table", (S, stride)),
-             (new_block_table, "new_block_table", (B, stride)), (new_context_len, "new_context_len", (B,)),
-             (copy_src, "copy_src", (B,)), (copy_dst, "copy_dst", (B,)), (page_refs, "page_refs", (page_refs.shape[0],)),
-             (new_refs, "new_page_refs", (page_refs.shape[0],))))
-    device, (src, clen, bt, refs, nbt, nlen, nrefs, cs, cd, ws) = _pointers(
-        (source, context_len, block_table, page_refs, new_block_table, new_context_len, new_refs, copy_src, copy_dst,
-         workspace))
-    _device_call("adaserve_fork_pages", device, stream, S, B, src, clen, page_size, bt, stride, refs, page_refs.shape[0],
-                 nbt, nlen, nrefs, cs, cd, ws, _bytes(workspace))
+    P, rows = page_refs.shape[0], (B,)
+    device, (src, clen, bt, refs, nbt, nlen, nrefs, cs, cd) = _int32s((
+        (source, "source", rows), (context_len, "context_len", (S,)), (block_table, "block_table", (S, stride)),
+        (page_refs, "page_refs", (P,)), (new_block_table, "new_block_table", (B, stride)),
+        (new_context_len, "new_context_len", rows), (new_refs, "new_page_refs", (P,)), (copy_src, "copy_src", rows),
+        (copy_dst, "copy_dst", rows)))
+    _device_call("adaserve_fork_pages", device, stream, S, B, src, clen, page_size, bt, stride, refs, P, nbt, nlen, nrefs,
+                 cs, cd, _on_device(workspace, device, "workspace"), _bytes(workspace))
 
 
 def adaserve_compact_pages(*, block_table, page_refs, new_place, move_src, move_dst, counts, new_block_table=None,
@@ -651,24 +672,24 @@ def adaserve_compact_pages(*, block_table, page_refs, new_place, move_src, move_
     P = page_refs.shape[0]
     new_bt = block_table if new_block_table is None else new_block_table
     new_refs = page_refs if new_page_refs is None else new_page_refs
-    _int32s(((block_table, "block_table", (B, stride)), (new_bt, "new_block_table", (B, stride)),
-             (page_refs, "page_refs", (P,)), (new_refs, "new_page_refs", (P,)), (new_place, "new_place", (P,)),
-             (move_src, "move_src", (P,)), (move_dst, "move_dst", (P,)), (counts, "counts", (2,))))
-    device, (bt, refs, nbt, nrefs, place, ms, md, cnt, ws) = _pointers(
-        (block_table, page_refs, new_bt, new_refs, new_place, move_src, move_dst, counts, workspace))
-    _device_call("adaserve_compact_pages", device, stream, B, bt, stride, refs, P, nbt, nrefs, place, ms, md, cnt, ws,
-                 _bytes(workspace))
+    table, pool = (B, stride), (P,)
+    device, (bt, refs, nbt, nrefs, place, ms, md, cnt) = _int32s((
+        (block_table, "block_table", table), (page_refs, "page_refs", pool), (new_bt, "new_block_table", table),
+        (new_refs, "new_page_refs", pool), (new_place, "new_place", pool), (move_src, "move_src", pool),
+        (move_dst, "move_dst", pool), (counts, "counts", (2,))))
+    _device_call("adaserve_compact_pages", device, stream, B, bt, stride, refs, P, nbt, nrefs, place, ms, md, cnt,
+                 _on_device(workspace, device, "workspace"), _bytes(workspace))
 
 
 def adaserve_copy_pages(*, src, dst, k_pages, v_pages, count=None, stream=None) -> None:
     """Pages src [n] of k_pages and v_pages ([P, Hkv, page_size, D], or [layers, P, Hkv, page_size, D]) to pages dst [n]
     (-1: none); count [1]: how many of them, read on the device."""
     n = src.shape[0]
-    _int32s(((src, "src", (n,)), (dst, "dst", (n,)), (count, "count", (1,))))
+    device, (s, d, c) = _int32s(((src, "src", (n,)), (dst, "dst", (n,)), (count, "count", (1,))))
     if k_pages.dim() not in (4, 5) or v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype:
         raise ValueError("k_pages and v_pages must be [pages, kv-heads, page_size, dim], or that of every layer")
     layers = k_pages.shape[0] if k_pages.dim() == 5 else 1
     P, hkv, ps, D = k_pages.shape[-4:]
-    device, (s, d, c, kp, vp) = _pointers((src, dst, count, k_pages, v_pages))
-    _device_call("adaserve_copy_pages", device, stream, n, s, d, c, kp, vp, layers, P * hkv * ps * D, P, hkv, ps, D,
+    _device_call("adaserve_copy_pages", device, stream, n, s, d, c, _on_device(k_pages, device, "k_pages"),
+                 _on_device(v_pages, device, "v_pages"), layers, P * hkv * ps * D, P, hkv, ps, D,
                  _dtype_code(k_pages))

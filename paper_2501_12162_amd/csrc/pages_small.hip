@@ -77,6 +77,23 @@ struct PageBits {
   }
 };
 
+// f(row, entry, value) of all entries of a table, a thread's next four loaded together.
+template <class F>
+__device__ __forceinline__ void for_entries(const int32_t *table, int32_t rows, int32_t stride, F f) {
+  constexpr int kAtOnce = 4;
+  const uint32_t n = (uint32_t)rows * (uint32_t)stride, wide = (uint32_t)stride;
+  for (uint32_t i0 = threadIdx.x; i0 < n; i0 += kAtOnce * kThreads) {
+    int32_t x[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) x[k] = table[min(i0 + k * kThreads, n - 1)];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const uint32_t i = i0 + k * kThreads, r = i / wide;
+      if (i < n) f((int32_t)r, (int32_t)(i - r * wide), x[k]);
+    }
+  }
+}
+
 // want[r] becomes the sum of the rows before r; by the first wave, up to its own barrier.
 __device__ __forceinline__ void sum_wants(int32_t *want, int32_t rows) {
   if (threadIdx.x < 64) {
@@ -94,42 +111,33 @@ __device__ __forceinline__ void sum_wants(int32_t *want, int32_t rows) {
 __global__ __launch_bounds__(kThreads) void update_small_kernel(PagesArgs a) {
   extern __shared__ int32_t refs[];
   __shared__ PageBits bits;
-  __shared__ int32_t want[kSmallRows];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ int32_t want[kSmallRows], from[kSmallRows], to[kSmallRows], first[kSmallRows], last[kSmallRows];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t ps = a.page_size;
   load_refs(a, refs);
-  __syncthreads();
-  // a row's entries that are to have pages: [first, last)
-  auto range = [&](int32_t c, int32_t need, int32_t &first, int32_t &last) {
-    first = min((int32_t)(((int64_t)c + ps - 1) / ps), a.stride);
-    last = need > 0 ? min((int32_t)(((int64_t)need + ps - 1) / ps), a.stride) : 0;
-    last = max(last, first);
-  };
-  for (int32_t r = wave; r < a.rows; r += kWaves) {
-    const int32_t c = a.context_len[r];
-    const int32_t *in = a.table + (int64_t)r * a.stride;
-    int32_t *out = a.new_table + (int64_t)r * a.stride;
-    int32_t from = 0, to = a.stride, first = 0, last = 0;   // entries [from, to) go
-    if (c >= 0) {
-      from = (int32_t)(((int64_t)a.sinks + ps - 1) / ps);
-      to = a.window > 0 && c >= a.window ? (c - a.window + 1) / ps : 0;
-      if (a.need_len) range(c, a.need_len[r], first, last);
+  if (tid < a.rows) {
+    // entries [from, to) go, [first, last) are to have pages
+    const int32_t c = a.context_len[tid];
+    int32_t f = 0, l = 0;
+    from[tid] = c < 0 ? 0 : (int32_t)(((int64_t)a.sinks + ps - 1) / ps);
+    to[tid] = c < 0 ? a.stride : a.window > 0 && c >= a.window ? (c - a.window + 1) / ps : 0;
+    if (a.need_len && c >= 0) {
+      const int32_t need = a.need_len[tid];
+      f = min((int32_t)(((int64_t)c + ps - 1) / ps), a.stride);
+      l = need > 0 ? max(f, min((int32_t)(((int64_t)need + ps - 1) / ps), a.stride)) : f;
     }
-    int32_t n = 0;
-    for (int32_t e0 = 0; e0 < a.stride; e0 += 64) {
-      const int32_t e = e0 + lane;
-      if (e < a.stride) {
-        const int32_t p = in[e];
-        const bool has = in_pool(a, p), gone = e >= from && e < to;
-        if (gone && has) atomicAdd(&refs[p], -1);
-        if (gone || out != in) out[e] = gone ? -1 : p;
-        n += e >= first && e < last && (gone || !has);
-      }
-    }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) n += __shfl_xor(n, off, 64);
-    if (lane == 0) want[r] = n;
+    first[tid] = f;
+    last[tid] = l;
+    want[tid] = 0;
   }
+  __syncthreads();
+  const bool same = a.new_table == a.table;
+  for_entries(a.table, a.rows, a.stride, [&](int32_t r, int32_t e, int32_t p) {
+    const bool has = in_pool(a, p), gone = e >= from[r] && e < to[r];
+    if (gone && has) atomicAdd(&refs[p], -1);
+    if (gone || !same) a.new_table[(int64_t)r * a.stride + e] = gone ? -1 : p;
+    if (e >= first[r] && e < last[r] && (gone || !has)) atomicAdd(&want[r], 1);
+  });
   __syncthreads();
   if (a.need_len) {
     bits.set(refs, a.pages, [](int32_t n) { return n <= 0; });
@@ -141,15 +149,14 @@ __global__ __launch_bounds__(kThreads) void update_small_kernel(PagesArgs a) {
         if (lane == 0) a.capacity[r] = 0;
         continue;
       }
-      int32_t first, last, missing = a.stride, rank0 = want[r];
-      range(c, need, first, last);
+      int32_t missing = a.stride, rank0 = want[r];
       // (from the entry that holds some of the c tokens on nothing has gone: the window ends before it)
-      for (int32_t e0 = min(c / ps, a.stride); e0 < last; e0 += 64) {
+      for (int32_t e0 = min(c / ps, a.stride); e0 < last[r]; e0 += 64) {
         const int32_t e = e0 + lane;
-        const bool without = e < last && !in_pool(a, a.table[(int64_t)r * a.stride + e]);
-        const unsigned long long wants = __ballot(without && e >= first);
+        const bool without = e < last[r] && !in_pool(a, a.table[(int64_t)r * a.stride + e]);
+        const unsigned long long wants = __ballot(without && e >= first[r]);
         const int32_t rank = rank0 + __popcll(wants & ((1ull << lane) - 1));
-        const bool taken = without && e >= first && rank < got;
+        const bool taken = without && e >= first[r] && rank < got;
         if (taken) {
           const int32_t p = bits.at(rank, a.pages);
           refs[p] = 1;
@@ -172,48 +179,44 @@ __global__ __launch_bounds__(kThreads) void update_small_kernel(PagesArgs a) {
 __global__ __launch_bounds__(kThreads) void fork_small_kernel(PagesArgs a) {
   extern __shared__ int32_t refs[];
   __shared__ PageBits bits;
-  __shared__ int32_t want[kSmallRows], takers[kSmallRows], first[kSmallRows];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ int32_t want[kSmallRows], takers[kSmallRows], first[kSmallRows], tokens[kSmallRows], source[kSmallRows];
+  const int tid = threadIdx.x;
   const int32_t ps = a.page_size;
-  const int64_t most = (int64_t)a.stride * ps;
   load_refs(a, refs);
   if (tid < a.sources) {
     takers[tid] = 0;
     first[tid] = a.rows;
+    tokens[tid] = (int32_t)min((int64_t)max(a.context_len[tid], 0), (int64_t)a.stride * ps);
   }
+  int32_t mine = tid < a.rows ? a.source[tid] : -1;   // (a thread per row, too)
+  if (mine < 0 || mine >= a.sources) mine = -1;
+  if (tid < a.rows) source[tid] = mine;
   __syncthreads();
-  const int32_t mine = tid < a.rows ? a.source[tid] : -1;   // (a thread per row, too)
-  const bool any = mine >= 0 && mine < a.sources;
-  if (any) {
+  if (mine >= 0) {
     atomicAdd(&takers[mine], 1);
     atomicMin(&first[mine], tid);
   }
   __syncthreads();
-  auto tokens = [&](int32_t s) { return (int32_t)min((int64_t)max(a.context_len[s], 0), most); };
-  for (int32_t s = wave; s < a.sources; s += kWaves) {
-    const int32_t whole = tokens(s) / ps, n = takers[s];
-    for (int32_t e = lane; e < a.stride; e += 64) {
-      const int32_t p = a.table[(int64_t)s * a.stride + e], more = e < whole ? n - 1 : n > 0 ? 0 : -1;
-      if (in_pool(a, p) && more != 0) atomicAdd(&refs[p], more);
-    }
-  }
+  for_entries(a.table, a.sources, a.stride, [&](int32_t s, int32_t e, int32_t p) {
+    const int32_t more = e < tokens[s] / ps ? takers[s] - 1 : takers[s] > 0 ? 0 : -1;
+    if (in_pool(a, p) && more != 0) atomicAdd(&refs[p], more);
+  });
   // a row's own entry of the partly filled page, where it needs one, is written at the end
   int32_t c = 0, from = -1;
   bool copy = false;
-  if (any) {
-    c = tokens(mine);
+  if (mine >= 0) {
+    c = tokens[mine];
     if (c % ps != 0 && first[mine] != tid) from = a.table[(int64_t)mine * a.stride + c / ps];
     copy = in_pool(a, from);
   }
   if (tid < a.rows) want[tid] = copy;
   __syncthreads();
-  for (int32_t r = wave; r < a.rows; r += kWaves) {
-    const int32_t s = a.source[r];
-    const bool ok = s >= 0 && s < a.sources;
-    const int32_t whole = ok ? tokens(s) / ps : 0, upto = !ok ? 0 : first[s] == r ? a.stride : whole;
-    const int32_t skip = want[r] ? whole : -1;
-    for (int32_t e = lane; e < a.stride; e += 64)
-      if (e != skip) a.new_table[(int64_t)r * a.stride + e] = e < upto ? a.table[(int64_t)s * a.stride + e] : -1;
+  const uint32_t n = (uint32_t)a.rows * (uint32_t)a.stride, wide = (uint32_t)a.stride;
+#pragma unroll 4
+  for (uint32_t i = tid; i < n; i += kThreads) {
+    const int32_t r = (int32_t)(i / wide), e = (int32_t)(i - r * wide), s = source[r];
+    const int32_t whole = s >= 0 ? tokens[s] / ps : 0, upto = s < 0 ? 0 : first[s] == r ? a.stride : whole;
+    if (!(want[r] && e == whole)) a.new_table[i] = e < upto ? a.table[(int64_t)s * a.stride + e] : -1;   // (no old row: no read)
   }
   __syncthreads();
   bits.set(refs, a.pages, [](int32_t n) { return n <= 0; });

@@ -333,11 +333,18 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   };
   auto mask = [&](f32x16 &x, int rt, int blk) {
     const int32_t left = vis[rt] - blk * KB - half * 4;
-    const int32_t from = vis_lo[rt] - blk * KB - half * 4, sunk = sinks - blk * KB - half * 4;
+    if constexpr (WINDOW) {
+      // a bit per key that is seen, spread over the word that picks the score or -inf
+      const auto below = [](int32_t n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
+      const uint32_t seen = below(left) & (~below(vis_lo[rt] - blk * KB - half * 4) | below(sinks - blk * KB - half * 4));
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int key = (i >> 2) * 8 + (i & 3);
-      x[i] = key < left && (!WINDOW || key >= from || key < sunk) ? x[i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int)seen, (i >> 2) * 8 + (i & 3), 1);
+        x[i] = __uint_as_float((__float_as_uint(x[i]) & all) | (0xff800000u & ~all));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = (i >> 2) * 8 + (i & 3) < left ? x[i] : -INFINITY;
     }
   };
   auto rowmax = [&](const f32x16 &x) {
@@ -351,14 +358,10 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
     return max_over_halves(__builtin_elementwise_maximum(__builtin_elementwise_maximum(m0, m1), x[15]));
   };
   // Takes row half rt's reference up to the maximum bm of sub-block scores where
-  // that is more than 2^8 above it.  Over a window that is done behind blocks without
-  // maxima, too: `beyond` keeps that their sums were further than with maxima, which
-  // the checks at the end no longer see (and a factor below 2^-126 loses them).
-  bool beyond = false;
+  // that is more than 2^8 above it.
   auto rescale = [&](int rt, float bm) __attribute__((always_inline)) {
     const bool up = bm > m_ref[rt] + up_raw;
     if (__any(up)) {
-      if (WINDOW) beyond = beyond || (up && !(lsum[rt] <= 0x1p8f * (float)k_end));
       const float mn = up ? bm : m_ref[rt];
       const float al = __builtin_amdgcn_exp2f((m_ref[rt] - mn) * c);
       m_ref[rt] = mn;
@@ -397,8 +400,12 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
     constexpr bool kMasked = decltype(masked)::value;
     constexpr bool kDma = decltype(dma)::value;
     constexpr int SLOTS = KS + 2 * DT;   // matrix instructions
-    if constexpr (kMasked) mask(sy, ry, yblk);
-    if (kMasked && (WINDOW || careful)) rescale(ry, rowmax(sy));
+    // Over a window, whose tiles are short, sub-blocks that all rows of the wave see take
+    // no mask on this path either.  Maxima are taken up to n_edge, by when every row that
+    // sees a key has a reference; none behind blocks without (a reference that jumps by
+    // 2^126 would lose their sums, and the checks at the end would not see it).
+    if (kMasked && (!WINDOW || careful || yblk < n_edge || yblk >= n_full)) mask(sy, ry, yblk);
+    if (kMasked && (careful || (WINDOW && yblk < n_edge))) rescale(ry, rowmax(sy));
     // A slot is one matrix instruction and the vector work that issues while it
     // runs: one step each of a few weights (scale; exponential; sum and
     // rounding), none of which waits for another, and two LDS reads.  The empty
@@ -520,7 +527,6 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
   start(load_pages(un, 0));
 #pragma unroll 1
   for (;;) {
-    beyond = false;
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
       lsum[rt] = 0.f;
@@ -580,7 +586,7 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
       any_sub(i++);
     }
     if (!careful) {
-      beyond = beyond || !(lsum[0] < kMost) || !(lsum[1] < kMost);
+      bool beyond = !(lsum[0] < kMost) || !(lsum[1] < kMost);
       // (rarely: 2 x 16 DT comparisons)
       const float fair = 0x1p8f * (float)k_end;
       if (__any(fmaxf(lsum[0], lsum[1]) > fair)) {
