@@ -37,13 +37,15 @@ struct PagesArgs {
   int32_t *ws_runs;              // [runs] free pages, or pages in use, per run
 };
 
-// Caches whose pages and tables one workgroup goes over sooner than several
-// launches do.
+// Caches small enough for one workgroup (pages_small.hip).  In a graph, 4096 pages,
+// one launch against three or four: update of 64 rows of 64 entries 9.4 | 11.7 us, 24 of 256
+// 8.0 | 11.4, 128 of 40 12.6 | 11.7 (its rows' second pass takes 16 at a time); fork of 128 rows of
+// 40 entries 10.0 | 10.5, 24 of 256 10.4 | 10.4, 128 of 128 18.4 | 10.5; compaction of 128 rows of
+// 128 entries 8.1 | 10.1, of 256 11.0 | 10.4.
 constexpr int kSmallPages = 4096;
-constexpr int kSmallSteps = 32;          // 64 entries of a row per step of its 16 waves
-constexpr int kSmallRows = 1024;         // of either table
-inline bool small_cache(int64_t rows, int64_t stride, int32_t pages) {
-  return pages <= kSmallPages && rows <= kSmallRows && ((rows + 15) / 16) * ((stride + 63) / 64) <= kSmallSteps;
+constexpr int kSmallRows = 1024;         // of either table: a thread each
+inline bool small_cache(int64_t rows, int64_t stride, int32_t pages, int64_t most_rows, int64_t most_entries) {
+  return pages <= kSmallPages && rows <= most_rows && rows * stride <= most_entries;
 }
 
 struct CopyPagesArgs {

@@ -432,7 +432,7 @@ unsigned run_bytes(const PagesArgs &a) { return blocks_of(a.pages, kPagesRun) * 
 }  // namespace
 
 hipError_t launch_update_pages(const PagesArgs &a, hipStream_t stream) {
-  if (small_cache(a.rows, a.stride, a.pages)) return launch_update_small(a, stream);
+  if (small_cache(a.rows, a.stride, a.pages, 64, 6144)) return launch_update_small(a, stream);
   hipError_t e = copy_refs(a, stream);
   if (e != hipSuccess || a.rows == 0) return e;
   hipLaunchKernelGGL(update_drop_kernel, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
@@ -445,7 +445,7 @@ hipError_t launch_update_pages(const PagesArgs &a, hipStream_t stream) {
 }
 
 hipError_t launch_fork_pages(const PagesArgs &a, hipStream_t stream) {
-  if (small_cache(a.rows > a.sources ? a.rows : a.sources, a.stride, a.pages)) return launch_fork_small(a, stream);
+  if (small_cache(a.rows > a.sources ? a.rows : a.sources, a.stride, a.pages, kSmallRows, 6144)) return launch_fork_small(a, stream);
   hipError_t e = copy_refs(a, stream);
   if (e != hipSuccess || a.rows + a.sources == 0) return e;
   hipLaunchKernelGGL(fork_rows_kernel, dim3((unsigned)(a.sources + a.rows)), dim3(kThreads), 0, stream, a);
@@ -458,7 +458,7 @@ hipError_t launch_fork_pages(const PagesArgs &a, hipStream_t stream) {
 }
 
 hipError_t launch_compact_pages(const PagesArgs &a, hipStream_t stream) {
-  if (small_cache(a.rows, a.stride, a.pages)) return launch_compact_small(a, stream);
+  if (small_cache(a.rows, a.stride, a.pages, kSmallRows, 24576)) return launch_compact_small(a, stream);
   const unsigned runs = blocks_of(a.pages, 4 * kPagesRun);
   if (runs > 0) hipLaunchKernelGGL(compact_count_kernel, dim3(runs), dim3(kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
