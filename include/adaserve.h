@@ -758,7 +758,8 @@ int32_t adaserve_compact_pages(int32_t num_requests, const int32_t *block_table,
  * a page outside [0, num_pages), or src = dst, is left out.  No page is the dst of two
  * pairs, or the src of one and the dst of another.  num_layers pools [num_pages, Hkv,
  * page_size, D], layer_stride elements apart (any for one layer), are copied in one
- * launch.  Rows of a head are a multiple of 16 bytes; dtype F32 or BF16.
+ * launch.  Rows of a head are a multiple of 16 bytes; a page of one pool has at most 2^30;
+ * at most 2^23 pairs, 65536 layers, 4096 kv-heads, head_dim 4096; dtype F32 or BF16.
  */
 int32_t adaserve_copy_pages(int32_t num_copies, const int32_t *src, const int32_t *dst, const int32_t *count,
                             void *k_pages, void *v_pages, int32_t num_layers, int64_t layer_stride,

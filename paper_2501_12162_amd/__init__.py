@@ -343,7 +343,7 @@ def _device_call(name: str, device: int, stream, *args) -> None:
     current for the call where it is not."""
     import torch
     fn = getattr(load_library(), name)
-    s = (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+    s = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
     if device == torch.cuda.current_device():
         st = fn(*args, s)
     else:

@@ -230,8 +230,8 @@ int32_t adaserve_copy_pages(int32_t num_copies, const int32_t *src, const int32_
     return fail(ADASERVE_ERR_UNSUPPORTED, "num_kv_heads %d, head_dim %d: at most 4096 each, rows a multiple of 16 bytes",
                 num_kv_heads, head_dim);
   const int64_t page_bytes = (int64_t)num_kv_heads * page_size * head_dim * esz;
-  if (num_pages > 0 && page_bytes > ((int64_t)1 << 48) / num_pages)
-    return fail(ADASERVE_ERR_UNSUPPORTED, "a pool of %d pages of %lld bytes", num_pages, (long long)page_bytes);
+  if (page_bytes > (int64_t)1 << 30)
+    return fail(ADASERVE_ERR_UNSUPPORTED, "pages of %lld bytes exceed 2^30", (long long)page_bytes);
   if (num_layers > 1) {
     if (layer_stride < page_bytes / esz * num_pages || layer_stride * esz % 16 != 0)
       return fail(ADASERVE_ERR_INVALID_ARGUMENT, "layer_stride %lld: less than a pool, or not a multiple of 16 bytes",

@@ -83,9 +83,17 @@ __device__ __forceinline__ int find_plan_entry(const TreeAttnArgs &a, int64_t ke
   return -1;
 }
 
+// Prefix keys that request r reads.
+template <bool WINDOW>
+__device__ __forceinline__ int32_t prefix_keys(const TreeAttnArgs &a, int32_t r) {
+  const int32_t L = max(a.prefix_len[r], 0);
+  return WINDOW ? window_prefix(L, a.window, a.sinks) : L;
+}
+
 // Finds the request that owns logical index `idx`, counting either work units
 // or (kv-head, row tile) groups per request.  Every lane of the wave ends with
 // the same answer.  Returns false when idx is past the end.
+template <bool WINDOW>
 __device__ bool locate_request(int64_t idx, bool count_groups, const TreeAttnArgs &a,
                                int32_t &r_out, int64_t &unit_base, int64_t &group_base) {
   const int lane = threadIdx.x & 63;
@@ -96,7 +104,7 @@ __device__ bool locate_request(int64_t idx, bool count_groups, const TreeAttnArg
     if (r < a.num_requests) {
       int32_t n = a.node_indptr[r + 1] - a.node_indptr[r];
       n = min(max(n, 0), kMaxTreeNodes);
-      const int32_t L = window_prefix(max(a.prefix_len[r], 0), a.window, a.sinks);
+      const int32_t L = prefix_keys<WINDOW>(a, r);
       ng = (int64_t)a.num_kv_heads * row_tiles(n, a.group, a.rows_per_tile);
       nu = ng * prefix_chunks(L, chunk_keys(n, a.group, a.rows_per_tile, a.chunk_target, a.chunk_floor));
     }
@@ -128,6 +136,7 @@ struct Unit {
   int32_t r, node_base, n, L, chunk_len;
   int64_t ubase;
 };
+template <bool WINDOW>
 __device__ __forceinline__ bool find_unit(const TreeAttnArgs &a, int64_t uid, Unit &u) {
   int32_t r, node_base, n, L, chunk_len;
   int64_t ubase;
@@ -143,10 +152,10 @@ __device__ __forceinline__ bool find_unit(const TreeAttnArgs &a, int64_t uid, Un
     L = plan_prefix_len(a.plan[lo].n_and_len);
   } else {
     int64_t gbase;
-    if (!locate_request(uid, false, a, r, ubase, gbase)) return false;
+    if (!locate_request<WINDOW>(uid, false, a, r, ubase, gbase)) return false;
     node_base = a.node_indptr[r];
     n = min(max(a.node_indptr[r + 1] - node_base, 0), kMaxTreeNodes);
-    L = window_prefix(max(a.prefix_len[r], 0), a.window, a.sinks);
+    L = prefix_keys<WINDOW>(a, r);
     chunk_len = chunk_keys(n, a.group, a.rows_per_tile, a.chunk_target, a.chunk_floor);
   }
   // Request values are uniform; make that visible so branches on them stay scalar.
@@ -251,7 +260,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
   const int64_t uid = xcd_swizzle(blockIdx.x, a.padded_grid);
   if (uid >= a.units) return;
   Unit unit;
-  if (!find_unit(a, uid, unit)) return;
+  if (!find_unit<WINDOW>(a, uid, unit)) return;
   const int32_t r = unit.r, node_base = unit.node_base, n = unit.n, L = unit.L, chunk_len = unit.chunk_len;
   // a chunk is whole 32-key blocks and its page ids fit the page-id registers
   if (chunk_len <= 0 || chunk_len > kMaxChunk || chunk_len % kKeysPerBlock != 0) return;
@@ -734,10 +743,10 @@ __global__ __launch_bounds__(kThreads) void tree_attn_combine_kernel(TreeAttnArg
     if (gid >= a.row_groups) return;
     int32_t r;
     int64_t gbase;
-    if (!locate_request(gid, true, a, r, ubase, gbase)) return;
+    if (!locate_request<WINDOW>(gid, true, a, r, ubase, gbase)) return;
     node_base = a.node_indptr[r];
     n = min(max(a.node_indptr[r + 1] - node_base, 0), kMaxTreeNodes);
-    L = window_prefix(max(a.prefix_len[r], 0), a.window, a.sinks);
+    L = prefix_keys<WINDOW>(a, r);
     chunk_len = chunk_keys(n, G, RT, a.chunk_target, a.chunk_floor);
     if (n == 0) return;
     const int32_t tiles_r = row_tiles(n, G, RT);
@@ -762,18 +771,14 @@ __global__ __launch_bounds__(kThreads) void tree_attn_combine_kernel(TreeAttnArg
   for (int cc = 0; cc < chunks; ++cc) {
     const int64_t slot = (ubase + ((int64_t)cc * a.num_kv_heads + g) * tiles + tile) * kMaxRowsPerTile + rl;
     const f32x2 ml = *(const f32x2 *)(a.ws_ml + slot * 2);
-    f32x4 part[CPT / 4];
+    u32x4 raw = {0u, 0u, 0u, 0u};  // CPT bf16 values
+    f32x4 part[CPT / 4];           // or fp32 ones
     if constexpr (WINDOW) {
 #pragma unroll
       for (int k = 0; k < CPT / 4; ++k) part[k] = *(const f32x4 *)((const float *)a.ws_o + slot * D + col + 4 * k);
     } else {
-      u32x4 raw = {0u, 0u, 0u, 0u};  // CPT bf16 values
       if (CPT == 8) raw = *(const u32x4 *)(a.ws_o + slot * D + col);
       else { const u32x2 h = *(const u32x2 *)(a.ws_o + slot * D + col); raw[0] = h[0]; raw[1] = h[1]; }
-#pragma unroll
-      for (int k = 0; k < CPT / 4; ++k)
-        part[k] = f32x4{bf16_bits_to_float(raw[2 * k] & 0xffffu), bf16_bits_to_float(raw[2 * k] >> 16),
-                        bf16_bits_to_float(raw[2 * k + 1] & 0xffffu), bf16_bits_to_float(raw[2 * k + 1] >> 16)};
     }
     const float m_new = fmaxf(mm, ml[0]);
     const float sa = __builtin_amdgcn_exp2f((mm - m_new) * c);
@@ -781,7 +786,15 @@ __global__ __launch_bounds__(kThreads) void tree_attn_combine_kernel(TreeAttnArg
     mm = m_new;
     ll = ll * sa + wb;
 #pragma unroll
-    for (int k = 0; k < CPT / 4; ++k) acc[k] = acc[k] * sa + part[k] * wb;
+    for (int k = 0; k < CPT / 4; ++k) {
+      if constexpr (WINDOW) {
+        acc[k] = acc[k] * sa + part[k] * wb;
+      } else {
+        const f32x4 v = {bf16_bits_to_float(raw[2 * k] & 0xffffu), bf16_bits_to_float(raw[2 * k] >> 16),
+                         bf16_bits_to_float(raw[2 * k + 1] & 0xffffu), bf16_bits_to_float(raw[2 * k + 1] >> 16)};
+        acc[k] = acc[k] * sa + v * wb;
+      }
+    }
   }
   const float inv = ll > 0.f ? 1.f / ll : 0.f;
   const int row = tile * RT + rl;
@@ -839,7 +852,7 @@ __global__ __launch_bounds__(kWavesF32 * 64) void tree_attn_f32_kernel(TreeAttnA
   const int64_t uid = xcd_swizzle(blockIdx.x, a.padded_grid);
   if (uid >= a.units) return;
   Unit unit;
-  if (!find_unit(a, uid, unit)) return;
+  if (!find_unit<WINDOW>(a, uid, unit)) return;
   const int32_t r = unit.r, node_base = unit.node_base, n = unit.n, L = unit.L;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

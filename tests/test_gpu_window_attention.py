@@ -203,6 +203,16 @@ def test_prompt_scores_that_rise(ada, d, new, ctx, window, sinks):  # noqa: F811
     calls.check("prompt", "bf16", got, calls.expected("prompt", cache, None, q, new, ctx, 1.0, window, sinks), 3000)
 
 
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 3e-7])
+@pytest.mark.parametrize("kind", KINDS)
+def test_f32_scales(ada, kind, scale):  # noqa: F811
+    rng = np.random.default_rng(12)
+    new, ctx, window, sinks = [9, 40], [300, 65], 50, 4
+    cache, trees, q = calls.case(rng, kind, "f32", 64, 4, 2, new, ctx, window, sinks)
+    got = calls.run(ada, kind, "f32", cache, trees, q, new, ctx, scale, window, sinks)
+    calls.check(kind, "f32", got, calls.expected(kind, cache, trees, q, new, ctx, scale, window, sinks), 400)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_trees_longer_than_their_window(ada, dtype):  # noqa: F811
     """Chains, whose first nodes leave the window of the last ones, over short prefixes; some of them are sinks."""
