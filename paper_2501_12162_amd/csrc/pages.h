@@ -37,16 +37,19 @@ struct PagesArgs {
   int32_t *ws_runs;              // [runs] free pages, or pages in use, per run
 };
 
-// Caches small enough for one workgroup (pages_small.hip).  In a graph, 4096 pages,
-// one launch against three or four: update of 64 rows of 64 entries 9.4 | 11.7 us, 24 of 256
-// 8.0 | 11.4, 128 of 40 12.6 | 11.7 (its rows' second pass takes 16 at a time); fork of 128 rows of
-// 40 entries 10.0 | 10.5, 24 of 256 10.4 | 10.4, 128 of 128 18.4 | 10.5; compaction of 128 rows of
-// 128 entries 8.1 | 10.1, of 256 11.0 | 10.4.
-constexpr int kSmallPages = 4096;
-constexpr int kSmallRows = 1024;         // of either table: a thread each
-inline bool small_cache(int64_t rows, int64_t stride, int32_t pages, int64_t most_rows, int64_t most_entries) {
-  return pages <= kSmallPages && rows <= most_rows && rows * stride <= most_entries;
-}
+// Caches small enough for one workgroup (pages_small.hip), whose counts and rows'
+// scalars lie in LDS.  One launch against three or four, us on the device (in a
+// graph): update of 24 rows of 256 entries, 4096 pages 8.0 | 11.4 (in place 7.9 | 7.5),
+// 12288 pages 11.0 | 11.4 (10.2 | 7.7), of 128 rows of 40 12.6 | 11.7; fork of 24 rows
+// of 256, 4096 pages 10.3 | 10.4, 12288 12.6 | 10.7, of 128 of 128 18.4 | 10.5;
+// compaction of 128 rows of 128, 4096 pages 8.1 | 10.3, of 256 11.0 | 10.4.  A call by
+// itself takes its launches' time on the host: 8.5 | 16.6 us.
+constexpr int kSmallPages = 8192;
+constexpr int kSmallRows = 512;          // of either table
+constexpr int kSmallUpdateRows = 64;
+constexpr int kSmallCompactPages = 4096; // (places and holes lie there, too)
+constexpr int kSmallEntries = 6144;
+constexpr int kSmallCompactEntries = 24576;
 
 struct CopyPagesArgs {
   int32_t copies;

@@ -420,6 +420,12 @@ hipError_t copy_refs(const PagesArgs &a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Whether one workgroup is sooner done than several launches.
+bool small(const PagesArgs &a, int32_t rows, int64_t entries, int32_t pages) {
+  const int32_t most = a.rows > a.sources ? a.rows : a.sources;
+  return a.pages <= pages && most <= rows && (int64_t)most * a.stride <= entries;
+}
+
 hipError_t find_free(const PagesArgs &a, hipStream_t stream) {
   if (a.pages == 0) return hipSuccess;
   hipLaunchKernelGGL(free_pages_kernel, dim3(blocks_of(a.pages, 4 * kPagesRun)), dim3(kThreads), 0, stream, a);
@@ -432,7 +438,7 @@ unsigned run_bytes(const PagesArgs &a) { return blocks_of(a.pages, kPagesRun) * 
 }  // namespace
 
 hipError_t launch_update_pages(const PagesArgs &a, hipStream_t stream) {
-  if (small_cache(a.rows, a.stride, a.pages, 64, 6144)) return launch_update_small(a, stream);
+  if (small(a, kSmallUpdateRows, kSmallEntries, kSmallPages)) return launch_update_small(a, stream);
   hipError_t e = copy_refs(a, stream);
   if (e != hipSuccess || a.rows == 0) return e;
   hipLaunchKernelGGL(update_drop_kernel, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
@@ -445,7 +451,7 @@ hipError_t launch_update_pages(const PagesArgs &a, hipStream_t stream) {
 }
 
 hipError_t launch_fork_pages(const PagesArgs &a, hipStream_t stream) {
-  if (small_cache(a.rows > a.sources ? a.rows : a.sources, a.stride, a.pages, kSmallRows, 6144)) return launch_fork_small(a, stream);
+  if (small(a, kSmallRows, kSmallEntries, kSmallPages)) return launch_fork_small(a, stream);
   hipError_t e = copy_refs(a, stream);
   if (e != hipSuccess || a.rows + a.sources == 0) return e;
   hipLaunchKernelGGL(fork_rows_kernel, dim3((unsigned)(a.sources + a.rows)), dim3(kThreads), 0, stream, a);
@@ -458,7 +464,7 @@ hipError_t launch_fork_pages(const PagesArgs &a, hipStream_t stream) {
 }
 
 hipError_t launch_compact_pages(const PagesArgs &a, hipStream_t stream) {
-  if (small_cache(a.rows, a.stride, a.pages, kSmallRows, 24576)) return launch_compact_small(a, stream);
+  if (small(a, kSmallRows, kSmallCompactEntries, kSmallCompactPages)) return launch_compact_small(a, stream);
   const unsigned runs = blocks_of(a.pages, 4 * kPagesRun);
   if (runs > 0) hipLaunchKernelGGL(compact_count_kernel, dim3(runs), dim3(kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();

@@ -11,7 +11,8 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kMostWords = kSmallPages / 64;
-static_assert(kSmallPages % 64 == 0 && kMostWords <= 2 * 64, "two words of pages per lane");
+constexpr int kWordsPerLane = (kMostWords + 63) / 64;
+static_assert(kSmallRows <= kThreads, "a thread per row");
 
 __device__ __forceinline__ bool in_pool(const PagesArgs &a, int32_t p) { return p >= 0 && p < a.pages; }
 
@@ -40,12 +41,20 @@ struct PageBits {
     }
     __syncthreads();
     if (threadIdx.x < 64) {
-      const int32_t n0 = 2 * lane < words ? __popcll(word[2 * lane]) : 0;
-      const int32_t n1 = 2 * lane + 1 < words ? __popcll(word[2 * lane + 1]) : 0;
-      const int32_t upto = (int32_t)wave_inclusive_scan(n0 + n1);
-      if (2 * lane < words) before[2 * lane] = upto - n0 - n1;
-      if (2 * lane + 1 < words) before[2 * lane + 1] = upto - n1;
+      int32_t n[kWordsPerLane], sum = 0;
+#pragma unroll
+      for (int k = 0; k < kWordsPerLane; ++k) {
+        const int32_t i = lane * kWordsPerLane + k;
+        n[k] = i < words ? __popcll(word[i]) : 0;
+        sum += n[k];
+      }
+      int32_t upto = (int32_t)wave_inclusive_scan(sum);
       if (lane == 63) before[kMostWords] = upto;
+#pragma unroll
+      for (int k = kWordsPerLane - 1; k >= 0; --k) {
+        upto -= n[k];
+        if (lane * kWordsPerLane + k < words) before[lane * kWordsPerLane + k] = upto;
+      }
     }
     __syncthreads();
   }
@@ -111,7 +120,8 @@ __device__ __forceinline__ void sum_wants(int32_t *want, int32_t rows) {
 __global__ __launch_bounds__(kThreads) void update_small_kernel(PagesArgs a) {
   extern __shared__ int32_t refs[];
   __shared__ PageBits bits;
-  __shared__ int32_t want[kSmallRows], from[kSmallRows], to[kSmallRows], first[kSmallRows], last[kSmallRows];
+  __shared__ int32_t want[kSmallUpdateRows], from[kSmallUpdateRows], to[kSmallUpdateRows], first[kSmallUpdateRows],
+      last[kSmallUpdateRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t ps = a.page_size;
   load_refs(a, refs);

@@ -65,6 +65,7 @@ def same(got, expected):
     (1, 1, 1, 16, 1, 0, 1), (5, 20, 60, 16, 64, 4, 1), (7, 33, 400, 16, 100, 40, 200), (3, 600, 900, 16, 0, 0, 5000),
     (40, 50, 900, 16, 33, 1, 400), (4, 9, 30, 1, 3, 2, 4), (6, 300, 20000, 7, 50, 5, 2100), (2, 5000, 40000, 16, 4096, 4, 70000),
     (1500, 6, 3000, 16, 20, 4, 90), (20, 40, 300, 16, 2 ** 31 - 1, 0, 300), (20, 40, 300, 16, 5, 2 ** 31 - 1, 300),
+    (64, 96, 8192, 16, 100, 4, 900), (64, 96, 8193, 16, 100, 4, 900), (65, 90, 4000, 16, 100, 4, 300), (64, 97, 4000, 16, 100, 4, 300),
 ])
 def test_update(ada, rows, stride, pages, ps, window, sinks, grow, in_place):  # noqa: F811
     rng = np.random.default_rng([rows, stride, pages, window % 1000])
@@ -123,7 +124,8 @@ def fork(ada, source, lens, ps, table, refs, in_place=False):  # noqa: F811
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("sources,rows,stride,pages,ps", [
     (1, 1, 1, 2, 16), (1, 8, 40, 60, 16), (8, 8, 20, 170, 16), (64, 64, 30, 2100, 16), (3, 1300, 4, 900, 16), (1100, 20, 3, 3400, 16),
-    (5, 9, 300, 20000, 1), (4, 4, 9, 36, 5), (6, 30, 7, 44, 16),
+    (5, 9, 300, 20000, 1), (4, 4, 9, 36, 5), (6, 30, 7, 44, 16), (512, 500, 12, 8192, 16), (500, 512, 12, 8193, 16),
+    (513, 40, 11, 5000, 16), (40, 513, 11, 5000, 16),
 ])
 def test_fork(ada, sources, rows, stride, pages, ps, in_place):  # noqa: F811
     rng = np.random.default_rng([sources, rows, stride])
@@ -164,7 +166,7 @@ def compact(ada, table, refs, in_place=False):  # noqa: F811
 
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("used", [0.0, 0.03, 0.5, 0.97, 1.0])
-@pytest.mark.parametrize("pages", [0, 1, 63, 64, 1024, 1025, 5000, 70001])
+@pytest.mark.parametrize("pages", [0, 1, 63, 64, 1024, 1025, 4096, 4097, 70001])
 def test_compact(ada, pages, used, in_place):  # noqa: F811
     rng = np.random.default_rng([pages, int(used * 100)])
     refs = np.where(rng.random(pages) < used, rng.integers(1, 4, pages), -rng.integers(0, 2, pages)).astype(np.int32)
