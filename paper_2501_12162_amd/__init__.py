@@ -325,7 +325,7 @@ def _pointers(dense, strided=()):
             pointers.append(None)
             continue
         at = t.get_device()
-        if at != device:
+        if at != device or at < 0:
             if at < 0 or device >= 0:
                 raise ValueError("expected a device tensor" if at < 0 else "tensors are on different devices")
             device = at
@@ -610,7 +610,7 @@ def _int32s(shaped):
         if t.dtype is not int32 or t.shape != shape:
             raise ValueError("%s must be int32 %s, is %s %s" % (name, list(shape), t.dtype, list(t.shape)))
         at = t.get_device()
-        if at != device:
+        if at != device or at < 0:
             if at < 0 or device >= 0:
                 raise ValueError("expected a device tensor" if at < 0 else "tensors are on different devices")
             device = at
