@@ -618,8 +618,9 @@ int32_t adaserve_sample(const void *logits, int64_t row_stride, int32_t num_rows
  *     root-to-node path a node sees those that its position sees.
  *
  * Everything else -- layouts, types, head groups, roundings, limits, zero pages,
- * lengths on the host and on the device, workspaces -- is as in those calls; rows of q
- * may lie apart in the first two.  Pages that hold no position seen by any row of
+ * lengths on the host and on the device, workspaces -- is as in those calls, but that
+ * the chunks of a split prefix keep their outputs in fp32; rows of q may lie apart in
+ * the first two.  Pages that hold no position seen by any row of
  * their request are not read, nor their block-table entries used: they may have
  * been freed (adaserve_update_pages), given to other requests or hold anything.
  * A position that a row does not see adds nothing to it, whatever key and value

@@ -37,6 +37,10 @@
 // the first two took 124 and 169 us; with three workgroups per CU (168 registers,
 // 8 of them spilled) 130 and 185.  Loading a run's first block before the end of
 // the run before gains nothing: 111 and 166.
+//
+// Over a window and sinks (WINDOW) the shares are of the blocks that are read, the sinks' and
+// the window's, numbered through.  64 requests of up to 16384 tokens over 2048, 64 on 8
+// heads, 530 MB: 86 us and 5 for the join; one of 20001 over 4096: 8.3 and 3.7.
 #include <float.h>
 
 #include <type_traits>

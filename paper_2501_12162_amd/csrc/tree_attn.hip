@@ -38,6 +38,11 @@
 //    denominator in fp32) and a second, fully parallel kernel merges them
 //    (the kernel boundary makes the partials of every XCD visible without
 //    per-workgroup cache flushes).
+//  * over a window and sinks (WINDOW) the prefix's blocks are the sinks' and those
+//    from the root's window on, numbered through; node i, at position L + depth,
+//    sees the prefix from its depth later on, and of its path what its position
+//    sees (16 trees of 16-64 nodes over 2048 of up to 20000 keys, 32 / 8 heads: 47 us
+//    and 8 for the merge; 4 fp32 ones over 255 keys 14.5).
 #include <float.h>
 
 #include <mutex>
@@ -660,7 +665,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_bf16_kernel(TreeAttnArg
   // tree_attn_combine_kernel merges the chunks after this kernel.
   // Over a window, whose calls are short and their partials few, they are fp32:
   // no rounding but those of P and the output (16 trees over windows of 2048, error
-  // against fp64 0.0029 -> 0.0021).
+  // against fp64 0.0029 -> 0.0023).
   const int64_t pslot = uid * kMaxRowsPerTile + (row - row0);
   if (WINDOW && chunks > 1) {
     if (row_valid) {
