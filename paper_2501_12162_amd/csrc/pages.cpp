@@ -233,11 +233,12 @@ int32_t adaserve_copy_pages(int32_t num_copies, const int32_t *src, const int32_
   if (page_bytes > (int64_t)1 << 30)
     return fail(ADASERVE_ERR_UNSUPPORTED, "pages of %lld bytes exceed 2^30", (long long)page_bytes);
   if (num_layers > 1) {
-    if (layer_stride < page_bytes / esz * num_pages || layer_stride * esz % 16 != 0)
-      return fail(ADASERVE_ERR_INVALID_ARGUMENT, "layer_stride %lld: less than a pool, or not a multiple of 16 bytes",
-                  (long long)layer_stride);
+    // (its range first: the products with the element's size are within 64 bits then)
     if (layer_stride > ((int64_t)1 << 48) / num_layers)
       return fail(ADASERVE_ERR_UNSUPPORTED, "%d layers %lld elements apart span more than 2^48 elements", num_layers,
+                  (long long)layer_stride);
+    if (layer_stride < page_bytes / esz * num_pages || layer_stride * esz % 16 != 0)
+      return fail(ADASERVE_ERR_INVALID_ARGUMENT, "layer_stride %lld: less than a pool, or not a multiple of 16 bytes",
                   (long long)layer_stride);
   }
   if (num_copies == 0 || num_layers == 0 || num_pages == 0) return ADASERVE_OK;
@@ -254,7 +255,7 @@ int32_t adaserve_copy_pages(int32_t num_copies, const int32_t *src, const int32_
   a.pool[0] = (char *)k_pages;
   a.pool[1] = (char *)v_pages;
   a.layers = num_layers;
-  a.layer_bytes = layer_stride * esz;
+  a.layer_bytes = num_layers > 1 ? layer_stride * esz : 0;
   a.page_bytes = page_bytes;
   a.pages = num_pages;
   return launch_status(launch_copy_pages(a, (hipStream_t)stream), "page copy launch");

@@ -1,0 +1,20 @@
+"""Arguments of the pages' entry points at the ends of their types, on the host before any HIP call."""
+import pytest
+
+import paper_2501_12162_amd as ada
+from test_abi_window import BAD, UNSUP, _copy, lib  # noqa: F401  (a fixture)
+
+INT64_MAX = 2 ** 63 - 1
+
+
+@pytest.mark.parametrize("dtype", [ada.ADASERVE_BF16, ada.ADASERVE_F32])
+@pytest.mark.parametrize("stride,code", [(2 ** 62, UNSUP), (2 ** 61, UNSUP), (INT64_MAX, UNSUP), (INT64_MAX - 15, UNSUP),
+                                         (2 ** 47 + 16, UNSUP), (2 ** 47 - 1, BAD), (-1, BAD), (-INT64_MAX - 1, BAD)])
+def test_layer_strides_beyond_any_pool(lib, stride, code, dtype):  # noqa: F811
+    """Their bytes do not fit 64 bits: refused without a product that overflows."""
+    assert _copy(lib, stride=stride, dtype=dtype) == code and lib.adaserve_last_error()
+
+
+def test_nothing_to_copy_at_any_stride(lib):  # noqa: F811
+    for stride in (INT64_MAX, -INT64_MAX - 1):
+        assert _copy(lib, n=0, layers=1, stride=stride) == 0
