@@ -53,9 +53,10 @@ int32_t validate_page_size(int32_t page_size) {
   return ADASERVE_OK;
 }
 
-// The workspace's parts, after its checks.
+// The workspace's parts, after its checks; none of a call without rows and pages.
 int32_t set_space(PagesArgs &a, int32_t rows, int32_t num_pages, void *workspace, size_t given) {
   const PagesSpace s = pages_space(rows, num_pages);
+  if (s.bytes == 0) return ADASERVE_OK;
   if (!workspace || given < s.bytes)
     return fail(ADASERVE_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace ? given : (size_t)0, s.bytes);
   if (!aligned(workspace, 256)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "workspace must be 256-byte aligned");

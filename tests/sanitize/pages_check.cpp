@@ -28,7 +28,10 @@ const char *hipGetErrorString(hipError_t) { return ""; }
 namespace adaserve {
 hipError_t launch_update_pages(const PagesArgs &, hipStream_t) { return hipSuccess; }
 hipError_t launch_fork_pages(const PagesArgs &, hipStream_t) { return hipSuccess; }
-hipError_t launch_compact_pages(const PagesArgs &, hipStream_t) { return hipSuccess; }
+hipError_t launch_compact_pages(const PagesArgs &, hipStream_t) {
+  ++launches;   // (the counts of an empty pool are written, too)
+  return hipSuccess;
+}
 hipError_t launch_copy_pages(const CopyPagesArgs &a, hipStream_t) {
   launched = a;
   ++launches;
@@ -66,5 +69,21 @@ int main() {
     CHECK(launches == 6);
     launches = 0;
   }
+  // nothing at all: no bytes of workspace are needed, and none are asked for
+  CHECK(adaserve_pages_workspace_bytes(0, 0) == 0);
+  int32_t *const counts = (int32_t *)at(1);
+  for (void *workspace : {(void *)nullptr, (void *)at(2)}) {
+    CHECK(adaserve_update_pages(0, nullptr, nullptr, 0, 0, 16, nullptr, 4, nullptr, 0, nullptr, nullptr, nullptr, workspace, 0,
+                                nullptr) == ADASERVE_OK);
+    CHECK(adaserve_fork_pages(0, 0, nullptr, nullptr, 16, nullptr, 4, nullptr, 0, nullptr, nullptr, nullptr, nullptr, nullptr,
+                              workspace, 0, nullptr) == ADASERVE_OK);
+    CHECK(launches == 0);
+    CHECK(adaserve_compact_pages(0, nullptr, 4, nullptr, 0, nullptr, nullptr, nullptr, nullptr, nullptr, counts, workspace, 0,
+                                 nullptr) == ADASERVE_OK);
+    CHECK(launches == 1);
+    launches = 0;
+  }
+  CHECK(adaserve_compact_pages(1, counts, 1, nullptr, 0, counts, nullptr, nullptr, nullptr, nullptr, (int32_t *)at(3), nullptr, 0,
+                               nullptr) == ADASERVE_ERR_WORKSPACE);
   std::printf("pages checks passed\n");
 }

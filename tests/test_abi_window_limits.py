@@ -18,3 +18,10 @@ def test_layer_strides_beyond_any_pool(lib, stride, code, dtype):  # noqa: F811
 def test_nothing_to_copy_at_any_stride(lib):  # noqa: F811
     for stride in (INT64_MAX, -INT64_MAX - 1):
         assert _copy(lib, n=0, layers=1, stride=stride) == 0
+
+
+def test_calls_of_nothing_take_no_workspace(lib):  # noqa: F811
+    """No rows and no pages need 0 bytes, and a tensor of 0 bytes has no address."""
+    assert lib.adaserve_pages_workspace_bytes(0, 0) == 0
+    assert lib.adaserve_update_pages(0, None, None, 0, 0, 16, None, 4, None, 0, None, None, None, None, 0, None) == 0
+    assert lib.adaserve_fork_pages(0, 0, None, None, 16, None, 4, None, 0, None, None, None, None, None, None, 0, None) == 0
