@@ -29,7 +29,8 @@ int32_t validate_arrays(const Array *a, int n) {
     if (!aligned(a[i].p, 4)) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "%s is not aligned to its elements", a[i].name);
     for (int k = 0; k < i; ++k) {
       const char *x = (const char *)a[i].p, *y = (const char *)a[k].p;
-      if (!x || !y || !(a[i].output || a[k].output) || x >= y + a[k].bytes || y >= x + a[i].bytes) continue;
+      if (a[i].bytes == 0 || a[k].bytes == 0 || !(a[i].output || a[k].output)) continue;
+      if (x >= y + a[k].bytes || y >= x + a[i].bytes) continue;
       if (x == y && (a[i].same == y || a[k].same == x)) continue;
       return fail(ADASERVE_ERR_INVALID_ARGUMENT, "%s overlaps %s", a[i].name, a[k].name);
     }

@@ -2,7 +2,7 @@
 import pytest
 
 import paper_2501_12162_amd as ada
-from test_abi_window import BAD, UNSUP, _copy, lib  # noqa: F401  (a fixture)
+from test_abi_window import BAD, UNSUP, _compact, _copy, _fork, _update, at, lib  # noqa: F401  (a fixture)
 
 INT64_MAX = 2 ** 63 - 1
 
@@ -25,3 +25,12 @@ def test_calls_of_nothing_take_no_workspace(lib):  # noqa: F811
     assert lib.adaserve_pages_workspace_bytes(0, 0) == 0
     assert lib.adaserve_update_pages(0, None, None, 0, 0, 16, None, 4, None, 0, None, None, None, None, 0, None) == 0
     assert lib.adaserve_fork_pages(0, 0, None, None, 16, None, 4, None, 0, None, None, None, None, None, None, 0, None) == 0
+
+
+def test_arrays_of_nothing_overlap_nothing(lib):  # noqa: F811
+    """Tables of no entries whose addresses lie within other arrays: calls fail for what they lack, not for these."""
+    inside = at(4) + 16
+    assert _update(lib, bts=0, bt=inside, nbt=inside, cap=at(1)) == BAD and b"capacity overlaps context_len" in lib.adaserve_last_error()
+    assert _fork(lib, bts=0, bt=inside, nbt=inside, cs=at(9)) == BAD and b"copy_dst overlaps copy_src" in lib.adaserve_last_error()
+    assert _compact(lib, bts=0, bt=at(2) + 4, nbt=at(2) + 4, ms=at(7)) == BAD
+    assert b"move_dst overlaps move_src" in lib.adaserve_last_error()
