@@ -29,14 +29,14 @@ const char *last_error_message() { return g_last_error.c_str(); }
 
 size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-// Scalar and host-mirror validation shared by the workspace query and the
-// verify call.  Does not touch device memory.
 int32_t validate_window(int32_t window, int32_t sinks) {
   if (window < 1) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "window %d < 1", window);
   if (sinks < 0) return fail(ADASERVE_ERR_INVALID_ARGUMENT, "sinks %d < 0", sinks);
   return ADASERVE_OK;
 }
 
+// Scalar and host-mirror validation shared by the workspace query and the
+// verify call.  Does not touch device memory.
 int32_t validate_attn_shape(int32_t num_requests, const int32_t *indptr_host, const int32_t *plen_host,
                             int32_t hq, int32_t hkv, int32_t head_dim, int32_t page_size, int32_t dtype,
                             int32_t bt_stride_or_neg, AttnShape &shape) {
