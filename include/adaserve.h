@@ -619,10 +619,15 @@ int32_t adaserve_sample(const void *logits, int64_t row_stride, int32_t num_rows
  *
  * Everything else -- layouts, types, head groups, roundings, limits, zero pages,
  * lengths on the host and on the device, workspaces -- is as in those calls, but that
- * the chunks of a split prefix keep their outputs in fp32; rows of q may lie apart in
- * the first two.  Pages that hold no position seen by any row of
- * their request are not read, nor their block-table entries used: they may have
- * been freed (adaserve_update_pages), given to other requests or hold anything.
+ * in trees the chunks of a split prefix keep their outputs in fp32; rows of q may lie
+ * apart in the first two.  Where the window or the sinks reach every position of the
+ * batch (of max_context, in the second), the call is the one without a window, bit for
+ * bit, with that call's bf16 chunks.
+ * Pages that hold no position seen by any row of their request add nothing, whatever
+ * they hold and whatever their block-table entries say: they may have been freed
+ * (adaserve_update_pages) and given to other requests.  (Keys are taken 32 positions
+ * together, so such a page beside one that is seen may be loaded, where its entry
+ * names one of the pool, and is then masked.)
  * A position that a row does not see adds nothing to it, whatever key and value
  * it holds; in BF16 trees that is so for prefix positions that no node of the
  * request sees and for nodes past the request's, and the values of the others must
