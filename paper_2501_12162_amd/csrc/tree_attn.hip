@@ -1212,7 +1212,7 @@ __global__ __launch_bounds__(kWavesF32 * 64) void tree_attn_f32_kernel(TreeAttnA
     }
     const int node = row / G, hh = row - node * G;
     f32x4 res = {0.f, 0.f, 0.f, 0.f};
-    if (den > 0.f) res = acc / den;
+    if (den != 0.f) res = acc / den;   // (a NaN stays one)
     *(f32x4 *)((float *)a.out + ((int64_t)(node_base + node) * a.num_q_heads + g * G + hh) * D + col) = res;
   }
 }
