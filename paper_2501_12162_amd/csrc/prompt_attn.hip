@@ -635,8 +635,11 @@ __global__ __launch_bounds__(kThreads, 1) void prompt_attn_bf16_kernel(PromptAtt
       const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
       const int32_t tok = ok ? row / G : 0, head = done.g * G + (ok ? row - tok * G : 0);
       // A key that the row does not see has weight 0, and 0 times an infinite
-      // value is NaN: such rows are taken again, key by key.
-      const bool again = ok && is_nan(rt) && !had_nan[rt];
+      // value is NaN: such rows are taken again, key by key.  (Over a window: but for
+      // those whose sum of weights is NaN, as it is by keys that the row sees alone.
+      // With a NaN in a sink's key every row was taken again: 16384 of them over 8192 keys, 32
+      // heads, in 751 ms; 3.6 now.)
+      const bool again = ok && is_nan(rt) && !(WINDOW ? l_tot != l_tot : had_nan[rt]);
       if (a.chunks > 1) {
         // the chunk's part: sums, and (reference in log2 units, sum of weights);
         // an infinite reference has the join take the row again
@@ -926,8 +929,9 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_f32_kernel(PromptAttnArg
     const int rl = rb * 16 + j;
     const float ls = sum_over_lane_rows(l[rb]);
     // a key that the row does not see has weight 0, and 0 times an infinite value
-    // is NaN: such rows are taken again, key by key
-    if ((WINDOW || b1 > n_full) && is_nan(rb) && !had_nan[rb]) taken[rl] = 1;
+    // is NaN: such rows are taken again, key by key (over a window but for those
+    // whose sum of weights is NaN)
+    if ((WINDOW || b1 > n_full) && is_nan(rb) && !(WINDOW ? ls != ls : had_nan[rb])) taken[rl] = 1;
     if (q == 0) {
       mw[wave][rl] = m[rb];
       lw[wave][rl] = ls;

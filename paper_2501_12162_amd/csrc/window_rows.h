@@ -100,6 +100,10 @@ __device__ __forceinline__ void attend_keys(const void *q, int64_t count, At at,
 #pragma unroll
       for (int i = 0; i < N; ++i) o[i] = __builtin_fmaf(wj, value(v, lane + i * 64), o[i]);
     }
+    bool nan = true;   // (in all columns: whatever comes, they stay so)
+#pragma unroll
+    for (int i = 0; i < N; ++i) nan = nan && (l != l || o[i] != o[i]);
+    if (__all(nan)) break;
     row_sync();
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;   // (a NaN stays one)
