@@ -43,7 +43,8 @@ struct PagesArgs {
 // 12288 pages 11.0 | 11.4 (10.2 | 7.7), of 128 rows of 40 12.6 | 11.7; fork of 24 rows
 // of 256, 4096 pages 10.3 | 10.4, 12288 12.6 | 10.7, of 128 of 128 18.4 | 10.5;
 // compaction of 128 rows of 128, 4096 pages 8.1 | 10.3, of 256 11.0 | 10.4.  A call by
-// itself takes its launches' time on the host: 8.5 | 16.6 us.
+// itself takes its launches' time on the host: 8.5 | 16.6 us.  The limits are where the times in a
+// graph meet, but for the entries of an update, which are those of forks: none beyond them were measured.
 constexpr int kSmallPages = 8192;
 constexpr int kSmallRows = 512;          // of either table
 constexpr int kSmallUpdateRows = 64;
